@@ -54,8 +54,8 @@ typedef enum {
   MW_EINVAL = -1,        /* null pointer, non-positive size, inconsistent sizes */
   MW_EUNSUPPORTED = -2,  /* head dimension other than 64, 72 or 128, or a limit exceeded */
   MW_EALIGN = -3,        /* a pointer that is not 16-byte aligned */
-  MW_EFULL = -4,         /* append to a ring whose slots are all live */
-  MW_EEMPTY = -5,        /* evict more chunks than are live */
+  MW_EFULL = -4,         /* append to a ring whose slots are all live, or with too few free pages */
+  MW_EEMPTY = -5,        /* evict more chunks (or full pages) than are live */
   MW_EHIP = -6           /* the HIP runtime reported an error at launch */
 } mw_status;
 
@@ -84,6 +84,9 @@ typedef struct {
 #define MW_MAX_QUEUED 64
 /* Largest ring of an e4m3 cache (its per-slot re-shift record, below). */
 #define MW_MAX_SLOTS 128
+/* Tokens of a page that share a scale, and sequences one paged call can name. */
+#define MW_PAGE_BLOCK 64
+#define MW_MAX_SEQS 256
 
 /* ------------------------------------------------------------------------
  * Training: block-causal attention (Sec. 3.2).
@@ -419,6 +422,169 @@ int mw_chunk_attn_cached_fp8(const void* q8, const void* k8_new, const void* v8_
                              const mw_kvcache* c, int window, int flags, void* o, float* lse, float scale,
                              float q_scale, void* workspace, size_t workspace_bytes, const mw_strides* o_strides,
                              mw_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Cross attention: the tokens' queries attend to an encoder's states (text,
+ * actions, another view), a sequence of another length.
+ *
+ * H query heads share Hkv key heads (Hkv divides H): query head h reads key head
+ * h / (H / Hkv).  With S = scale * Q K^T over the first kv_len[b] states of batch
+ * member b (every state where kv_len is NULL):
+ *     O = softmax(S) V,  LSE = log(sum_j exp(S_ij))
+ * A batch member without a state (kv_len[b] <= 0) has O = 0 and LSE = -inf.
+ *
+ * q, o     : bf16 [B, H, T, D];  k, v : bf16 [B, Hkv, M, D]
+ * kv_len   : int32 [B] in device memory, or NULL.  Values are taken as at most M.
+ *            States behind kv_len[b] are not read: they may hold anything.
+ * lse      : fp32 [B, H, T], or NULL
+ * strides  : 4 entries, for q, k, v, o (NULL = all contiguous).  A k or v stride
+ *            of 0 shares the states between batch members or heads.
+ * workspace: optional.  With mw_cross_attn_workspace_size(...) bytes the keys of a
+ *            call of few rows are split over several workgroups, as in
+ *            mw_chunk_attn_cached; NULL or a smaller buffer: fewer ranges.
+ * D        : 64, 72 or 128.  T = 1 (one token) and M = 1 are ordinary sizes.
+ * Arithmetic as in mw_block_causal_attn_fwd.  The calling thread's current device
+ * must be the device of the stream and of the tensors.
+ * Errors: MW_EINVAL (null q, k, v or o, sizes < 1, H not a multiple of Hkv, scale
+ * not finite and > 0, the stride checks of mw_strides), MW_EALIGN,
+ * MW_EUNSUPPORTED (D; T * H / Hkv or M above 2^24), MW_EHIP.
+ * ---------------------------------------------------------------------- */
+size_t mw_cross_attn_workspace_size(int B, int H, int Hkv, int T, int M, int D);
+int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t* kv_len, void* o, float* lse,
+                      const mw_strides* strides, int B, int H, int Hkv, int T, int M, int D, float scale,
+                      void* workspace, size_t workspace_bytes, mw_stream_t stream);
+
+/* Bytes of device workspace mw_cross_attn_bwd needs: two fp32 for each row, and the
+ * fp32 dK and dV of the slices the rows are cut into. */
+size_t mw_cross_attn_bwd_workspace_size(int B, int H, int Hkv, int T, int M, int D);
+
+/* Backward of mw_cross_attn_fwd for the loss sum(dO * O): dQ, and dK and dV summed
+ * over the query heads that share a key head.  Gradients of states behind
+ * kv_len[b] are 0, and so is all of dQ of a member without a state.
+ * q, k, v, kv_len, o, lse : as given to and left by the forward
+ * d_o : bf16 [B, H, T, D];  dq : bf16 [B, H, T, D], dk, dv : bf16 [B, Hkv, M, D],
+ *       written (not accumulated).  Where the forward read states shared between
+ *       batch members, dk and dv still hold each member's own gradient.
+ * strides : 8 entries, for q, k, v, o, d_o, dq, dk, dv (NULL = all contiguous)
+ * The result is deterministic (no atomics).
+ * Errors: as the forward, plus MW_EINVAL for a null pointer or a workspace too small. */
+int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t* kv_len, const void* o,
+                      const void* d_o, const float* lse, void* dq, void* dk, void* dv, void* workspace,
+                      size_t workspace_bytes, const mw_strides* strides, int B, int H, int Hkv, int T, int M, int D,
+                      float scale, mw_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Paged 8-bit cache with a scale for each block of tokens and head.
+ *
+ * A pool of P pages of L tokens each holds the keys and values of up to N
+ * sequences; sequence s is the list of pages table[s], of which it fills lens[s]
+ * tokens.  Sequences may share pages (mw_kvpages_fork), differ in length, and grow
+ * by any number of tokens: branches of one rollout keep their common history once.
+ *
+ * Keys and values are e4m3 codes with a scale for each MW_PAGE_BLOCK = 64 tokens of
+ * a page and head:
+ *     scale = 2^e, e the least integer with max|x| <= 448 * 2^e (within [-100, 100]),
+ *     code  = RNE_e4m3(clamp(x / scale, -448, 448)),  value = code * scale.
+ * Powers of two, so that the quotient, the product and a later change of scale are
+ * exact (but for codes that become subnormal), and a value is exact in bf16: the
+ * attention reads precisely the values the cache stands for.  Tokens appended
+ * behind others in a block may raise its scale; the older codes are then rounded
+ * again as RNE_e4m3(code * 2^(e_old - e)).  Infinities saturate, a NaN stays NaN
+ * and leaves the scale to the block's other values.
+ *
+ * Who owns which page is kept in the caller's host memory; the device's copy of the
+ * table and lengths is written by the calls' kernels in stream order, so the calls on
+ * one cache go to one stream (or streams that wait for each other), from one thread
+ * at a time, and with the stream's device current.  Pages are taken lowest index first.
+ * Operations that change a cache must run outside HIP graph capture; a captured
+ * mw_chunk_attn_paged reads the table and lengths as they are when it is replayed.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  void* k_pages;   /* e4m3 [P, H, L, D] */
+  void* v_pages;
+  float* k_scales; /* fp32 [P, H, L / 64] */
+  float* v_scales;
+  int32_t* table;  /* device int32 [N, W]: pages of each sequence, in token order */
+  int32_t* lens;   /* device int32 [N]: tokens of each sequence */
+  int32_t* host;   /* host memory of mw_kvpages_host_bytes(P, N, W) bytes */
+  int P, H, L, D, N, W;
+} mw_kvpages;
+
+/* Bytes of host memory the bookkeeping takes (0 for sizes out of range). */
+size_t mw_kvpages_host_bytes(int P, int N, int W);
+
+/* Initialise an empty cache over caller-owned buffers: N sequences of at most W pages.
+ * The caller has cleared lens (all zeros); no device work.  L: a multiple of 64.
+ * D: 64, 72 or 128.
+ * Errors: MW_EINVAL (null, sizes < 1, L, host block too small), MW_EALIGN,
+ * MW_EUNSUPPORTED (D; P > 2^24, N > 2^16, H > 2^14, W * L > 2^24, N * W > 2^28 or
+ * H * L * D > 2^30). */
+int mw_kvpages_init(mw_kvpages* c, void* k_pages, void* v_pages, float* k_scales, float* v_scales, int32_t* table,
+                    int32_t* lens, int32_t* host, size_t host_bytes, int P, int H, int L, int D, int N, int W);
+
+/* Tokens of a sequence; free pages; the page that holds entry `index` of a sequence.
+ * Host only; a negative mw_status for an invalid cache, sequence or index. */
+int mw_kvpages_len(const mw_kvpages* c, int seq);
+int mw_kvpages_n_free(const mw_kvpages* c);
+int mw_kvpages_page_of(const mw_kvpages* c, int seq, int index);
+
+/* Commit n_tokens >= 1 tokens to the end of each listed sequence (n_seqs different
+ * ones): k, v : bf16 [n_seqs, H, n_tokens, D] views (strides: 2 entries, NULL =
+ * contiguous).  A partly filled last page that other sequences share is first taken
+ * over into a page of the sequence's own (copy on write, by every listed sequence
+ * that shares it at the time of the call).  All or nothing.
+ * Errors: MW_EINVAL (also a sequence out of range or listed twice), MW_EALIGN,
+ * MW_EFULL (too few free pages, or a row of W pages exceeded), MW_EUNSUPPORTED
+ * (n_seqs > MW_MAX_SEQS), MW_EHIP. */
+int mw_kvpages_append(mw_kvpages* c, const int32_t* seqs, int n_seqs, const void* k, const void* v,
+                      const mw_strides* strides, int n_tokens, mw_stream_t stream);
+
+/* Make the empty sequence dst a branch of src: it shares src's pages.
+ * Errors: MW_EINVAL (src = dst, dst not empty, out of range), MW_EHIP. */
+int mw_kvpages_fork(mw_kvpages* c, int src, int dst, mw_stream_t stream);
+
+/* Make the empty sequence dst a copy of src in pages of its own (as a snapshot that
+ * shares nothing).  Errors: as fork, plus MW_EFULL. */
+int mw_kvpages_copy(mw_kvpages* c, int src, int dst, mw_stream_t stream);
+
+/* Empty the listed sequences (n_seqs different ones); pages that no other sequence
+ * shares become free.  Errors: MW_EINVAL, MW_EUNSUPPORTED, MW_EHIP. */
+int mw_kvpages_free(mw_kvpages* c, const int32_t* seqs, int n_seqs, mw_stream_t stream);
+
+/* Drop the full pages [first_page, first_page + n_pages) of a sequence: the rolling
+ * window, with first_page > 0 behind an anchor that is kept.  The tokens behind them
+ * move up in the list; their keys stay as committed.
+ * Errors: MW_EINVAL, MW_EEMPTY (not that many full pages), MW_EHIP. */
+int mw_kvpages_evict(mw_kvpages* c, int seq, int first_page, int n_pages, mw_stream_t stream);
+
+/* Move live pages so that they are the pool's first ones (what is behind them can then
+ * be given back or lent out).  Returns the number of pages moved, or a negative status.
+ * Errors: MW_EINVAL, MW_EHIP. */
+int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
+
+/* Cached chunk attention over the pages: batch member b attends to the tokens of
+ * sequence seqs[b] (host array, n_seqs <= MW_MAX_SEQS entries, repeats allowed) and
+ * to the queued tokens' own keys, under the visibility rules of mw_chunk_attn_cached:
+ * every queued token sees all cached ones; of the queued ones those of chunks up to
+ * its own (MW_QUEUED_CAUSAL; with q_len = 1 the token-causal rule) or of its own
+ * chunk (MW_QUEUED_ISOLATED).
+ * q, o         : bf16 [n_seqs, H, n_queued * q_len, D]; the cache's H heads are shared
+ *                by H / cache->H query heads each
+ * k_new, v_new : bf16 [n_seqs, cache->H, n_queued * q_len, D], or both NULL: the
+ *                cached tokens alone (O = 0, LSE = -inf where there are none)
+ * lse          : fp32 [n_seqs, H, n_queued * q_len], or NULL
+ * workspace    : optional, as in mw_chunk_attn_cached; sized for the sequences'
+ *                present lengths by mw_chunk_attn_paged_workspace_size
+ * strides      : 4 entries, for q, k_new, v_new, o (NULL = all contiguous)
+ * Arithmetic as in mw_chunk_attn_cached over the values of the codes.
+ * Errors: MW_EINVAL, MW_EALIGN, MW_EUNSUPPORTED (n_queued > MW_MAX_QUEUED, n_seqs >
+ * MW_MAX_SEQS, sizes), MW_EHIP. */
+size_t mw_chunk_attn_paged_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int n_queued,
+                                          int q_len);
+int mw_chunk_attn_paged(const void* q, const void* k_new, const void* v_new, int n_queued, int q_len,
+                        const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int flags, void* o, float* lse,
+                        float scale, void* workspace, size_t workspace_bytes, const mw_strides* strides,
+                        mw_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Pipelined denoising schedule (Sec. 3.5, "Pipelined Denoising" and the

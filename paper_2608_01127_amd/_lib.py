@@ -7,6 +7,7 @@ exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -27,6 +28,8 @@ MW_QUEUED_ISOLATED = 1
 MW_MAX_WINDOW = 64
 MW_MAX_QUEUED = 64
 MW_MAX_SLOTS = 128
+MW_PAGE_BLOCK = 64
+MW_MAX_SEQS = 256
 
 STATUS_NAMES = {0: "MW_OK", -1: "MW_EINVAL", -2: "MW_EUNSUPPORTED", -3: "MW_EALIGN", -4: "MW_EFULL",
                 -5: "MW_EEMPTY", -6: "MW_EHIP"}
@@ -47,6 +50,13 @@ class mw_kvcache(ctypes.Structure):
                 ("rope_total", ctypes.c_int64), ("rope_offset", ctypes.c_int), ("rope_count", ctypes.c_int),
                 ("rope_theta", ctypes.c_float), ("rope_set", ctypes.c_int),
                 ("rope_at_commit", ctypes.c_int64 * MW_MAX_SLOTS)]
+
+
+class mw_kvpages(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("host", ctypes.c_void_p), ("P", ctypes.c_int), ("H", ctypes.c_int), ("L", ctypes.c_int),
+                ("D", ctypes.c_int), ("N", ctypes.c_int), ("W", ctypes.c_int)]
 
 
 class mw_rope(ctypes.Structure):
@@ -76,6 +86,8 @@ _vp, _i, _f, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_size_
 _ip = ctypes.POINTER(ctypes.c_int)
 _cache_p = ctypes.POINTER(mw_kvcache)
 _str_p = ctypes.POINTER(mw_strides)
+_pages_p = ctypes.POINTER(mw_kvpages)
+_seq_p = ctypes.POINTER(ctypes.c_int32)
 SIGNATURES = {
     "mw_last_error": ([], ctypes.c_char_p),
     "mw_version": ([], _i),
@@ -102,6 +114,23 @@ SIGNATURES = {
     "mw_kvcache_init_fp8": ([_cache_p, _vp, _vp, _i, _i, _i, _i, _i, _f, _f], _i),
     "mw_chunk_attn_cached_fp8": ([_vp, _vp, _vp, _i, _i, _cache_p, _i, _i, _vp, _vp, _f, _f, _vp, _sz, _str_p, _vp],
                                  _i),
+    "mw_cross_attn_workspace_size": ([_i] * 6, _sz),
+    "mw_cross_attn_fwd": ([_vp] * 6 + [_str_p] + [_i] * 6 + [_f, _vp, _sz, _vp], _i),
+    "mw_cross_attn_bwd_workspace_size": ([_i] * 6, _sz),
+    "mw_cross_attn_bwd": ([_vp] * 11 + [_sz, _str_p] + [_i] * 6 + [_f, _vp], _i),
+    "mw_kvpages_host_bytes": ([_i, _i, _i], _sz),
+    "mw_kvpages_init": ([_pages_p] + [_vp] * 7 + [_sz] + [_i] * 6, _i),
+    "mw_kvpages_len": ([_pages_p, _i], _i),
+    "mw_kvpages_n_free": ([_pages_p], _i),
+    "mw_kvpages_page_of": ([_pages_p, _i, _i], _i),
+    "mw_kvpages_append": ([_pages_p, _seq_p, _i, _vp, _vp, _str_p, _i, _vp], _i),
+    "mw_kvpages_fork": ([_pages_p, _i, _i, _vp], _i),
+    "mw_kvpages_copy": ([_pages_p, _i, _i, _vp], _i),
+    "mw_kvpages_free": ([_pages_p, _seq_p, _i, _vp], _i),
+    "mw_kvpages_evict": ([_pages_p, _i, _i, _i, _vp], _i),
+    "mw_kvpages_compact": ([_pages_p, _vp], _i),
+    "mw_chunk_attn_paged_workspace_size": ([_pages_p, _seq_p] + [_i] * 4, _sz),
+    "mw_chunk_attn_paged": ([_vp] * 3 + [_i, _i, _pages_p, _seq_p] + [_i] * 3 + [_vp, _vp, _f, _vp, _sz, _str_p, _vp], _i),
     "mw_sched_num_ticks": ([ctypes.POINTER(mw_sched_config)], ctypes.c_int64),
     "mw_sched_plan": ([ctypes.POINTER(mw_sched_config), ctypes.c_int64, ctypes.POINTER(mw_sched_tick)], _i),
 }
@@ -532,6 +561,249 @@ def mw_chunk_attn_cached_fp8(q8, k8_new, v8_new, n_queued: int, q_len: int, cach
     _check(load().mw_chunk_attn_cached_fp8(_ptr(q8), _ptr(k8_new), _ptr(v8_new), int(n_queued), int(q_len),
                                            ctypes.byref(d), int(window), int(flags), _ptr(o), _ptr(lse), scale,
                                            float(q_scale), _ptr(workspace), nbytes, _strides(o), _stream_handle(dev)))
+    return o, lse
+
+
+# ----------------------------------------------------------------------------- cross attention
+
+def _on_device(dev):
+    """The calls below launch on the current device: make `dev` current for one that is not."""
+    torch = _torch()
+    if not torch.cuda.is_initialized() or torch.cuda.current_device() == dev.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(dev)
+
+
+def _check_like(name, t, shape, dev):
+    """A bf16 view of the given shape on `dev` (its strides are the library's to check)."""
+    _bf16_4d(name, t, view=True)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != dev:
+        raise ValueError("all tensors must be on the same device")
+
+
+def _check_workspace(workspace, dev):
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the device of the inputs")
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def _cross_args(q, k, v, kv_len):
+    torch = _torch()
+    for n, t in (("q", q), ("k", k), ("v", v)):
+        _bf16_4d(n, t, view=True)
+    B, H, T, D = q.shape
+    Hkv, M = k.shape[1], k.shape[2]
+    dev = q.device
+    for n, t in (("k", k), ("v", v)):
+        _check_like(n, t, (B, Hkv, M, D), dev)
+    if kv_len is not None and (kv_len.dtype != torch.int32 or tuple(kv_len.shape) != (B,) or kv_len.device != dev
+                               or not kv_len.is_contiguous()):
+        raise ValueError(f"kv_len must be a contiguous int32 tensor of shape {(B,)} on the device of the inputs")
+    return B, H, Hkv, T, M, D, dev
+
+
+def mw_cross_attn_workspace_size(B: int, H: int, Hkv: int, T: int, M: int, D: int) -> int:
+    return int(load().mw_cross_attn_workspace_size(B, H, Hkv, T, M, D))
+
+
+def mw_cross_attn_fwd(q, k, v, kv_len=None, scale=None, out=None, lse=None, workspace=None):
+    """Cross attention forward.  q: bf16 [B,H,T,D]; k, v: bf16 [B,Hkv,M,D] with Hkv dividing H (views with a
+    contiguous head dimension are read in place); kv_len: int32 [B] on the GPU, the valid states of each batch
+    member (None: all M).  Returns (o, lse).
+
+    With no workspace given, one of the size the library asks for is allocated here (torch)."""
+    torch = _torch()
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len)
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    o = torch.empty_like(q) if out is None else out
+    _check_like("out", o, (B, H, T, D), dev)
+    lse = torch.empty((B, H, T), dtype=torch.float32, device=dev) if lse is None else lse
+    _check_lse(lse, (B, H, T), dev)
+    if workspace is None:
+        need = mw_cross_attn_workspace_size(B, H, Hkv, T, M, D)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    nbytes = _check_workspace(workspace, dev)
+    with _on_device(dev):
+        _check(load().mw_cross_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(lse),
+                                        _strides(q, k, v, o), B, H, Hkv, T, M, D, scale, _ptr(workspace), nbytes,
+                                        _stream_handle(dev)))
+    return o, lse
+
+
+def mw_cross_attn_bwd_workspace_size(B: int, H: int, Hkv: int, T: int, M: int, D: int) -> int:
+    return int(load().mw_cross_attn_bwd_workspace_size(B, H, Hkv, T, M, D))
+
+
+def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=None, dq=None, dk=None, dv=None):
+    """Backward of mw_cross_attn_fwd.  Returns (dq, dk, dv): bf16 [B,H,T,D] and twice [B,Hkv,M,D], the latter
+    summed over the query heads that share a key head and 0 behind kv_len."""
+    torch = _torch()
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len)
+    for n, t in (("o", o), ("d_o", d_o)):
+        _check_like(n, t, (B, H, T, D), dev)
+    if lse is None:
+        raise ValueError("lse is required")
+    _check_lse(lse, (B, H, T), dev)
+    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
+    if workspace is None:
+        workspace = torch.empty(mw_cross_attn_bwd_workspace_size(B, H, Hkv, T, M, D), dtype=torch.uint8, device=dev)
+    nbytes = _check_workspace(workspace, dev)
+    # (a gradient of states shared between batch members or heads does not share their strides)
+    dq = torch.empty((B, H, T, D), dtype=q.dtype, device=dev) if dq is None else dq
+    dk = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dk is None else dk
+    dv = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dv is None else dv
+    _check_like("dq", dq, (B, H, T, D), dev)
+    for n, t in (("dk", dk), ("dv", dv)):
+        _check_like(n, t, (B, Hkv, M, D), dev)
+    with _on_device(dev):
+        _check(load().mw_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(d_o), _ptr(lse), _ptr(dq),
+                                        _ptr(dk), _ptr(dv), _ptr(workspace), nbytes,
+                                        _strides(q, k, v, o, d_o, dq, dk, dv), B, H, Hkv, T, M, D, scale,
+                                        _stream_handle(dev)))
+    return dq, dk, dv
+
+
+# ----------------------------------------------------------------------------- paged 8-bit cache
+
+class KVPages:
+    """Paged cache of e4m3 keys and values with a power-of-two scale for each 64 tokens and head, over
+    torch-owned tensors: k_pages, v_pages uint8 [P,H,L,D], k_scales, v_scales fp32 [P,H,L/64], table int32
+    [N,W] and lens int32 [N].  N sequences of at most W pages of L tokens; the page bookkeeping is the library's.
+
+    Wraps the mw_kvpages descriptor.
+    """
+
+    def __init__(self, P: int, H: int, L: int, D: int, N: int, W: int, device="cuda"):
+        torch = _torch()
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        need = int(load().mw_kvpages_host_bytes(P, N, W))
+        if need == 0 or min(H, L, D) < 1:
+            raise MWError(MW_EINVAL, f"KVPages: sizes out of range (P={P}, H={H}, L={L}, D={D}, N={N}, W={W})")
+        self.k_pages, self.v_pages = (torch.empty((P, H, L, D), dtype=torch.uint8, device=device) for _ in range(2))
+        self.k_scales, self.v_scales = (torch.empty((P, H, max(1, L // MW_PAGE_BLOCK)), dtype=torch.float32,
+                                                    device=device) for _ in range(2))
+        self.table = torch.empty((N, W), dtype=torch.int32, device=device)
+        self.lens = torch.zeros((N,), dtype=torch.int32, device=device)
+        self._host = (ctypes.c_int32 * (need // 4))()
+        self.desc = mw_kvpages()
+        _check(load().mw_kvpages_init(ctypes.byref(self.desc), _ptr(self.k_pages), _ptr(self.v_pages),
+                                      _ptr(self.k_scales), _ptr(self.v_scales), _ptr(self.table), _ptr(self.lens),
+                                      ctypes.addressof(self._host), need, P, H, L, D, N, W))
+
+    @property
+    def device(self):
+        return self.k_pages.device
+
+    @property
+    def n_free(self) -> int:
+        return _check(load().mw_kvpages_n_free(ctypes.byref(self.desc)))
+
+    def len(self, seq: int) -> int:
+        return _check(load().mw_kvpages_len(ctypes.byref(self.desc), int(seq)))
+
+    def page_of(self, seq: int, index: int) -> int:
+        return _check(load().mw_kvpages_page_of(ctypes.byref(self.desc), int(seq), int(index)))
+
+
+@functools.lru_cache(maxsize=512)
+def _seq_array(seqs):
+    return (ctypes.c_int32 * len(seqs))(*seqs)
+
+
+def _seqs(seqs):
+    """Host array of sequence numbers (the library only reads it)."""
+    return _seq_array(tuple(int(s) for s in seqs))
+
+
+def mw_kvpages_append(cache: KVPages, seqs, k, v) -> None:
+    """Commit k, v (bf16 [len(seqs),H,n_tokens,D] views) to the ends of the listed sequences."""
+    d, dev = cache.desc, cache.device
+    seqs = _seqs(seqs)
+    for n, t in (("k", k), ("v", v)):
+        _bf16_4d(n, t, view=True)
+        _check_like(n, t, (len(seqs), d.H, k.shape[2], d.D), dev)
+    with _on_device(dev):
+        _check(load().mw_kvpages_append(ctypes.byref(d), seqs, len(seqs), _ptr(k), _ptr(v), _strides(k, v), k.shape[2],
+                                        _stream_handle(dev)))
+
+
+def mw_kvpages_fork(cache: KVPages, src: int, dst: int) -> None:
+    """Make the empty sequence dst a branch of src that shares its pages."""
+    with _on_device(cache.device):
+        _check(load().mw_kvpages_fork(ctypes.byref(cache.desc), int(src), int(dst), _stream_handle(cache.device)))
+
+
+def mw_kvpages_copy(cache: KVPages, src: int, dst: int) -> None:
+    """Make the empty sequence dst a copy of src in pages of its own."""
+    with _on_device(cache.device):
+        _check(load().mw_kvpages_copy(ctypes.byref(cache.desc), int(src), int(dst), _stream_handle(cache.device)))
+
+
+def mw_kvpages_free(cache: KVPages, seqs) -> None:
+    """Empty the listed sequences; pages that no other sequence shares become free."""
+    seqs = _seqs(seqs)
+    with _on_device(cache.device):
+        _check(load().mw_kvpages_free(ctypes.byref(cache.desc), seqs, len(seqs), _stream_handle(cache.device)))
+
+
+def mw_kvpages_evict(cache: KVPages, seq: int, first_page: int, n_pages: int) -> None:
+    """Drop the full pages [first_page, first_page + n_pages) of a sequence."""
+    with _on_device(cache.device):
+        _check(load().mw_kvpages_evict(ctypes.byref(cache.desc), int(seq), int(first_page), int(n_pages),
+                                       _stream_handle(cache.device)))
+
+
+def mw_kvpages_compact(cache: KVPages) -> int:
+    """Move live pages to the front of the pool; returns how many moved."""
+    with _on_device(cache.device):
+        return _check(load().mw_kvpages_compact(ctypes.byref(cache.desc), _stream_handle(cache.device)))
+
+
+def mw_chunk_attn_paged_workspace_size(cache: KVPages, seqs, H: int, n_queued: int, q_len: int) -> int:
+    seqs = _seqs(seqs)
+    return int(load().mw_chunk_attn_paged_workspace_size(ctypes.byref(cache.desc), seqs, len(seqs), int(H),
+                                                         int(n_queued), int(q_len)))
+
+
+def mw_chunk_attn_paged(q, k_new, v_new, n_queued: int, q_len: int, cache: KVPages, seqs,
+                        flags: int = MW_QUEUED_CAUSAL, scale=None, out=None, lse=None, want_lse: bool = False,
+                        workspace=None, split: bool = True):
+    """Cached chunk attention of n_queued in-flight chunks over the pages of the listed sequences.  q: bf16
+    [len(seqs),H,n_queued*q_len,D]; k_new, v_new: the queued tokens' keys and values with the cache's heads, or
+    None, None.  Returns (o, lse or None); workspace and split as in mw_chunk_attn_cached."""
+    torch = _torch()
+    d, dev = cache.desc, cache.device
+    seqs = _seqs(seqs)
+    B, T = len(seqs), n_queued * q_len
+    _bf16_4d("q", q, view=True)
+    H = q.shape[1]
+    _check_like("q", q, (B, H, T, d.D), dev)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new are given together or not at all")
+    if k_new is not None:
+        for n, t in (("k_new", k_new), ("v_new", v_new)):
+            _check_like(n, t, (B, d.H, T, d.D), dev)
+    scale = 1.0 / math.sqrt(d.D) if scale is None else float(scale)
+    o = torch.empty_like(q) if out is None else out
+    _check_like("out", o, (B, H, T, d.D), dev)
+    if want_lse and lse is None:
+        lse = torch.empty((B, H, T), dtype=torch.float32, device=dev)
+    _check_lse(lse, (B, H, T), dev)
+    if not split:
+        workspace = None
+    elif workspace is None:
+        need = mw_chunk_attn_paged_workspace_size(cache, seqs, H, n_queued, q_len)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    nbytes = _check_workspace(workspace, dev)
+    ks, vs = (q, q) if k_new is None else (k_new, v_new)
+    with _on_device(dev):
+        _check(load().mw_chunk_attn_paged(_ptr(q), _ptr(k_new), _ptr(v_new), int(n_queued), int(q_len), ctypes.byref(d),
+                                          seqs, B, H, int(flags), _ptr(o), _ptr(lse), scale, _ptr(workspace), nbytes,
+                                          _strides(q, ks, vs, o), _stream_handle(dev)))
     return o, lse
 
 

@@ -44,6 +44,12 @@ UNITS = [  # (object name, source, extra flags)
     ("attn_bwd128", "attn_bwd.hip", ["-DMW_BWD_HEAD_DIM=128"]),
     ("attn_fwd_fp8", "attn_fwd_fp8.hip", ILP),
     ("kvcache", "kvcache.hip", []),
+    *((f"cross{d}", "attn_rows.hip", [f"-DMW_ROWS_HEAD_DIM={d}"]) for d in (64, 72, 128)),
+    *((f"paged{d}", "attn_rows.hip", [f"-DMW_ROWS_HEAD_DIM={d}", "-DMW_ROWS_PAGED"]) for d in (64, 72, 128)),
+    *((f"cross_bwd{d}", "attn_cross_bwd.hip", [f"-DMW_CROSS_HEAD_DIM={d}"]) for d in (64, 72, 128)),
+    ("kvpages", "kvpages.hip", []),
+    ("mw_cross", "mw_cross.cpp", []),
+    ("mw_pages", "mw_pages.cpp", []),
     ("mw_api", "mw_api.cpp", []),
     ("sched", "sched.cpp", []),
 ]

@@ -1,0 +1,561 @@
+// Attention of the rows of one key head over a list of keys that is not the rows' own
+// sequence: cross attention (an encoder's states) and cached attention over pages of
+// 8-bit keys and values (gfx950).
+//
+// Rows.  The G = H / Hkv query heads of a key head share its keys, so they are the rows
+// of one tile: row r of key head hk is token r / G of query head hk G + r % G.  With one
+// token and G heads a tile then reads the keys once for all of them.
+//
+// Keys.  A workgroup visits key steps of BK keys: first the cached tokens of its
+// sequence (PAGED), then the bf16 keys (the states, or the queued tokens' own keys).
+// Each kind starts a step of its own and its last step may be partly filled; rows of a
+// staged tile behind the last key repeat it, so that nothing behind the data is read and
+// the masked products meet finite values.
+//
+// Cached tokens are e4m3 codes with a power-of-two scale for each 64 tokens and head: a
+// step never straddles a page, and a code times its scale is exact in bf16, so a tile is
+// converted once on its way into LDS (global load, v_cvt_scalef32_pk_bf16_fp8, LDS
+// write) and the products are the bf16 ones on the cache's very values.
+#pragma once
+
+#include "mw_device.h"
+#include "mw_kernels.h"
+
+namespace mw {
+
+// Sequence of each batch member (paged calls), by value: a call keeps no memory of the caller's.
+template <bool PAGED>
+struct RowsSeqs {
+  int seq[PAGED ? kMaxSeqs : 1];
+};
+
+// Address of row r of key head hk in a [B, H, T, D] view.
+__device__ __forceinline__ long long row_offset(const Strides& s, int b, int hk, int G, int r) {
+  const int t = G == 1 ? r : (int)((unsigned)r / (unsigned)G);
+  return b * s.b + (long long)(hk * G + (r - t * G)) * s.h + t * s.t;
+}
+
+// Barrier that waits for this wave's LDS accesses and leaves its global loads in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Online softmax and output of 32 rows of a wave (row = lane % 32), as S^T = K Q^T and
+// O^T += V^T P^T (layouts at the top of mw_device.h).
+template <int D, int BN>
+struct RowBlock {
+  static constexpr int KK = (D + 15) / 16, DB = D / 32, KB = BN / 32;
+  static constexpr bool TAIL = D % 32 != 0;
+  // The running maximum moves when a step raises it by more than this many powers of two;
+  // until then probabilities are taken against the old one and stay below 2^8.
+  static constexpr float kRaise = 8.f;
+  f32x16 o[DB];
+  f32x4 ot[2];  // (TAIL) columns 64.. of rows 0..15 and 16..31
+  float m, l;
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = zero16();
+    ot[0] = ot[1] = zero4();
+    m = -INFINITY;
+    l = 0.f;
+  }
+
+  // One step of BN staged keys; `key0` + i is the place of key i, and (MASKED) a row sees
+  // places lo <= place < hi.
+  template <bool MASKED>
+  __device__ __forceinline__ void step(const bf16_t* Kt, const bf16_t* Vt, const FragOffsets<D>& fo, const Tail72& ft,
+                                       const bf16x8 (&qf)[KK], float c, int key0, int lo, int hi, int lane) {
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) s[kb] = zero16();
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] = mfma32(fo.row8(Kt, kb * 32, kk), qf[kk], s[kb]);
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = key0 + kb * 32 + acc_row(i, lane);
+          s[kb][i] = ((key >= lo) & (key < hi)) ? s[kb][i] : -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[kb][i]);
+    mx = max_halves(mx) * c;
+    const bool raise = mx > m + kRaise;
+    if (wave_any(raise)) {
+      // rows that keep their maximum (it may be -inf still) keep a factor of 1
+      const float a = raise ? fast_exp2(m - mx) : 1.f;
+      l *= a;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= a;
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) ot[e] *= __shfl(a, 16 * e + (lane & 15));
+      }
+      m = raise ? mx : m;
+    }
+    const float nm = m == -INFINITY ? 0.f : -m;
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[kb][i] = fast_exp2(fmaf(s[kb][i], c, nm));
+        sum += s[kb][i];
+      }
+    l += sum;
+    // the probabilities go to the matrix product in bf16; their sum stays in 32 bits
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      bf16x8 p[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        p[t] = pack8(s[kb], t);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = mfma32(fo.tr8(Vt, kb * 32, t, db), p[t], o[db]);
+      }
+      if constexpr (TAIL) {
+        const bf16x8 vt = ft.read(Vt, kb * 32);
+        tail_operands(p[0], p[1]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) ot[e] = mfma16(vt, p[e], ot[e]);
+      }
+    }
+  }
+
+  // Floats of LDS that merge() takes.
+  template <int KG, int NWR>
+  static constexpr int merge_floats() {
+    return (KG - 1) * NWR * (DB * 16 + 2 + (TAIL ? 8 : 0)) * 64;
+  }
+  // The key groups' results of the same rows, joined in group 0 (in group order): with M the
+  // largest m_g, O = sum 2^(m_g - M) O_g and l likewise.  Every wave of the workgroup calls it
+  // after the last read of `x`; afterwards only group 0 holds the result.
+  template <int KG, int NWR>
+  __device__ __forceinline__ void merge(int kg, int rw, int lane, float* x) {
+    constexpr int N = DB * 16 + 2 + (TAIL ? 8 : 0);
+    if (kg > 0) {
+      float* y = x + ((kg - 1) * NWR + rw) * N * 64 + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(db * 16 + i) * 64] = o[db][i];
+      y[DB * 16 * 64] = m;
+      y[(DB * 16 + 1) * 64] = l;
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[(DB * 16 + 2 + i) * 64] = ot[i / 4][i % 4];
+      }
+    }
+    __syncthreads();
+    if (kg > 0) return;
+    float M = m, w[KG];
+#pragma unroll
+    for (int g = 1; g < KG; ++g) {
+      w[g] = x[((g - 1) * NWR + rw) * N * 64 + DB * 16 * 64 + lane];
+      M = fmaxf(M, w[g]);
+    }
+    w[0] = m;
+#pragma unroll
+    for (int g = 0; g < KG; ++g) w[g] = w[g] == -INFINITY ? 0.f : fast_exp2(w[g] - M);
+    l *= w[0];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] *= w[0];
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) ot[e] *= __shfl(w[0], 16 * e + (lane & 15));
+    }
+#pragma unroll
+    for (int g = 1; g < KG; ++g) {
+      const float* y = x + ((g - 1) * NWR + rw) * N * 64 + lane;
+      l = fmaf(w[g], y[(DB * 16 + 1) * 64], l);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] = fmaf(w[g], y[(db * 16 + i) * 64], o[db][i]);
+      if constexpr (TAIL) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float wt = __shfl(w[g], 16 * e + (lane & 15));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) ot[e][i] = fmaf(wt, y[(DB * 16 + 2 + 4 * e + i) * 64], ot[e][i]);
+        }
+      }
+    }
+    m = M;
+  }
+};
+
+// A tile of 64 cached tokens of one head on its way into LDS: this thread's pieces of the K
+// and V codes in registers.  Pieces of 16 codes (8 at D = 72, whose 72-byte rows are only
+// 8-byte aligned), NT threads a round.
+template <int D, int NT>
+struct CodeTile {
+  static constexpr int PC = D == 72 ? 8 : 16;  // codes per piece
+  static constexpr int PPR = D / PC;           // pieces per row
+  static constexpr int PIECES = 64 * PPR;
+  static constexpr int ROUNDS = (PIECES + NT - 1) / NT;
+  static constexpr bool WHOLE = PIECES % NT == 0;
+  unsigned k[ROUNDS][PC / 4], v[ROUNDS][PC / 4];
+  float ks, vs;
+
+  // Codes of the tile at `kp`, `vp` (row 0 of the tile in its page), of which rows 0..last
+  // hold tokens; `e`: index of the block's scales.
+  __device__ __forceinline__ void fetch(const uint8_t* kp, const uint8_t* vp, const float* k_scale,
+                                        const float* v_scale, int last, int tid) {
+    ks = *k_scale;
+    vs = *v_scale;
+#pragma unroll
+    for (int it = 0; it < ROUNDS; ++it) {
+      const int p = it * NT + tid;
+      if (!WHOLE && p >= PIECES) break;
+      const int row = p / PPR, col = (p - row * PPR) * PC;
+      const int at = min(row, last) * D + col;
+      if constexpr (PC == 16) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(kp + at), b = *reinterpret_cast<const u32x4*>(vp + at);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          k[it][j] = a[j];
+          v[it][j] = b[j];
+        }
+      } else {
+        const u32x2 a = *reinterpret_cast<const u32x2*>(kp + at), b = *reinterpret_cast<const u32x2*>(vp + at);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          k[it][j] = a[j];
+          v[it][j] = b[j];
+        }
+      }
+    }
+  }
+
+  // Eight codes (two words) -> bf16 values at a power-of-two scale.
+  __device__ __forceinline__ static bf16x8 decode(unsigned w0, unsigned w1, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+
+  // The tile in bf16 into LDS rows row0.. of the K and V tiles.
+  __device__ __forceinline__ void commit(bf16_t* Kt, bf16_t* Vt, int row0, int tid) const {
+#pragma unroll
+    for (int it = 0; it < ROUNDS; ++it) {
+      const int p = it * NT + tid;
+      if (!WHOLE && p >= PIECES) break;
+      const int row = p / PPR, col = (p - row * PPR) * PC;
+#pragma unroll
+      for (int j = 0; j < PC / 8; ++j) {
+        const int at = Tile<D>::off(row0 + row, col + 8 * j);
+        *reinterpret_cast<bf16x8*>(Kt + at) = decode(k[it][2 * j], k[it][2 * j + 1], ks);
+        *reinterpret_cast<bf16x8*>(Vt + at) = decode(v[it][2 * j], v[it][2 * j + 1], vs);
+      }
+    }
+  }
+};
+
+// NW waves in KG key groups of NW / KG waves of 32 rows each; a step stages KG * BN keys,
+// of which a group takes its BN.  WPS: waves per SIMD the registers are allocated for.
+template <int D, bool PAGED, int NW, int BN, int KG, int WPS>
+__global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, RowsSeqs<PAGED> seqs) {
+  constexpr int NWR = NW / KG, BM = 32 * NWR, NT = 64 * NW, BK = BN * KG, NB = BK / 64;
+  static_assert(NW % KG == 0 && BK % 64 == 0, "whole 64-token blocks a step");
+  using RB = RowBlock<D, BN>;
+  using Codes = CodeTile<D, NT>;
+  constexpr int KK = RB::KK, DB = RB::DB;
+  constexpr bool TAIL = RB::TAIL;
+  constexpr int TE = stage_elems<D, BK, NT>();
+  __shared__ __attribute__((aligned(16))) bf16_t lds[2][2][TE];  // K, V x two stages
+  static_assert(RB::template merge_floats<KG, NWR>() * 4 <= (int)sizeof(lds), "the merge fits the stages");
+  bf16_t(*Ks)[TE] = lds[0];
+  bf16_t(*Vs)[TE] = lds[1];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % NWR, kg = wave / NWR;
+  // Consecutive workgroups are dealt to the 8 XCDs in turn: each gets one contiguous range of
+  // (head, key range, row tile), so that a head's keys stay in one L2.
+  int item;
+  {
+    const int n = gridDim.x, x = blockIdx.x % 8, q = n / 8, rem = n % 8;
+    item = x * q + min(x, rem) + blockIdx.x / 8;
+  }
+  const int per_head = p.n_rtiles * p.n_splits;
+  const int bh = item / per_head;
+  const int in_head = item - bh * per_head;
+  const int split = in_head / p.n_rtiles, rt = in_head - split * p.n_rtiles;
+  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const int G = p.G, r0 = rt * BM;
+
+  // this lane's row and its Q fragments; rows behind the last and columns past D are zeros
+  const int row = r0 + rw * 32 + (lane & 31);
+  bf16x8 qf[KK];
+  {
+    const bf16_t* qp = p.q + row_offset(p.sq, b, hk, G, min(row, p.R - 1)) + 8 * (lane >> 5);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      if (row < p.R && (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D)) {
+        qf[kk] = *reinterpret_cast<const bf16x8*>(qp + 16 * kk);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[kk][j] = (__bf16)0.f;
+      }
+    }
+  }
+
+  // the bf16 keys: n_new of them; a row sees [lo, hi)
+  int n_new = p.M, len = 0;
+  if (p.kv_len != nullptr) n_new = max(0, min(p.M, p.kv_len[b]));
+  int lo = 0, hi = n_new, first = 0, last = n_new, lo_all = 0, hi_all = n_new;  // of the row, of any row, of every row
+  if (PAGED && p.mode != ROWS_SEE_ALL) {
+    const int r1 = min(r0 + BM, p.R) - 1;
+    const int c0 = r0 / G / p.qlen, c1 = r1 / G / p.qlen, c = min(row, p.R - 1) / G / p.qlen;
+    const bool own = p.mode == ROWS_SEE_OWN;
+    hi = (c + 1) * p.qlen;
+    lo = own ? c * p.qlen : 0;
+    last = (c1 + 1) * p.qlen;
+    first = own ? c0 * p.qlen : 0;
+    hi_all = (c0 + 1) * p.qlen;
+    lo_all = own ? c1 * p.qlen : 0;
+  }
+  const int new0 = first / BK, n_newt = last > first ? (last + BK - 1) / BK - new0 : 0;
+  int n_old = 0, seq = 0;
+  if constexpr (PAGED) {
+    seq = seqs.seq[b];
+    if constexpr (TAIL) {
+      // D = 72: the last row's reads run into the slack behind the tile and meet zeros in Q; it
+      // has to be finite, and only the bf16 staging fills it
+      constexpr int SLACK = TE - BK * D;
+      for (int i = tid; i < 4 * SLACK; i += NT) (&lds[0][0][0])[(i / SLACK) * TE + BK * D + i % SLACK] = 0;
+    }
+    len = max(0, min(p.lens[seq], p.W * p.L));
+    n_old = (len + BK - 1) / BK;
+  }
+  const int n_all = n_old + n_newt;
+  const int beg = (int)((long long)n_all * split / p.n_splits), end = (int)((long long)n_all * (split + 1) / p.n_splits);
+
+  const long long kbase = b * p.sk.b + hk * p.sk.h, vbase = b * p.sv.b + hk * p.sv.h;
+  const RowOffsets<D, BK, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
+  // bf16 keys of step i (i >= n_old) straight into LDS
+  auto stage_new = [&](int i, int buf) {
+    const int k0 = (new0 + i - n_old) * BK;
+    if (k0 + BK <= n_new) {
+      stage_rows_s<D, BK, NT>(Ks[buf], p.k + kbase + k0 * p.sk.t, ro_k, tid);
+      stage_rows_s<D, BK, NT>(Vs[buf], p.v + vbase + k0 * p.sv.t, ro_v, tid);
+    } else {
+      stage_kv_rows_direct<D, BK, NT>(Ks[buf], Vs[buf], [&](int r) -> RowPair {
+        const long long j = min(k0 + r, n_new - 1);
+        return {p.k + kbase + j * p.sk.t, p.v + vbase + j * p.sv.t};
+      }, tid);
+    }
+  };
+  // cached tokens of step i < n_old into registers
+  Codes codes[PAGED ? NB : 1];
+  auto fetch = [&](int i) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int pos = min(i * BK + nb * 64, (len - 1) & ~63);  // a block behind the last repeats it
+        const int w = pos / p.L, off = pos - w * p.L;
+        const long long page = p.table[(long long)seq * p.W + w];
+        const long long head = page * p.Hkv + hk;
+        const long long at = (head * p.L + off) * D;
+        const long long e = head * (p.L >> 6) + (off >> 6);
+        codes[nb].fetch(p.k_pages + at, p.v_pages + at, p.k_scales + e, p.v_scales + e, len - 1 - pos, tid);
+      }
+    }
+  };
+  auto commit = [&](int buf) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) codes[nb].commit(Ks[buf], Vs[buf], nb * 64, tid);
+    }
+  };
+
+  const FragOffsets<D> fo(lane, kg * BN * D);
+  const Tail72 ft(lane, kg * BN * D);
+  RB rb;
+  rb.init();
+  const float c = p.scale_log2;
+  auto compute = [&](int i, int buf) {
+    if (PAGED && i < n_old) {
+      const int k0 = i * BK;
+      if (k0 + BK <= len) {
+        rb.template step<false>(Ks[buf], Vs[buf], fo, ft, qf, c, 0, 0, 0, lane);
+      } else {
+        rb.template step<true>(Ks[buf], Vs[buf], fo, ft, qf, c, k0 + kg * BN, 0, len, lane);
+      }
+      return;
+    }
+    const int k0 = (new0 + i - n_old) * BK;
+    if (k0 >= lo_all && k0 + BK <= hi_all) {
+      rb.template step<false>(Ks[buf], Vs[buf], fo, ft, qf, c, 0, 0, 0, lane);
+    } else {
+      rb.template step<true>(Ks[buf], Vs[buf], fo, ft, qf, c, k0 + kg * BN, lo, hi, lane);
+    }
+  };
+
+  if (beg < end) {
+    // Two LDS stages.  A cached step is in registers one step before it is written to LDS,
+    // and in LDS one step before it is used; a bf16 step goes to LDS during the step before it.
+    if (PAGED && beg < n_old) {
+      fetch(beg);
+      commit(0);
+      if (beg + 1 < min(end, n_old)) fetch(beg + 1);
+    } else {
+      stage_new(beg, 0);
+      wait_vmem();
+    }
+    lds_barrier();
+    int buf = 0;
+    for (int i = beg; i < end; ++i) {
+      bool direct = false;
+      if (i + 1 < end) {
+        if (PAGED && i + 1 < n_old) {
+          commit(buf ^ 1);
+          if (i + 2 < min(end, n_old)) fetch(i + 2);
+        } else {
+          stage_new(i + 1, buf ^ 1);
+          direct = true;
+        }
+      }
+      compute(i, buf);
+      if (direct) wait_vmem();
+      lds_barrier();
+      buf ^= 1;
+    }
+  }
+
+  if constexpr (KG > 1) {
+    rb.template merge<KG, NWR>(kg, rw, lane, reinterpret_cast<float*>(&lds[0][0][0]));
+    if (kg > 0) return;  // no barrier follows
+  }
+  const float l = sum_halves(rb.l);
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that saw no key gives zeros
+  if (p.n_splits > 1) {
+    // unnormalised partial of this key range: O, and the pair (m, l)
+    const long long prow = ((long long)split * p.B * p.Hkv + bh) * p.R;
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = r0 + rw * 32 + 16 * e + (lane & 15);
+        if (lane < 32 && r < p.R)
+          *reinterpret_cast<f32x4*>(p.part + (prow + r) * D + 64 + 4 * (lane >> 4)) = rb.ot[e];
+      }
+    }
+    if (row >= p.R) return;
+    float* po = p.part + (prow + row) * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = rb.o[db][4 * g + j];
+        *reinterpret_cast<f32x4*>(po + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
+      }
+    if (lane < 32) {
+      float* ml = p.part + (long long)p.n_splits * p.B * p.Hkv * p.R * D + 2 * (prow + row);
+      ml[0] = rb.m;
+      ml[1] = l;
+    }
+    return;
+  }
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float iv = __shfl(inv, 16 * e + (lane & 15));
+      const int r = r0 + rw * 32 + 16 * e + (lane & 15);
+      if (lane < 32 && r < p.R) {
+        bf16x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = to_bf16(rb.ot[e][j] * iv);
+        *reinterpret_cast<bf16x4*>(p.o + row_offset(p.so, b, hk, G, r) + 64 + 4 * (lane >> 4)) = w;
+      }
+    }
+  }
+  if (row >= p.R) return;
+  bf16_t* orow = p.o + row_offset(p.so, b, hk, G, row);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = to_bf16(rb.o[db][4 * g + j] * inv);
+      *reinterpret_cast<bf16x4*>(orow + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
+    }
+  if (p.lse != nullptr && lane < 32) {
+    const int t = row / G;
+    p.lse[((long long)b * p.Hkv * G + hk * G + (row - t * G)) * p.T + t] =
+        l == 0.f ? -INFINITY : (rb.m + __log2f(l)) * 0.69314718055994530942f;
+  }
+}
+
+// Join of the key ranges' partials: with M the largest m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s
+// and LSE = (M + log2 of that sum) ln 2.  One thread for four columns of a row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsParams p) {
+  constexpr int TPR = D / 4;
+  const long long rows = (long long)p.B * p.Hkv * p.R;
+  const long long gid = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long pr = gid / TPR;
+  if (pr >= rows) return;
+  const int col = (int)(gid - pr * TPR) * 4;
+  const int bh = (int)(pr / p.R), r = (int)(pr - (long long)bh * p.R);
+  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const float* ml = p.part + (long long)p.n_splits * rows * D;
+  float M = -INFINITY, L = 0.f;
+  f32x4 acc = zero4();
+  constexpr int U = 4;  // ranges in flight
+  for (int s0 = 0; s0 < p.n_splits; s0 += U) {
+    float mv[U], lv[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = s0 + u < p.n_splits;
+      const long long x = (long long)(in ? s0 + u : s0) * rows + pr;
+      mv[u] = in ? ml[2 * x] : -INFINITY;
+      lv[u] = ml[2 * x + 1];
+      v[u] = *reinterpret_cast<const f32x4*>(p.part + x * D + col);
+    }
+    float Mn = M;
+#pragma unroll
+    for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, mv[u]);
+    const float a = M == -INFINITY ? 0.f : fast_exp2(M - Mn);
+    L *= a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] *= a;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float w = mv[u] == -INFINITY ? 0.f : fast_exp2(mv[u] - Mn);  // an empty range
+      L = fmaf(w, lv[u], L);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = fmaf(w, v[u][j], acc[j]);
+    }
+    M = Mn;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  bf16x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = to_bf16(acc[j] * inv);
+  *reinterpret_cast<bf16x4*>(p.o + row_offset(p.so, b, hk, p.G, r) + col) = w;
+  if (p.lse != nullptr && col == 0) {
+    const int t = r / p.G;
+    p.lse[((long long)b * p.Hkv * p.G + hk * p.G + (r - t * p.G)) * p.T + t] =
+        L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.69314718055994530942f;
+  }
+}
+
+}  // namespace mw

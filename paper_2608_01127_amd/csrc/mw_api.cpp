@@ -11,11 +11,16 @@
 #include <string>
 
 #include "mw.h"
+#include "mw_host.h"
 #include "mw_kernels.h"
 
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+namespace mw {
 
 int fail(int code, const char* fmt, ...) {
   char buf[512];
@@ -33,8 +38,6 @@ int ok() {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr int kMaxT = 1 << 24;  // keeps every in-kernel row * D index within 32 bits
 
 int check_ptrs(const char* fn, std::initializer_list<std::pair<const char*, const void*>> ptrs) {
   for (auto& pr : ptrs)
@@ -59,8 +62,6 @@ int hip_status(const char* fn, hipError_t e) {
   if (e != hipSuccess) return fail(MW_EHIP, "%s: HIP error %s", fn, hipGetErrorString(e));
   return ok();
 }
-
-const float kLog2e = 1.4426950408889634f;
 
 mw::Strides contiguous(int H, int T, int D) { return {(long long)H * T * D, (long long)T * D, D}; }
 
@@ -100,14 +101,13 @@ int check_view(const char* fn, const char* name, const mw_strides& s, int B, int
 
 mw::Strides to_internal(const mw_strides& s) { return {s.b, s.h, s.t}; }
 
-}  // namespace
-
-namespace mw {
 int set_error(int code, const char* msg) {
   g_err = code == MW_OK ? std::string() : std::string(msg);
   return code;
 }
 }  // namespace mw
+
+using namespace mw;
 
 extern "C" {
 
@@ -324,8 +324,6 @@ int mw_kvcache_init(mw_kvcache* c, void* k_slots, void* v_slots, int S, int B, i
   for (int i = 0; i < MW_MAX_SLOTS; ++i) c->rope_at_commit[i] = 0;
   return ok();
 }
-
-static bool good_scale(float s) { return s > 0.f && std::isfinite(s); }
 
 int mw_kvcache_init_fp8(mw_kvcache* c, void* k_slots, void* v_slots, int S, int B, int H, int L, int D, float k_scale,
                         float v_scale) {

@@ -313,6 +313,119 @@ hipError_t launch_kv_copy(const uint16_t* k_src, const uint16_t* v_src, uint16_t
 hipError_t launch_kv_gather(const uint16_t* k_src, const uint16_t* v_src, Strides sk, Strides sv, uint16_t* k_dst,
                             uint16_t* v_dst, int B, int H, int L, int D, hipStream_t stream);
 
+// ---------------------------------------------------------------------------
+// Attention of the rows of a key head over other keys (attn_rows.h): cross
+// attention and cached attention over pages.
+// ---------------------------------------------------------------------------
+constexpr int kMaxSeqs = 256;  // batch members of a paged call (their sequences travel in the kernel's arguments)
+// Which of the bf16 keys a row sees: all (the first kv_len), the queued chunks up to its own,
+// or its own chunk only.
+enum RowsMode { ROWS_SEE_ALL = 0, ROWS_SEE_EARLIER = 1, ROWS_SEE_OWN = 2 };
+struct RowsParams {
+  const uint16_t* q;
+  const uint16_t* k;  // bf16 keys: the states [B, Hkv, M, D], or the queued tokens' own
+  const uint16_t* v;
+  uint16_t* o;
+  float* lse;  // [B, H, T], or null
+  Strides sq, sk, sv, so;
+  int B, Hkv, G, T;
+  int R;              // rows of a key head: T * G, row r = token r / G of query head hk G + r % G
+  int M;              // bf16 keys
+  const int* kv_len;  // device [B]: how many of the bf16 keys are valid, or null (all)
+  int mode, qlen;
+  float scale_log2;
+  // pages: codes [P, Hkv, L, D], scales [P, Hkv, L / 64], table [N, W], lengths [N]
+  const uint8_t* k_pages;
+  const uint8_t* v_pages;
+  const float* k_scales;
+  const float* v_scales;
+  const int* table;
+  const int* lens;
+  int L, W;
+  // n_rtiles row tiles of a key head over n_splits key ranges (set by the launcher)
+  int n_rtiles, n_splits;
+  float* part;  // [n_splits][B Hkv][R][D] unnormalised O, then [n_splits][B Hkv][R][2] (m, l)
+};
+// How a call is divided: rows of a tile and key ranges.
+struct RowsPlan {
+  int bm, n_splits;
+};
+RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws_bytes);
+size_t rows_part_bytes(int D, int BHkv, int R, int n_splits);
+hipError_t launch_cross_64(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_cross_72(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_cross_128(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_paged_64(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_paged_72(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_paged_128(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
+
+// Backward of the cross attention (attn_cross_bwd.hip).
+struct CrossBwdParams {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const uint16_t* o;
+  const uint16_t* d_o;
+  const float* lse;  // [B, H, T]
+  const int* kv_len;
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  float* delta;  // [B Hkv][R]: -rowsum(dO O)
+  float* lse2;   // [B Hkv][R]: LSE log2 e (rows without a key: +inf)
+  float* part;   // n_slices > 1: [n_slices][2][B Hkv][M][D] fp32 dK, dV of a slice of the rows
+  Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  int B, Hkv, G, T, R, M;
+  int n_slices;
+  float scale, scale_log2;
+};
+int cross_bwd_slices(int D, int BHkv, int R, int M);
+hipError_t launch_cross_bwd_64(const CrossBwdParams& p, hipStream_t stream);
+hipError_t launch_cross_bwd_72(const CrossBwdParams& p, hipStream_t stream);
+hipError_t launch_cross_bwd_128(const CrossBwdParams& p, hipStream_t stream);
+
+// Page operations (kvpages.hip).  What the host has decided travels in the kernels' arguments.
+struct PagePool {
+  uint8_t* k_pages;
+  uint8_t* v_pages;
+  float* k_scales;
+  float* v_scales;
+  int* table;
+  int* lens;
+  int H, L, D, W;
+};
+// A run of tokens of one sequence that starts behind `pos` tokens (job fields by column, so that
+// the arguments stay below 4 KB).  Its pages are pages[page0..], the first one holding token
+// `pos` (or the next one, where `pos` ends a page); cow >= 0: the page whose tokens below `pos`
+// the first page takes over.
+constexpr int kAppendJobs = 32, kAppendPages = 512;
+struct AppendArgs {
+  int n_jobs;
+  int seq[kAppendJobs], row[kAppendJobs], pos[kAppendJobs], tok[kAppendJobs], n_tok[kAppendJobs], page0[kAppendJobs],
+      cow[kAppendJobs], len[kAppendJobs];
+  int pages[kAppendPages];
+};
+hipError_t launch_pages_append(const PagePool& c, const uint16_t* k, const uint16_t* v, Strides sk, Strides sv,
+                               const AppendArgs& a, hipStream_t stream);
+constexpr int kPagePairs = 400;
+struct PairArgs {
+  int n;
+  int src[kPagePairs], dst[kPagePairs];
+};
+// Copies pages src -> dst.  seq >= 0: dst pages become entries w0.. of that sequence's row, whose
+// length becomes `len`; seq < 0: every live table entry src becomes dst (`n_seqs` rows; src ascending).
+hipError_t launch_pages_copy(const PagePool& c, const PairArgs& a, int seq, int w0, int len, int n_seqs,
+                             hipStream_t stream);
+// Row `dst` := row `src` (n entries), of the same length.
+hipError_t launch_pages_fork(const PagePool& c, int src, int dst, int n, int len, hipStream_t stream);
+struct SeqArgs {
+  int n;
+  int seq[kMaxSeqs];
+};
+hipError_t launch_pages_clear(const PagePool& c, const SeqArgs& a, hipStream_t stream);
+// Entries from first + n on of a row move to `first`; its length becomes `len`.
+hipError_t launch_pages_evict(const PagePool& c, int seq, int first, int n, int used, int len, hipStream_t stream);
+
 // Record the calling thread's status message (what mw_last_error returns)
 // and return `code`; MW_OK clears it.
 int set_error(int code, const char* msg);
