@@ -4,12 +4,12 @@
 // over the rows r of a key head (its query heads' tokens, attn_rows.h), so that the gradients of
 // shared heads are sums over more rows and need nothing else.
 //
-//   row terms  : -Delta and LSE log2 e, one pass over O and dO;
-//   one grid   : dK/dV work (a tile of keys held in registers walks a slice of the rows) and
-//                dQ work (a tile of rows walks the keys);
-//   slices     : the rows are many and the keys few, so the rows of a key tile are cut into
-//                slices that fill the card; each leaves fp32 dK, dV, which the last kernel adds in
-//                slice order.  No atomics: the result is deterministic.
+//   dQ kernel    : a wave owns 32 rows and walks the keys; it has the rows' dO in registers, so it also
+//                  forms Delta (and LSE log2 e) for the other kernel.  Few rows over many keys: the keys are cut
+//                  into ranges that leave fp32 dQ.
+//   dK/dV kernel : a wave owns 32 keys and walks rows staged in LDS.  The rows are many and the keys few, so the
+//                  rows of a key tile are cut into slices that fill the card and leave fp32 dK, dV.
+//   join kernel  : adds ranges and slices in their order.  No atomics: the result is deterministic.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,70 +21,78 @@ namespace {
 
 constexpr int kD = MW_CROSS_HEAD_DIM;
 
-template <int D>
-__global__ __launch_bounds__(256) void cross_rowterms_kernel(CrossBwdParams p) {
-  constexpr int CPR = D == 64 ? 8 : 16;  // lanes per row (D = 72: nine of 16 have a piece)
-  const long long gid = (long long)blockIdx.x * 256 + threadIdx.x, n_rows = (long long)p.B * p.Hkv * p.R;
-  const long long rr = gid / CPR;
-  const int c = (int)(gid % CPR);
-  float acc = 0.f;
-  int b = 0, h = 0, t = 0;
-  if (rr < n_rows) {
-    const long long bh = rr / p.R;
-    const int r = (int)(rr - bh * p.R);
-    t = r / p.G;
-    b = (int)(bh / p.Hkv);
-    h = (int)(bh - (long long)b * p.Hkv) * p.G + (r - t * p.G);
-    if (c < D / 8) {
-      const bf16x8 x = *reinterpret_cast<const bf16x8*>(p.o + b * p.so.b + h * p.so.h + t * p.so.t + c * 8);
-      const bf16x8 y = *reinterpret_cast<const bf16x8*>(p.d_o + b * p.sdo.b + h * p.sdo.h + t * p.sdo.t + c * 8);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) acc = fmaf((float)x[j], (float)y[j], acc);
-    }
-  }
-#pragma unroll
-  for (int w = CPR / 2; w >= 1; w >>= 1) acc += __shfl_xor(acc, w);
-  if (rr < n_rows && c == 0) {
-    const float l = p.lse[((long long)b * p.Hkv * p.G + h) * p.T + t];
-    p.delta[rr] = -acc;
-    p.lse2[rr] = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;  // a row without a key: P = 0
-  }
-}
-
 // Valid keys of batch member b.
 __device__ __forceinline__ int valid_keys(const CrossBwdParams& p, int b) {
   return p.kv_len == nullptr ? p.M : max(0, min(p.M, p.kv_len[b]));
 }
 
-// Work items [0, n) of a part of the grid that starts at a multiple of 8: XCD x gets one contiguous range.
+// Consecutive workgroups are dealt to the 8 XCDs in turn: each gets one contiguous range of the work.
 __device__ __forceinline__ int xcd_range(int id, int n) {
   const int x = id % 8, q = n / 8, rem = n % 8;
   return x * q + min(x, rem) + id / 8;
 }
 
-template <int D, int NW, int BM>
+// LDS of the dK/dV kernel: Q and dO tiles of BS rows, LSE and -Delta of those rows (two stages each), then VL V
+// fragments of each key wave.
+template <int D, int NWK, int QG, int BM, int VL>
 struct CrossLds {
-  static constexpr int TE = stage_elems<D, BM, 64 * NW>();
-  static constexpr int RT = BM < 64 ? 64 : BM;
-  static constexpr int BYTES = 2 * 2 * TE * 2 + 2 * 2 * RT * 4;
+  static constexpr int NT = 64 * NWK * QG, BS = BM * QG;
+  static constexpr int TE = stage_elems<D, BS, NT>();
+  static constexpr int RT = BS < 64 ? 64 : BS;
+  static constexpr int STAGES = 2 * 2 * TE * 2 + 2 * 2 * RT * 4;
+  static constexpr int MERGE = QG == 1 ? 0 : (QG / 2) * NWK * (D / 32 + (D % 32 != 0)) * 16 * 64 * 4;
+  static constexpr int BYTES = STAGES + NWK * VL * 1024 > MERGE ? STAGES + NWK * VL * 1024 : MERGE;
 };
 
-// dK/dV work: a wave owns 32 keys (K and V fragments, dK^T and dV^T in registers) and walks rows
-// [beg, end) of the key head, BM a step, staged in LDS.  Lanes behind the last key repeat it and
-// store zeros.
-template <int D, int NW, int BM>
-__device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int kt, int slice, unsigned char* lds) {
-  constexpr int BN = 32 * NW, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
+// Sum of the row groups' tiles in group 0, through LDS: in each round the upper half of the groups hands its tiles
+// to the lower half (a fixed order).  Every wave calls it after the last read of `x`.
+template <int G, int NWK, int N>
+__device__ __forceinline__ void add_groups(f32x16 (&acc)[N], int group, int slot, int lane, float* x) {
+#pragma unroll
+  for (int half = G / 2; half >= 1; half >>= 1) {
+    __syncthreads();
+    if (group >= half && group < 2 * half) {
+      float* y = x + ((group - half) * NWK + slot) * N * 1024 + lane;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(n * 16 + i) * 64] = acc[n][i];
+    }
+    __syncthreads();
+    if (group < half) {
+      const float* y = x + (group * NWK + slot) * N * 1024 + lane;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[n][i] += y[(n * 16 + i) * 64];
+    }
+  }
+}
+
+// dK/dV: NWK key waves of 32 keys each (K fragments, dK^T and dV^T in registers) in QG row groups; a step stages
+// BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
+// first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
+// the registers).  Lanes behind the last key repeat it and store zeros.
+template <int D, int NWK, int QG, int BM, int VL>
+__global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdParams p, int n_ktiles) {
+  constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
-  using LD = CrossLds<D, NW, BM>;
+  static_assert(16 * VL <= D, "the V fragments in LDS have no columns past D");
+  using LD = CrossLds<D, NWK, QG, BM, VL>;
   constexpr int TE = LD::TE, RT = LD::RT;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[LD::BYTES];
   bf16_t(*Qs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);
   bf16_t(*Os)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds + 4 * TE);
   float(*lse_s)[RT] = reinterpret_cast<float(*)[RT]>(lds + 8 * TE);
   float(*dlt_s)[RT] = reinterpret_cast<float(*)[RT]>(lds + 8 * TE + 8 * RT);
+  bf16_t* Vs = reinterpret_cast<bf16_t*>(lds + LD::STAGES);
+  const int item = xcd_range(blockIdx.x, gridDim.x);
+  const int per = n_ktiles * p.n_slices, bh = item / per, x = item - bh * per, slice = x / n_ktiles;
+  const int kt = x - slice * n_ktiles;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kw = wave % NWK, qg = wave / NWK, gq = qg * BM;
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv, G = p.G, R = p.R;
-  const int k0 = kt * BN, key = k0 + wave * 32 + (lane & 31), n = valid_keys(p, b);
+  const int k0 = kt * BN, key = k0 + kw * 32 + (lane & 31), n = valid_keys(p, b);
   f32x16 dk[DB], dv[DB];
   f32x4 tail[4] = {zero4(), zero4(), zero4(), zero4()};  // (TAIL) dV^T, dK^T of keys 0..15 and 16..31
 #pragma unroll
@@ -92,6 +100,7 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
 
   if (k0 < n) {
     bf16x8 kf[KK], vf[KK];
+    const bf16_t* vfrag = Vs + (kw * VL * 64 + lane) * 8;
     {
       const long long kr = min(key, n - 1);
       const bf16_t* ka = p.k + b * p.sk.b + hk * p.sk.h + kr * p.sk.t + 8 * (lane >> 5);
@@ -105,25 +114,26 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
 #pragma unroll
           for (int j = 0; j < 8; ++j) kf[kk][j] = vf[kk][j] = (__bf16)0.f;
         }
+        if (kk < VL && qg == 0) *reinterpret_cast<bf16x8*>(Vs + ((kw * VL + kk) * 64 + lane) * 8) = vf[kk];
       }
     }
-    const FragOffsets<D> fo(lane, 0);
-    const Tail72 ft(lane, 0);
-    const RowOffsets<D, BM, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
+    const FragOffsets<D> fo(lane, gq * D);
+    const Tail72 ft(lane, gq * D);
+    const RowOffsets<D, BS, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
     const long long qb = b * p.sq.b + hk * p.sq.h, ob = b * p.sdo.b + hk * p.sdo.h;
     const float* lse2 = p.lse2 + (long long)bh * R;
     const float* dlt = p.delta + (long long)bh * R;
-    const int n_steps = (R + BM - 1) / BM;
-    const int beg = (int)((long long)n_steps * slice / p.n_slices) * BM;
-    const int end = min(R, (int)((long long)n_steps * (slice + 1) / p.n_slices) * BM);
+    const int n_steps = (R + BS - 1) / BS;
+    const int beg = (int)((long long)n_steps * slice / p.n_slices) * BS;
+    const int end = min(R, (int)((long long)n_steps * (slice + 1) / p.n_slices) * BS);
     auto stage = [&](int r0, int buf) {
-      if (G == 1 && r0 + BM <= R) {
-        stage_rows_s<D, BM, NT>(Qs[buf], p.q + qb + r0 * p.sq.t, ro_q, tid);
-        stage_rows_s<D, BM, NT>(Os[buf], p.d_o + ob + r0 * p.sdo.t, ro_o, tid);
+      if (G == 1 && r0 + BS <= R) {
+        stage_rows_s<D, BS, NT>(Qs[buf], p.q + qb + r0 * p.sq.t, ro_q, tid);
+        stage_rows_s<D, BS, NT>(Os[buf], p.d_o + ob + r0 * p.sdo.t, ro_o, tid);
       } else {
-        stage_rows_direct<D, BM, NT>(Qs[buf], [&](int r) { return p.q + row_offset(p.sq, b, hk, G, min(r0 + r, R - 1)); },
+        stage_rows_direct<D, BS, NT>(Qs[buf], [&](int r) { return p.q + row_offset(p.sq, b, hk, G, min(r0 + r, R - 1)); },
                                      tid);
-        stage_rows_direct<D, BM, NT>(Os[buf],
+        stage_rows_direct<D, BS, NT>(Os[buf],
                                      [&](int r) { return p.d_o + row_offset(p.sdo, b, hk, G, min(r0 + r, R - 1)); }, tid);
       }
 #pragma unroll
@@ -144,18 +154,19 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
         f32x16 s = zero16(), dp;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][qb * 32 + 8 * g + 4 * (lane >> 5)]);
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][gq + qb * 32 + 8 * g + 4 * (lane >> 5)]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) dp[4 * g + j] = d4[j];
         }
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
           s = mfma32(fo.row8(Qs[buf], qb * 32, kk), kf[kk], s);
-          dp = mfma32(fo.row8(Os[buf], qb * 32, kk), vf[kk], dp);
+          const bf16x8 vk = kk < VL ? *reinterpret_cast<const bf16x8*>(vfrag + kk * 512) : vf[kk];
+          dp = mfma32(fo.row8(Os[buf], qb * 32, kk), vk, dp);
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const int rr = qb * 32 + 8 * g + 4 * (lane >> 5);
+          const int rr = gq + qb * 32 + 8 * g + 4 * (lane >> 5);
           const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][rr]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -197,27 +208,42 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
       wait_vmem();
       __syncthreads();
       int buf = 0;
-      for (int r0 = beg; r0 < end; r0 += BM) {
-        if (r0 + BM < end) stage(r0 + BM, buf ^ 1);
-        if (r0 + BM <= R) {
-          step(std::false_type{}, r0, buf);
-        } else {
-          step(std::true_type{}, r0, buf);
+      int r0 = beg;
+      auto run = [&](auto ragged, int stop) {
+        for (; r0 < stop; r0 += BS) {
+          if (r0 + BS < end) stage(r0 + BS, buf ^ 1);
+          if (k0 + kw * 32 < n) step(ragged, r0, buf);
+          wait_vmem();
+          __syncthreads();
+          buf ^= 1;
         }
-        wait_vmem();
-        __syncthreads();
-        buf ^= 1;
-      }
+      };
+      run(std::false_type{}, min(end, R / BS * BS));
+      run(std::true_type{}, end);
     }
   }
 
+  if constexpr (QG > 1) {
+    float* m = reinterpret_cast<float*>(lds);
+    add_groups<QG, NWK>(dv, qg, kw, lane, m);
+    add_groups<QG, NWK>(dk, qg, kw, lane, m);
+    if constexpr (TAIL) {
+      f32x16 all[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) all[0][i] = tail[i / 4][i % 4];
+      add_groups<QG, NWK>(all, qg, kw, lane, m);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tail[i / 4][i % 4] = all[0][i];
+    }
+    if (qg > 0) return;  // no barrier follows
+  }
   if (p.n_slices > 1) {
     const long long half = (long long)p.B * p.Hkv * p.M * D;
     float* pk = p.part + slice * 2 * half + (long long)bh * p.M * D;  // dK; dV half further on
     if constexpr (TAIL) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int kr = k0 + wave * 32 + 16 * e + (lane & 15);
+        const int kr = k0 + kw * 32 + 16 * e + (lane & 15);
         if (lane < 32 && kr < n) {
           float* x = pk + (long long)kr * D + 64 + 4 * (lane >> 4);
           *reinterpret_cast<f32x4*>(x) = tail[2 + e];
@@ -245,7 +271,7 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
   if constexpr (TAIL) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int kr = k0 + wave * 32 + 16 * e + (lane & 15), col = 64 + 4 * (lane >> 4);
+      const int kr = k0 + kw * 32 + 16 * e + (lane & 15), col = 64 + 4 * (lane >> 4);
       if (lane < 32 && kr < p.M) {
         bf16x4 wk, wv;
 #pragma unroll
@@ -277,14 +303,18 @@ __device__ __forceinline__ void dkdv_work(const CrossBwdParams& p, int bh, int k
     }
 }
 
-// dQ work: a wave owns 32 rows (Q and dO fragments, dQ^T in registers) and walks the keys, BN a step.
-template <int D, int NW, int BN>
-__device__ __forceinline__ void dq_work(const CrossBwdParams& p, int bh, int rt, unsigned char* lds) {
+// dQ: NW waves of 32 rows each (Q and dO fragments, dQ^T in registers), walking the keys of range `split`, BN a step.
+template <int D, int NW, int BN, int WPS>
+__global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p, int n_rtiles) {
   constexpr int BM = 32 * NW, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
   constexpr int TE = stage_elems<D, BN, NT>();
-  bf16_t(*Ks)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);
-  bf16_t(*Vs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds + 4 * TE);
+  __shared__ __attribute__((aligned(16))) bf16_t lds[2][2][TE];
+  bf16_t(*Ks)[TE] = lds[0];
+  bf16_t(*Vs)[TE] = lds[1];
+  const int item = xcd_range(blockIdx.x, gridDim.x);
+  const int per = n_rtiles * p.n_ranges, bh = item / per, x = item - bh * per, split = x / n_rtiles;
+  const int rt = x - split * n_rtiles;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv, G = p.G, R = p.R;
   const int row = rt * BM + wave * 32 + (lane & 31), rc = min(row, R - 1), n = valid_keys(p, b);
@@ -292,21 +322,36 @@ __device__ __forceinline__ void dq_work(const CrossBwdParams& p, int bh, int rt,
   f32x4 tail[2] = {zero4(), zero4()};
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = zero16();
+  // (a batch member without a key has no use for the row terms either)
+  const int steps = (n + BN - 1) / BN;
+  const int beg = (int)((long long)steps * split / p.n_ranges) * BN;
+  const int end = min(n, (int)((long long)steps * (split + 1) / p.n_ranges) * BN);
   if (n > 0) {
     bf16x8 qf[KK], of[KK];
     const bf16_t* qa = p.q + row_offset(p.sq, b, hk, G, rc) + 8 * (lane >> 5);
-    const bf16_t* oa = p.d_o + row_offset(p.sdo, b, hk, G, rc) + 8 * (lane >> 5);
+    const bf16_t* da = p.d_o + row_offset(p.sdo, b, hk, G, rc) + 8 * (lane >> 5);
+    const bf16_t* oa = p.o + row_offset(p.so, b, hk, G, rc) + 8 * (lane >> 5);
+    float dot = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
         qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
-        of[kk] = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
+        of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
+        const bf16x8 y = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[j], dot);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = (__bf16)0.f;
       }
     }
-    const float lse2 = p.lse2[(long long)bh * R + rc], ndlt = p.delta[(long long)bh * R + rc], c = p.scale_log2;
+    const float ndlt = -sum_halves(dot), c = p.scale_log2;
+    const int t = rc / G;
+    const float lse2 = p.lse[((long long)b * p.Hkv * G + hk * G + (rc - t * G)) * p.T + t] * 1.4426950408889634f;
+    if (split == 0 && lane < 32 && row < R) {
+      p.delta[(long long)bh * R + row] = ndlt;
+      p.lse2[(long long)bh * R + row] = lse2;
+    }
     f32x16 nd;
 #pragma unroll
     for (int i = 0; i < 16; ++i) nd[i] = ndlt;
@@ -328,6 +373,7 @@ __device__ __forceinline__ void dq_work(const CrossBwdParams& p, int bh, int rt,
     auto step = [&](auto ragged, int k0, int buf) {
 #pragma unroll
       for (int kq = 0; kq < BN / 32; ++kq) {
+        if (decltype(ragged)::value && k0 + kq * 32 >= n) break;
         f32x16 s = zero16(), dp = nd;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
@@ -355,21 +401,42 @@ __device__ __forceinline__ void dq_work(const CrossBwdParams& p, int bh, int rt,
         }
       }
     };
-    stage(0, 0);
+    if (beg < end) stage(beg, 0);
     wait_vmem();
     __syncthreads();
-    int buf = 0;
-    for (int k0 = 0; k0 < n; k0 += BN) {
-      if (k0 + BN < n) stage(k0 + BN, buf ^ 1);
-      if (k0 + BN <= n) {
-        step(std::false_type{}, k0, buf);
-      } else {
-        step(std::true_type{}, k0, buf);
+    int buf = 0, k0 = beg;
+    auto run = [&](auto ragged, int stop) {
+      for (; k0 < stop; k0 += BN) {
+        if (k0 + BN < end) stage(k0 + BN, buf ^ 1);
+        step(ragged, k0, buf);
+        wait_vmem();
+        __syncthreads();
+        buf ^= 1;
       }
-      wait_vmem();
-      __syncthreads();
-      buf ^= 1;
+    };
+    run(std::false_type{}, min(end, n / BN * BN));
+    run(std::true_type{}, end);
+  }
+  if (p.n_ranges > 1) {  // fp32 dQ of this key range
+    float* part = p.part_q + ((long long)split * p.B * p.Hkv + bh) * R * D;
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = rt * BM + wave * 32 + 16 * e + (lane & 15);
+        if (lane < 32 && r < R) *reinterpret_cast<f32x4*>(part + (long long)r * D + 64 + 4 * (lane >> 4)) = tail[e];
+      }
     }
+    if (row >= R) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = dq[db][4 * g + j];
+        *reinterpret_cast<f32x4*>(part + (long long)row * D + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
+      }
+    return;
   }
   if constexpr (TAIL) {
 #pragma unroll
@@ -396,50 +463,59 @@ __device__ __forceinline__ void dq_work(const CrossBwdParams& p, int bh, int rt,
     }
 }
 
-template <int D, int NW, int BMK, int BNQ, int WPS>
-__global__ __launch_bounds__(64 * NW, WPS) void cross_grad_kernel(CrossBwdParams p, int n_dkdv, int first_dq, int n_ktiles,
-                                                                  int n_rtiles) {
-  constexpr int B1 = CrossLds<D, NW, BMK>::BYTES, B2 = 8 * stage_elems<D, BNQ, 64 * NW>();
-  __shared__ __attribute__((aligned(16))) unsigned char lds[B1 > B2 ? B1 : B2];
-  const int id = blockIdx.x;
-  if (id < first_dq) {
-    if (id >= n_dkdv) return;  // (the dQ work starts at a multiple of 8)
-    const int item = xcd_range(id, n_dkdv);
-    const int per = n_ktiles * p.n_slices, bh = item / per, x = item - bh * per, slice = x / n_ktiles;
-    dkdv_work<D, NW, BMK>(p, bh, x - slice * n_ktiles, slice, lds);
-  } else {
-    const int item = xcd_range(id - first_dq, (int)gridDim.x - first_dq);
-    const int bh = item / n_rtiles;
-    dq_work<D, NW, BNQ>(p, bh, item - bh * n_rtiles, lds);
+// Sums of the slices (dK, dV; zeros for the padding keys) and of the key ranges (dQ), each in order.  One thread
+// for four columns of a row; the first n_kv workgroups take the keys.
+template <int D>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossBwdParams p, int n_kv) {
+  constexpr int TPR = D / 4;
+  if ((int)blockIdx.x < n_kv) {
+    const long long rows = (long long)p.B * p.Hkv * p.M, gid = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long kr = gid / TPR;
+    if (kr >= rows) return;
+    const int col = (int)(gid - kr * TPR) * 4;
+    const int bh = (int)(kr / p.M), key = (int)(kr - (long long)bh * p.M), b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    f32x4 k = zero4(), v = zero4();
+    if (key < valid_keys(p, b)) {
+      const long long half = rows * D;
+      const float* x = p.part + kr * D + col;
+#pragma unroll 4
+      for (int s = 0; s < p.n_slices; ++s) {
+        k += *reinterpret_cast<const f32x4*>(x + 2 * s * half);
+        v += *reinterpret_cast<const f32x4*>(x + (2 * s + 1) * half);
+      }
+    }
+    bf16x4 wk, wv;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      wk[j] = to_bf16(k[j] * p.scale);
+      wv[j] = to_bf16(v[j]);
+    }
+    *reinterpret_cast<bf16x4*>(p.dk + b * p.sdk.b + hk * p.sdk.h + key * p.sdk.t + col) = wk;
+    *reinterpret_cast<bf16x4*>(p.dv + b * p.sdv.b + hk * p.sdv.h + key * p.sdv.t + col) = wv;
+    return;
   }
+  const long long rows = (long long)p.B * p.Hkv * p.R, gid = (long long)(blockIdx.x - n_kv) * 256 + threadIdx.x;
+  const long long rr = gid / TPR;
+  if (rr >= rows) return;
+  const int col = (int)(gid - rr * TPR) * 4;
+  const int bh = (int)(rr / p.R), r = (int)(rr - (long long)bh * p.R), b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  f32x4 q = zero4();
+#pragma unroll 4
+  for (int s = 0; s < p.n_ranges; ++s) q += *reinterpret_cast<const f32x4*>(p.part_q + (s * rows + rr) * D + col);
+  bf16x4 w;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = to_bf16(q[j] * p.scale);
+  *reinterpret_cast<bf16x4*>(p.dq + row_offset(p.sdq, b, hk, p.G, r) + col) = w;
 }
 
-// dK and dV: the slices' sums in slice order, and zeros for the padding keys.  One thread for four columns.
-template <int D>
-__global__ __launch_bounds__(256) void cross_join_kernel(CrossBwdParams p) {
-  constexpr int TPR = D / 4;
-  const long long rows = (long long)p.B * p.Hkv * p.M, gid = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long kr = gid / TPR;
-  if (kr >= rows) return;
-  const int col = (int)(gid - kr * TPR) * 4;
-  const int bh = (int)(kr / p.M), key = (int)(kr - (long long)bh * p.M), b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  f32x4 k = zero4(), v = zero4();
-  if (key < valid_keys(p, b)) {
-    const long long half = rows * D;
-    const float* x = p.part + kr * D + col;
-    for (int s = 0; s < p.n_slices; ++s, x += 2 * half) {
-      k += *reinterpret_cast<const f32x4*>(x);
-      v += *reinterpret_cast<const f32x4*>(x + half);
-    }
-  }
-  bf16x4 wk, wv;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    wk[j] = to_bf16(k[j] * p.scale);
-    wv[j] = to_bf16(v[j]);
-  }
-  *reinterpret_cast<bf16x4*>(p.dk + b * p.sdk.b + hk * p.sdk.h + key * p.sdk.t + col) = wk;
-  *reinterpret_cast<bf16x4*>(p.dv + b * p.sdv.b + hk * p.sdv.h + key * p.sdv.t + col) = wv;
+template <int NWK, int QG, int BM, int VL>
+hipError_t launch_dkdv(const CrossBwdParams& p, hipStream_t stream) {
+  const int n_ktiles = (p.M + 32 * NWK - 1) / (32 * NWK);
+  const long long grid = (long long)p.B * p.Hkv * n_ktiles * p.n_slices;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((cross_dkdv_kernel<kD, NWK, QG, BM, VL>), dim3((unsigned)grid), dim3(64 * NWK * QG), 0, stream, p,
+                     n_ktiles);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -447,29 +523,35 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossBwdParams p) {
 #define MW_CAT_(a, b) a##b
 #define MW_CAT(a, b) MW_CAT_(a, b)
 hipError_t MW_CAT(launch_cross_bwd_, MW_CROSS_HEAD_DIM)(const CrossBwdParams& p, hipStream_t stream) {
-  const long long rows = (long long)p.B * p.Hkv * p.R, threads = rows * (kD == 64 ? 8 : 16);
-  hipLaunchKernelGGL(cross_rowterms_kernel<kD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p);
+  constexpr int NW = 4;
+  const int n_rtiles = (p.R + 32 * NW - 1) / (32 * NW);
+  const long long grid = (long long)p.B * p.Hkv * n_rtiles * p.n_ranges;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((cross_dq_kernel<kD, NW, 64, kD == 128 ? 2 : 3>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p,
+                     n_rtiles);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int NW = 4;
-  const int n_ktiles = (p.M + 32 * NW - 1) / (32 * NW), n_rtiles = (p.R + 32 * NW - 1) / (32 * NW);
-  const long long n_dkdv = (long long)p.B * p.Hkv * n_ktiles * p.n_slices, first_dq = (n_dkdv + 7) / 8 * 8;
-  const long long grid = first_dq + (long long)p.B * p.Hkv * n_rtiles;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((cross_grad_kernel<kD, NW, kD == 128 ? 32 : 64, 64, kD == 128 ? 1 : 2>), dim3((unsigned)grid),
-                     dim3(64 * NW), 0, stream, p, (int)n_dkdv, (int)first_dq, n_ktiles, n_rtiles);
-  e = hipGetLastError();
-  if (e != hipSuccess || p.n_slices == 1) return e;
-  const long long n = (long long)p.B * p.Hkv * p.M * (kD / 4);
-  hipLaunchKernelGGL(cross_join_kernel<kD>, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, p);
+  e = p.M <= 64 ? launch_dkdv<2, 4, 32, kD == 128 ? 7 : 0>(p, stream) : launch_dkdv<4, 2, 32, kD == 128 ? 6 : 0>(p, stream);
+  if (e != hipSuccess || (p.n_slices == 1 && p.n_ranges == 1)) return e;
+  const long long bhkv = (long long)p.B * p.Hkv;
+  const long long n_kv = p.n_slices > 1 ? (bhkv * p.M * (kD / 4) + 255) / 256 : 0;
+  const long long n_q = p.n_ranges > 1 ? (bhkv * p.R * (kD / 4) + 255) / 256 : 0;
+  hipLaunchKernelGGL(cross_join_kernel<kD>, dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);
   return hipGetLastError();
 }
 
 #if MW_CROSS_HEAD_DIM == 128
+// Slices of the rows: workgroups of eight waves for about one a CU, of at least two steps.
 int cross_bwd_slices(int D, int BHkv, int R, int M) {
   (void)D;
-  const long long tiles = (long long)BHkv * ((M + 127) / 128);
-  return (int)std::max(1LL, std::min({(256 + tiles - 1) / tiles, (long long)R / 256, 64LL}));
+  const long long tiles = (long long)BHkv * (M <= 64 ? 1 : (M + 127) / 128);
+  return (int)std::max(1LL, std::min({256 / tiles, (long long)R / 128, 64LL}));
+}
+// Key ranges of the dQ kernel: workgroups of four waves for about two a CU, of at least two steps.
+int cross_bwd_ranges(int D, int BHkv, int R, int M) {
+  (void)D;
+  const long long tiles = (long long)BHkv * ((R + 127) / 128);
+  return (int)std::max(1LL, std::min({512 / tiles, (long long)M / 128, 64LL}));
 }
 #endif
 

@@ -18,6 +18,8 @@
 // write) and the products are the bf16 ones on the cache's very values.
 #pragma once
 
+#include <type_traits>
+
 #include "mw_device.h"
 #include "mw_kernels.h"
 
@@ -211,9 +213,9 @@ struct CodeTile {
   // Codes of the tile at `kp`, `vp` (row 0 of the tile in its page), of which rows 0..last
   // hold tokens; `e`: index of the block's scales.
   __device__ __forceinline__ void fetch(const uint8_t* kp, const uint8_t* vp, const float* k_scale,
-                                        const float* v_scale, int last, int tid) {
-    ks = *k_scale;
-    vs = *v_scale;
+                                        const float* v_scale, int last, int tid, int vzero) {
+    ks = k_scale[vzero];
+    vs = v_scale[vzero];
 #pragma unroll
     for (int it = 0; it < ROUNDS; ++it) {
       const int p = it * NT + tid;
@@ -255,11 +257,21 @@ struct CodeTile {
       const int p = it * NT + tid;
       if (!WHOLE && p >= PIECES) break;
       const int row = p / PPR, col = (p - row * PPR) * PC;
-#pragma unroll
-      for (int j = 0; j < PC / 8; ++j) {
-        const int at = Tile<D>::off(row0 + row, col + 8 * j);
-        *reinterpret_cast<bf16x8*>(Kt + at) = decode(k[it][2 * j], k[it][2 * j + 1], ks);
-        *reinterpret_cast<bf16x8*>(Vt + at) = decode(v[it][2 * j], v[it][2 * j + 1], vs);
+      if constexpr (PC == 16) {
+        // a piece fills two neighbouring 16-byte slots: odd rows write the upper one first, so that two
+        // rows' writes together cover every bank
+        const bool up = row & 1;
+        const unsigned k0 = k[it][0], k1 = k[it][1], k2 = k[it][2], k3 = k[it][3];
+        const unsigned v0 = v[it][0], v1 = v[it][1], v2 = v[it][2], v3 = v[it][3];
+        const int first = Tile<D>::off(row0 + row, up ? col + 8 : col), second = Tile<D>::off(row0 + row, up ? col : col + 8);
+        *reinterpret_cast<bf16x8*>(Kt + first) = decode(up ? k2 : k0, up ? k3 : k1, ks);
+        *reinterpret_cast<bf16x8*>(Vt + first) = decode(up ? v2 : v0, up ? v3 : v1, vs);
+        *reinterpret_cast<bf16x8*>(Kt + second) = decode(up ? k0 : k2, up ? k1 : k3, ks);
+        *reinterpret_cast<bf16x8*>(Vt + second) = decode(up ? v0 : v2, up ? v1 : v3, vs);
+      } else {
+        const int at = Tile<D>::off(row0 + row, col);
+        *reinterpret_cast<bf16x8*>(Kt + at) = decode(k[it][0], k[it][1], ks);
+        *reinterpret_cast<bf16x8*>(Vt + at) = decode(v[it][0], v[it][1], vs);
       }
     }
   }
@@ -294,7 +306,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
   const int per_head = p.n_rtiles * p.n_splits;
   const int bh = item / per_head;
   const int in_head = item - bh * per_head;
-  const int split = in_head / p.n_rtiles, rt = in_head - split * p.n_rtiles;
+  const int split = in_head / p.n_rtiles, rt = p.n_rtiles - 1 - (in_head - split * p.n_rtiles);  // late rows see more
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
   const int G = p.G, r0 = rt * BM;
 
@@ -329,8 +341,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
     hi_all = (c0 + 1) * p.qlen;
     lo_all = own ? c1 * p.qlen : 0;
   }
-  const int new0 = first / BK, n_newt = last > first ? (last + BK - 1) / BK - new0 : 0;
-  int n_old = 0, seq = 0;
+  int seq = 0;
   if constexpr (PAGED) {
     seq = seqs.seq[b];
     if constexpr (TAIL) {
@@ -340,16 +351,27 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
       for (int i = tid; i < 4 * SLACK; i += NT) (&lds[0][0][0])[(i / SLACK) * TE + BK * D + i % SLACK] = 0;
     }
     len = max(0, min(p.lens[seq], p.W * p.L));
-    n_old = (len + BK - 1) / BK;
   }
-  const int n_all = n_old + n_newt;
+  // The key steps, those that every row sees whole first, so that the mask is evaluated in a
+  // loop of its own: cached steps [0, old_full), bf16 steps [full0, full1), then the partly
+  // filled cached step (old_part of them) and the bf16 steps [new0, full0) and [full1, new1).
+  const int old_full = len / BK, old_part = len > old_full * BK;
+  const int new0 = first / BK, new1 = last > first ? (last + BK - 1) / BK : new0;
+  const int full0 = min(max((lo_all + BK - 1) / BK, new0), new1), full1 = min(max(hi_all / BK, full0), new1);
+  const int n_full = old_full + full1 - full0, n_all = n_full + old_part + (full0 - new0) + (new1 - full1);
   const int beg = (int)((long long)n_all * split / p.n_splits), end = (int)((long long)n_all * (split + 1) / p.n_splits);
+  // Step i: cached step x as x, bf16 step x as ~x.
+  auto place = [&](int i) {
+    if (i < n_full) return i < old_full ? i : ~(full0 + i - old_full);
+    const int j = i - n_full - old_part;
+    if (j < 0) return old_full;
+    return ~(j < full0 - new0 ? new0 + j : full1 + j - (full0 - new0));
+  };
 
   const long long kbase = b * p.sk.b + hk * p.sk.h, vbase = b * p.sv.b + hk * p.sv.h;
   const RowOffsets<D, BK, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
-  // bf16 keys of step i (i >= n_old) straight into LDS
-  auto stage_new = [&](int i, int buf) {
-    const int k0 = (new0 + i - n_old) * BK;
+  // bf16 keys from k0 on straight into LDS
+  auto stage_new = [&](int k0, int buf) {
     if (k0 + BK <= n_new) {
       stage_rows_s<D, BK, NT>(Ks[buf], p.k + kbase + k0 * p.sk.t, ro_k, tid);
       stage_rows_s<D, BK, NT>(Vs[buf], p.v + vbase + k0 * p.sv.t, ro_v, tid);
@@ -360,19 +382,32 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
       }, tid);
     }
   };
-  // cached tokens of step i < n_old into registers
+  // Cached tokens of a step into registers (and from there into LDS).  Their pages are looked up one
+  // step before that.  The lookups and the scales go through vector loads: a scalar load in flight
+  // makes every wait for an LDS read a wait for it too.
   Codes codes[PAGED ? NB : 1];
-  auto fetch = [&](int i) {
+  int vzero;
+  asm volatile("v_mov_b32 %0, 0" : "=v"(vzero));
+  int page_v[PAGED ? NB : 1];
+  auto block_at = [&](int x, int nb) { return min(x * NB + nb, (len - 1) >> 6); };  // one behind the last repeats it
+  auto look = [&](int x) {
     if constexpr (PAGED) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const int pos = min(i * BK + nb * 64, (len - 1) & ~63);  // a block behind the last repeats it
-        const int w = pos / p.L, off = pos - w * p.L;
-        const long long page = p.table[(long long)seq * p.W + w];
-        const long long head = page * p.Hkv + hk;
-        const long long at = (head * p.L + off) * D;
-        const long long e = head * (p.L >> 6) + (off >> 6);
-        codes[nb].fetch(p.k_pages + at, p.v_pages + at, p.k_scales + e, p.v_scales + e, len - 1 - pos, tid);
+        const unsigned w = __umulhi((unsigned)block_at(x, nb), p.per_page_magic);
+        page_v[nb] = p.table[(long long)seq * p.W + (int)(p.per_page == 1 ? block_at(x, nb) : w) + vzero];
+      }
+    }
+  };
+  auto fetch = [&](int x) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int blk = block_at(x, nb);
+        const int off = p.per_page == 1 ? 0 : blk - (int)__umulhi((unsigned)blk, p.per_page_magic) * p.per_page;
+        const long long head = (long long)__builtin_amdgcn_readfirstlane(page_v[nb]) * p.Hkv + hk;
+        const long long e = head * p.per_page + off, at = e * (64 * D);
+        codes[nb].fetch(p.k_pages + at, p.v_pages + at, p.k_scales + e, p.v_scales + e, len - 1 - 64 * blk, tid, vzero);
       }
     }
   };
@@ -388,53 +423,50 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
   RB rb;
   rb.init();
   const float c = p.scale_log2;
-  auto compute = [&](int i, int buf) {
-    if (PAGED && i < n_old) {
-      const int k0 = i * BK;
-      if (k0 + BK <= len) {
-        rb.template step<false>(Ks[buf], Vs[buf], fo, ft, qf, c, 0, 0, 0, lane);
-      } else {
-        rb.template step<true>(Ks[buf], Vs[buf], fo, ft, qf, c, k0 + kg * BN, 0, len, lane);
-      }
-      return;
-    }
-    const int k0 = (new0 + i - n_old) * BK;
-    if (k0 >= lo_all && k0 + BK <= hi_all) {
-      rb.template step<false>(Ks[buf], Vs[buf], fo, ft, qf, c, 0, 0, 0, lane);
-    } else {
-      rb.template step<true>(Ks[buf], Vs[buf], fo, ft, qf, c, k0 + kg * BN, lo, hi, lane);
-    }
-  };
-
   if (beg < end) {
     // Two LDS stages.  A cached step is in registers one step before it is written to LDS,
     // and in LDS one step before it is used; a bf16 step goes to LDS during the step before it.
-    if (PAGED && beg < n_old) {
-      fetch(beg);
+    int x = place(beg), next = beg + 1 < end ? place(beg + 1) : -1;  // this step and the one behind it
+    int after = beg + 2 < end ? place(beg + 2) : -1;
+    if (PAGED && x >= 0) {
+      look(x);
+      fetch(x);
       commit(0);
-      if (beg + 1 < min(end, n_old)) fetch(beg + 1);
     } else {
-      stage_new(beg, 0);
+      stage_new(~x * BK, 0);
       wait_vmem();
     }
-    lds_barrier();
-    int buf = 0;
-    for (int i = beg; i < end; ++i) {
-      bool direct = false;
-      if (i + 1 < end) {
-        if (PAGED && i + 1 < n_old) {
-          commit(buf ^ 1);
-          if (i + 2 < min(end, n_old)) fetch(i + 2);
-        } else {
-          stage_new(i + 1, buf ^ 1);
-          direct = true;
-        }
-      }
-      compute(i, buf);
-      if (direct) wait_vmem();
-      lds_barrier();
-      buf ^= 1;
+    if (PAGED && next >= 0) {
+      look(next);
+      fetch(next);
     }
+    if (PAGED && after >= 0) look(after);
+    lds_barrier();
+    int buf = 0, i = beg;
+    auto run = [&](auto masked, int stop) {
+      for (; i < stop; ++i) {
+        const int later = i + 3 < end ? place(i + 3) : -1;
+        const bool more = i + 1 < end, direct = more && (!PAGED || next < 0);
+        if (direct) {
+          stage_new(~next * BK, buf ^ 1);
+        } else if (more) {
+          commit(buf ^ 1);
+        }
+        if (PAGED && after >= 0) fetch(after);
+        if (PAGED && later >= 0) look(later);
+        const bool old = PAGED && x >= 0;
+        const int k0 = (old ? x : ~x) * BK + kg * BN;
+        rb.template step<decltype(masked)::value>(Ks[buf], Vs[buf], fo, ft, qf, c, k0, old ? 0 : lo, old ? len : hi, lane);
+        if (direct) wait_vmem();
+        lds_barrier();
+        buf ^= 1;
+        x = next;
+        next = after;
+        after = later;
+      }
+    };
+    run(std::false_type{}, min(n_full, end));
+    run(std::true_type{}, end);
   }
 
   if constexpr (KG > 1) {

@@ -33,7 +33,8 @@ template <bool PAGED>
 hipError_t launch_rows(const RowsParams& p, const RowsSeqs<PAGED>& seqs, const RowsPlan& plan, hipStream_t stream) {
   if (plan.bm == 32) return launch_tile<PAGED, 4, 32, 4, 2>(p, seqs, plan, stream);
   if (plan.bm == 64) return launch_tile<PAGED, 4, 32, 2, 2>(p, seqs, plan, stream);
-  return launch_tile<PAGED, 4, 64, 1, 2>(p, seqs, plan, stream);
+  if (plan.bm == 128) return launch_tile<PAGED, 4, 64, 1, kD == 128 ? 2 : (kD == 64 && !PAGED ? 4 : 3)>(p, seqs, plan, stream);
+  return launch_tile<PAGED, 8, 64, 1, 1>(p, seqs, plan, stream);
 }
 
 }  // namespace

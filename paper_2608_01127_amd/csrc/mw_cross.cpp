@@ -83,13 +83,25 @@ int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t
                                   : launch_cross_128(p, plan, hs));
 }
 
-// Row terms (two fp32 a row), then the fp32 dK and dV of the slices.
-static size_t row_bytes(int B, int H, int T) { return round256((size_t)B * H * T * sizeof(float)); }
+// Workspace of the backward: row terms (two fp32 a row), the fp32 dK and dV of the slices, the fp32 dQ of the
+// key ranges.
+struct CrossBwdLayout {
+  int n_slices, n_ranges;
+  size_t rows, part, part_q;  // bytes of one row term, of the slices and of the ranges
+  CrossBwdLayout(int B, int H, int Hkv, int T, int M, int D) {
+    const int R = T * (H / Hkv);
+    n_slices = cross_bwd_slices(D, B * Hkv, R, M);
+    n_ranges = cross_bwd_ranges(D, B * Hkv, R, M);
+    rows = round256((size_t)B * H * T * sizeof(float));
+    part = n_slices > 1 ? round256((size_t)n_slices * 2 * B * Hkv * M * D * sizeof(float)) : 0;
+    part_q = n_ranges > 1 ? round256((size_t)n_ranges * B * H * T * D * sizeof(float)) : 0;
+  }
+  size_t bytes() const { return 2 * rows + part + part_q; }
+};
 
 size_t mw_cross_attn_bwd_workspace_size(int B, int H, int Hkv, int T, int M, int D) {
   if (check_cross("mw_cross_attn_bwd_workspace_size", B, H, Hkv, T, M, D)) return 0;
-  const int n = cross_bwd_slices(D, B * Hkv, T * (H / Hkv), M);
-  return 2 * row_bytes(B, H, T) + (n > 1 ? (size_t)n * 2 * B * Hkv * M * D * sizeof(float) : 0);
+  return CrossBwdLayout(B, H, Hkv, T, M, D).bytes();
 }
 
 int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t* kv_len, const void* o, const void* d_o,
@@ -103,7 +115,8 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
   if (st) return st;
   if (!good_scale(scale)) return fail(MW_EINVAL, "%s: scale must be finite and > 0", fn);
   if (!aligned16(kv_len)) return fail(MW_EALIGN, "%s: kv_len is not 16-byte aligned", fn);
-  const size_t need = mw_cross_attn_bwd_workspace_size(B, H, Hkv, T, M, D);
+  const CrossBwdLayout lay(B, H, Hkv, T, M, D);
+  const size_t need = lay.bytes();
   if (workspace_bytes < need)
     return fail(MW_EINVAL, "%s: workspace of %zu bytes is smaller than the %zu bytes needed", fn, workspace_bytes, need);
   Strides sv[8];
@@ -129,8 +142,9 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
   p.dv = static_cast<uint16_t*>(dv);
   char* ws = static_cast<char*>(workspace);
   p.delta = reinterpret_cast<float*>(ws);
-  p.lse2 = reinterpret_cast<float*>(ws + row_bytes(B, H, T));
-  p.part = reinterpret_cast<float*>(ws + 2 * row_bytes(B, H, T));
+  p.lse2 = reinterpret_cast<float*>(ws + lay.rows);
+  p.part = reinterpret_cast<float*>(ws + 2 * lay.rows);
+  p.part_q = reinterpret_cast<float*>(ws + 2 * lay.rows + lay.part);
   p.sq = sv[0];
   p.sk = sv[1];
   p.sv = sv[2];
@@ -145,7 +159,8 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
   p.T = T;
   p.R = T * p.G;
   p.M = M;
-  p.n_slices = cross_bwd_slices(D, B * Hkv, p.R, M);
+  p.n_slices = lay.n_slices;
+  p.n_ranges = lay.n_ranges;
   p.scale = scale;
   p.scale_log2 = scale * kLog2e;
   hipStream_t hs = static_cast<hipStream_t>(stream);

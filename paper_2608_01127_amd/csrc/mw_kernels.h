@@ -342,6 +342,8 @@ struct RowsParams {
   const int* table;
   const int* lens;
   int L, W;
+  int per_page;             // blocks of 64 tokens in a page
+  unsigned per_page_magic;  // ceil(2^32 / per_page): block / per_page is the high word of their product
   // n_rtiles row tiles of a key head over n_splits key ranges (set by the launcher)
   int n_rtiles, n_splits;
   float* part;  // [n_splits][B Hkv][R][D] unnormalised O, then [n_splits][B Hkv][R][2] (m, l)
@@ -371,15 +373,17 @@ struct CrossBwdParams {
   uint16_t* dq;
   uint16_t* dk;
   uint16_t* dv;
-  float* delta;  // [B Hkv][R]: -rowsum(dO O)
-  float* lse2;   // [B Hkv][R]: LSE log2 e (rows without a key: +inf)
-  float* part;   // n_slices > 1: [n_slices][2][B Hkv][M][D] fp32 dK, dV of a slice of the rows
+  float* delta;   // [B Hkv][R]: -rowsum(dO O)
+  float* lse2;    // [B Hkv][R]: LSE log2 e
+  float* part;    // n_slices > 1: [n_slices][2][B Hkv][M][D] fp32 dK, dV of a slice of the rows
+  float* part_q;  // n_ranges > 1: [n_ranges][B Hkv][R][D] fp32 dQ of a range of the keys
   Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   int B, Hkv, G, T, R, M;
-  int n_slices;
+  int n_slices, n_ranges;
   float scale, scale_log2;
 };
 int cross_bwd_slices(int D, int BHkv, int R, int M);
+int cross_bwd_ranges(int D, int BHkv, int R, int M);
 hipError_t launch_cross_bwd_64(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_72(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_128(const CrossBwdParams& p, hipStream_t stream);

@@ -51,9 +51,10 @@ int check_sizes(const char* fn, int P, int H, int L, int D, int N, int W) {
   if (D != 64 && D != 72 && D != 128)
     return fail(MW_EUNSUPPORTED, "%s: head dimension %d is not supported (64, 72 or 128)", fn, D);
   if (L % MW_PAGE_BLOCK) return fail(MW_EINVAL, "%s: L = %d is not a multiple of %d", fn, L, MW_PAGE_BLOCK);
-  if (P > (1 << 24) || N > (1 << 16) || H > (1 << 14) || (long long)W * L > kMaxT || (long long)N * W > (1LL << 28) ||
+  // (L up to 2^16: block numbers below 2^18 are then divided exactly by the high word of a product)
+  if (P > (1 << 24) || N > (1 << 16) || L > (1 << 16) || H > (1 << 14) || (long long)W * L > kMaxT || (long long)N * W > (1LL << 28) ||
       (long long)H * L * D > (1LL << 30))
-    return fail(MW_EUNSUPPORTED, "%s: P, N, H, W * L, N * W or H * L * D is too large", fn);
+    return fail(MW_EUNSUPPORTED, "%s: P, N, H, L, W * L, N * W or H * L * D is too large", fn);
   return MW_OK;
 }
 
@@ -468,6 +469,8 @@ int mw_chunk_attn_paged(const void* q, const void* k_new, const void* v_new, int
   p.lens = pool.lens;
   p.L = c->L;
   p.W = c->W;
+  p.per_page = c->L / MW_PAGE_BLOCK;
+  p.per_page_magic = (unsigned)(((1ULL << 32) + p.per_page - 1) / p.per_page);  // (2^32 wraps to 0 at 1, which is not used)
   p.part = static_cast<float*>(workspace);
   const RowsPlan plan = paged_plan(c, seqs, n_seqs, H, T, workspace != nullptr ? workspace_bytes : 0);
   hipStream_t hs = static_cast<hipStream_t>(stream);
