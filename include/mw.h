@@ -518,7 +518,7 @@ size_t mw_kvpages_host_bytes(int P, int N, int W);
  * D: 64, 72 or 128.
  * Errors: MW_EINVAL (null, sizes < 1, L, host block too small), MW_EALIGN,
  * MW_EUNSUPPORTED (D; P > 2^24, N > 2^16, H > 2^14, L > 2^16, W * L > 2^24, N * W > 2^28 or
- * H * L * D > 2^30). */
+ * H * L * D > 2^30 or P * H * L / 64 >= 2^31). */
 int mw_kvpages_init(mw_kvpages* c, void* k_pages, void* v_pages, float* k_scales, float* v_scales, int32_t* table,
                     int32_t* lens, int32_t* host, size_t host_bytes, int P, int H, int L, int D, int N, int W);
 

@@ -438,29 +438,11 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
       }
     return;
   }
-  if constexpr (TAIL) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int r = rt * BM + wave * 32 + 16 * e + (lane & 15);
-      if (lane < 32 && r < R) {
-        bf16x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = to_bf16(tail[e][j] * p.scale);
-        *reinterpret_cast<bf16x4*>(p.dq + row_offset(p.sdq, b, hk, G, r) + 64 + 4 * (lane >> 4)) = w;
-      }
-    }
-  }
-  if (row >= R) return;
-  bf16_t* dst = p.dq + row_offset(p.sdq, b, hk, G, row);
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      bf16x4 w;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = to_bf16(dq[db][4 * g + j] * p.scale);
-      *reinterpret_cast<bf16x4*>(dst + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
-    }
+  // (every wave has passed the last barrier: a half stage holds the rows of BN / 32 waves)
+  static_assert(NW <= 2 * (BN / 32), "one stage holds the rows of every wave");
+  const int r0 = rt * BM + wave * 32, half = wave / (BN / 32);
+  store_rows<D>(dq, tail, (half ? Vs : Ks)[0] + (wave - half * (BN / 32)) * 32 * D, min(32, R - r0), lane, p.scale,
+                [&](int r) { return p.dq + row_offset(p.sdq, b, hk, G, r0 + r); });
 }
 
 // Sums of the slices (dK, dV; zeros for the padding keys) and of the key ranges (dQ), each in order.  One thread

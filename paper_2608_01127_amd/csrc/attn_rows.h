@@ -25,6 +25,8 @@
 
 namespace mw {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
 // Sequence of each batch member (paged calls), by value: a call keeps no memory of the caller's.
 template <bool PAGED>
 struct RowsSeqs {
@@ -39,6 +41,47 @@ __device__ __forceinline__ long long row_offset(const Strides& s, int b, int hk,
 
 // Barrier that waits for this wave's LDS accesses and leaves its global loads in flight.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// A wave's 32 x D result (accumulator layout: lane l, register i of block db holds column 32 db + 8 (i / 4) +
+// 4 (l / 32) + i % 4 of row l % 32; at D = 72 `tail` holds the last eight) as bf16 rows in memory, by way of `x`, the
+// wave's own 32 rows of an LDS tile: 16 bytes a lane, whole rows at once.  Storing from the accumulators, 8 bytes a
+// lane and 16 to a row, cost 10 of 51 us at 12 heads x 19200 rows x 128 keys (D = 128).  `mul` scales the lane's row;
+// `row_ptr(r)` is the address of row r of the block, of which there are n.
+template <int D, class RowPtr>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[D / 32], const f32x4 (&tail)[2], bf16_t* x, int n, int lane,
+                                           float mul, RowPtr row_ptr) {
+  constexpr int DB = D / 32, PPR = D / 8;
+  const int row = lane & 31;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = to_bf16(acc[db][4 * g + j] * mul);
+      *reinterpret_cast<bf16x4*>(x + Tile<D>::off(row, db * 32 + 8 * g + 4 * (lane >> 5))) = w;
+    }
+  if constexpr (D % 32 != 0) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 16 * e + (lane & 15);
+      const float m = __shfl(mul, r);
+      bf16x4 w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = to_bf16(tail[e][j] * m);
+      if (lane < 32) *reinterpret_cast<bf16x4*>(x + Tile<D>::off(r, 64 + 4 * (lane >> 4))) = w;
+    }
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own rows: no barrier)
+#pragma unroll
+  for (int p0 = 0; p0 < 32 * PPR; p0 += 64) {
+    const int p = p0 + lane, r = p / PPR, slot = p - r * PPR;
+    if (r < n) {  // (n <= 32)
+      const u32x4 w = *reinterpret_cast<const u32x4*>(x + r * D + slot * 8);
+      *reinterpret_cast<u32x4*>(row_ptr(r) + (slot ^ Tile<D>::swz(r)) * 8) = w;
+    }
+  }
+}
 
 // Online softmax and output of 32 rows of a wave (row = lane % 32), as S^T = K Q^T and
 // O^T += V^T P^T (layouts at the top of mw_device.h).
@@ -73,15 +116,24 @@ struct RowBlock {
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] = mfma32(fo.row8(Kt, kb * 32, kk), qf[kk], s[kb]);
-    if constexpr (MASKED) {
+    if constexpr (MASKED) hide(s, key0, lo, hi, lane);
+    weigh(s, c, lane);
+    add(s, [&](int kb, int t, int db) { return fo.tr8(Vt, kb * 32, t, db); }, [&](int kb) { return ft.read(Vt, kb * 32); });
+  }
+
+  // Scores of keys that the row does not see: -inf.
+  __device__ __forceinline__ static void hide(f32x16 (&s)[KB], int key0, int lo, int hi, int lane) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + kb * 32 + acc_row(i, lane);
-          s[kb][i] = ((key >= lo) & (key < hi)) ? s[kb][i] : -INFINITY;
-        }
-    }
+      for (int i = 0; i < 16; ++i) {
+        const int key = key0 + kb * 32 + acc_row(i, lane);
+        s[kb][i] = ((key >= lo) & (key < hi)) ? s[kb][i] : -INFINITY;
+      }
+  }
+
+  // Scores -> probabilities against the running maximum; their sum.
+  __device__ __forceinline__ void weigh(f32x16 (&s)[KB], float c, int lane) {
     float mx = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -113,7 +165,12 @@ struct RowBlock {
         sum += s[kb][i];
       }
     l += sum;
-    // the probabilities go to the matrix product in bf16; their sum stays in 32 bits
+  }
+
+  // O^T += V^T P^T; the probabilities go to the matrix product in bf16 (their sum stays in 32 bits).  vf(kb, t, db):
+  // V fragment of 16-key step t and column block db of key block kb; vt(kb): (TAIL) that of columns 64...
+  template <class VF, class VT>
+  __device__ __forceinline__ void add(const f32x16 (&s)[KB], VF vf, VT vt) {
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       bf16x8 p[2];
@@ -121,13 +178,13 @@ struct RowBlock {
       for (int t = 0; t < 2; ++t) {
         p[t] = pack8(s[kb], t);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] = mfma32(fo.tr8(Vt, kb * 32, t, db), p[t], o[db]);
+        for (int db = 0; db < DB; ++db) o[db] = mfma32(vf(kb, t, db), p[t], o[db]);
       }
       if constexpr (TAIL) {
-        const bf16x8 vt = ft.read(Vt, kb * 32);
+        const bf16x8 x = vt(kb);
         tail_operands(p[0], p[1]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) ot[e] = mfma16(vt, p[e], ot[e]);
+        for (int e = 0; e < 2; ++e) ot[e] = mfma16(x, p[e], ot[e]);
       }
     }
   }
@@ -157,7 +214,7 @@ struct RowBlock {
       }
     }
     __syncthreads();
-    if (kg > 0) return;
+    if (kg > 0) return;  // (the caller's barrier follows)
     float M = m, w[KG];
 #pragma unroll
     for (int g = 1; g < KG; ++g) {
@@ -196,6 +253,62 @@ struct RowBlock {
     m = M;
   }
 };
+
+// Results of rows t0.. of key head bh = (b, hk): of one key range of several as an unnormalised fp32 O and the pair
+// (m, l), else O and LSE.  x: LDS scratch of 32 rows.
+template <int D, int BN>
+__device__ __forceinline__ void finish_rows(const RowsParams& p, const RowBlock<D, BN>& rb, int split, int bh, int b, int hk,
+                                            int t0, bf16_t* x, int lane) {
+  constexpr int DB = D / 32;
+  constexpr bool TAIL = D % 32 != 0;
+  const int row = t0 + (lane & 31), G = p.G;
+  const float l = sum_halves(rb.l);
+  if (p.n_splits > 1) {
+    const long long prow = ((long long)split * p.B * p.Hkv + bh) * p.R;
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = t0 + 16 * e + (lane & 15);
+        if (lane < 32 && r < p.R) *reinterpret_cast<f32x4*>(p.part + (prow + r) * D + 64 + 4 * (lane >> 4)) = rb.ot[e];
+      }
+    }
+    if (row >= p.R) return;
+    float* po = p.part + (prow + row) * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = rb.o[db][4 * g + j];
+        *reinterpret_cast<f32x4*>(po + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
+      }
+    if (lane < 32) {
+      float* ml = p.part + (long long)p.n_splits * p.B * p.Hkv * p.R * D + 2 * (prow + row);
+      ml[0] = rb.m;
+      ml[1] = l;
+    }
+    return;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that saw no key gives zeros
+  store_rows<D>(rb.o, rb.ot, x, min(32, p.R - t0), lane, inv,
+                [&](int r) { return p.o + row_offset(p.so, b, hk, G, t0 + r); });
+  if (p.lse != nullptr && lane < 32 && row < p.R) {
+    const int t = row / G;
+    p.lse[((long long)b * p.Hkv * G + hk * G + (row - t * G)) * p.T + t] =
+        l == 0.f ? -INFINITY : (rb.m + __log2f(l)) * 0.69314718055994530942f;
+  }
+}
+
+// Eight codes (two words) -> bf16 values at a power-of-two scale.
+__device__ __forceinline__ bf16x8 decode(unsigned w0, unsigned w1, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 
 // A tile of 64 cached tokens of one head on its way into LDS: this thread's pieces of the K
 // and V codes in registers.  Pieces of 16 codes (8 at D = 72, whose 72-byte rows are only
@@ -238,16 +351,6 @@ struct CodeTile {
         }
       }
     }
-  }
-
-  // Eight codes (two words) -> bf16 values at a power-of-two scale.
-  __device__ __forceinline__ static bf16x8 decode(unsigned w0, unsigned w1, float scale) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false);
-    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true);
-    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false);
-    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   }
 
   // The tile in bf16 into LDS rows row0.. of the K and V tiles.
@@ -308,7 +411,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
   const int in_head = item - bh * per_head;
   const int split = in_head / p.n_rtiles, rt = p.n_rtiles - 1 - (in_head - split * p.n_rtiles);  // late rows see more
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
-  const int G = p.G, r0 = rt * BM;
+  const int G = p.G;
+  const int r0 = rt * BM;
 
   // this lane's row and its Q fragments; rows behind the last and columns past D are zeros
   const int row = r0 + rw * 32 + (lane & 31);
@@ -420,14 +524,15 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
 
   const FragOffsets<D> fo(lane, kg * BN * D);
   const Tail72 ft(lane, kg * BN * D);
+  const float c = p.scale_log2;
   RB rb;
   rb.init();
-  const float c = p.scale_log2;
+  int buf = 0;
   if (beg < end) {
-    // Two LDS stages.  A cached step is in registers one step before it is written to LDS,
-    // and in LDS one step before it is used; a bf16 step goes to LDS during the step before it.
+    // Two LDS stages.  A cached step is in registers one step before it is written to LDS, and in LDS one step
+    // before it is used; a bf16 step goes to LDS during the step before it.
     int x = place(beg), next = beg + 1 < end ? place(beg + 1) : -1;  // this step and the one behind it
-    int after = beg + 2 < end ? place(beg + 2) : -1;
+    int after = PAGED && beg + 2 < end ? place(beg + 2) : -1;
     if (PAGED && x >= 0) {
       look(x);
       fetch(x);
@@ -442,11 +547,13 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
     }
     if (PAGED && after >= 0) look(after);
     lds_barrier();
-    int buf = 0, i = beg;
+    int i = beg;
     auto run = [&](auto masked, int stop) {
       for (; i < stop; ++i) {
-        const int later = i + 3 < end ? place(i + 3) : -1;
-        const bool more = i + 1 < end, direct = more && (!PAGED || next < 0);
+        const int later = PAGED && i + 3 < end ? place(i + 3) : -1;
+        const bool more = i + 1 < end;
+        if (!PAGED && more) next = place(i + 1);
+        const bool direct = more && (!PAGED || next < 0);
         if (direct) {
           stage_new(~next * BK, buf ^ 1);
         } else if (more) {
@@ -468,71 +575,281 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
     run(std::false_type{}, min(n_full, end));
     run(std::true_type{}, end);
   }
-
   if constexpr (KG > 1) {
     rb.template merge<KG, NWR>(kg, rw, lane, reinterpret_cast<float*>(&lds[0][0][0]));
+    __syncthreads();     // (the stages are written again below)
     if (kg > 0) return;  // no barrier follows
   }
-  const float l = sum_halves(rb.l);
-  const float inv = l == 0.f ? 0.f : 1.f / l;  // a row that saw no key gives zeros
-  if (p.n_splits > 1) {
-    // unnormalised partial of this key range: O, and the pair (m, l)
-    const long long prow = ((long long)split * p.B * p.Hkv + bh) * p.R;
-    if constexpr (TAIL) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = r0 + rw * 32 + 16 * e + (lane & 15);
-        if (lane < 32 && r < p.R)
-          *reinterpret_cast<f32x4*>(p.part + (prow + r) * D + 64 + 4 * (lane >> 4)) = rb.ot[e];
-      }
-    }
-    if (row >= p.R) return;
-    float* po = p.part + (prow + row) * D;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        f32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = rb.o[db][4 * g + j];
-        *reinterpret_cast<f32x4*>(po + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
-      }
-    if (lane < 32) {
-      float* ml = p.part + (long long)p.n_splits * p.B * p.Hkv * p.R * D + 2 * (prow + row);
-      ml[0] = rb.m;
-      ml[1] = l;
-    }
-    return;
+
+  // scratch: a half stage holds the rows of BK / 32 waves (every wave has passed the last barrier)
+  constexpr int PER = BK / 32;
+  const int half = rw / PER;
+  finish_rows<D, BN>(p, rb, split, bh, b, hk, r0 + rw * 32, (half & 1 ? Vs : Ks)[half >> 1] + (rw - half * PER) * 32 * D, lane);
+}
+
+// Few rows over pages (RB blocks of 32 rows): bound by reading the codes, so nothing is shared and nothing waits but
+// for them.  Each of NW waves streams units of 32 tokens of its own, every NW-th of the workgroup's key range, through
+// NSTG private LDS stages: codes go there as they are (32 rows of a head are contiguous in a page), NSTG - 1 units
+// ahead, and are converted as the fragments are read; no barrier separates the steps.  K: 16 codes of a row a lane,
+// eight for each of two contraction steps (Q's fragments follow that order).  V: ds_read_b64_tr_b8 gives a lane the
+// codes of eight keys of its column (in each group of 16 lanes, byte j of lane i is byte i % 8 of the 8 bytes
+// addressed by lane 2 j + i / 8).  The waves' results are joined at the end.
+template <int D>
+struct RawTile {  // 32 rows of D codes, 16-byte slots permuted so that row and transposing reads spread over the banks
+  static constexpr int SLOTS = D / 16;
+  static constexpr int ROUNDS = (32 * D + 1023) / 1024;  // 1 KB loads of a tile
+  static constexpr int BYTES = ROUNDS * 1024;
+  __device__ __forceinline__ static int swz(int row) {
+    if constexpr (D == 128) return (row & 7) ^ ((row >> 1) & 4);
+    if constexpr (D == 64) return (row >> 2) & 3;
+    return 0;  // D = 72: rows are dense, 18 banks apart
   }
-  if constexpr (TAIL) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float iv = __shfl(inv, 16 * e + (lane & 15));
-      const int r = r0 + rw * 32 + 16 * e + (lane & 15);
-      if (lane < 32 && r < p.R) {
-        bf16x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = to_bf16(rb.ot[e][j] * iv);
-        *reinterpret_cast<bf16x4*>(p.o + row_offset(p.so, b, hk, G, r) + 64 + 4 * (lane >> 4)) = w;
-      }
+  __device__ __forceinline__ static int off(int row, int col) {  // col: a multiple of 8
+    if constexpr (D == 72) return row * D + col;
+    return row * D + (((col >> 4) ^ swz(row)) << 4) + (col & 15);
+  }
+  // byte of the (unswizzled) tile that lane `lane` of load `it` fetches; rows behind `last` repeat it
+  __device__ __forceinline__ static unsigned source(int it, int lane, int last) {
+    if constexpr (D == 72) {
+      // (144 pieces of 16 bytes do not end with a row: two halves of 8 could; `last` is met by the reader instead)
+      (void)last;
+      return (unsigned)min(it * 64 + lane, 32 * D / 16 - 1) * 16u;
+    } else {
+      const int p = it * 64 + lane, row = p / SLOTS, slot = p - row * SLOTS;
+      return (unsigned)(min(row, last) * D + ((slot ^ swz(row)) << 4));
     }
   }
-  if (row >= p.R) return;
-  bf16_t* orow = p.o + row_offset(p.so, b, hk, G, row);
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      bf16x4 w;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = to_bf16(rb.o[db][4 * g + j] * inv);
-      *reinterpret_cast<bf16x4*>(orow + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
-    }
-  if (p.lse != nullptr && lane < 32) {
-    const int t = row / G;
-    p.lse[((long long)b * p.Hkv * G + hk * G + (row - t * G)) * p.T + t] =
-        l == 0.f ? -INFINITY : (rb.m + __log2f(l)) * 0.69314718055994530942f;
+};
+
+constexpr int kMetaBlocks = 256;  // blocks of 64 tokens whose page and scales are looked up at a time
+
+template <int D, int RB, int NW, int NSTG>
+__global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(RowsParams p, RowsSeqs<true> seqs, int chunk) {
+  using RT = RawTile<D>;
+  using Rows = RowBlock<D, 32>;
+  constexpr int KK = Rows::KK, DB = Rows::DB, LOADS = 2 * RT::ROUNDS;
+  constexpr bool TAIL = Rows::TAIL;
+  static_assert(NSTG >= 2 && NSTG <= 4 && LOADS * (NSTG - 1) <= 63, "the wait counts the units in flight");
+  constexpr int STAGE = 2 * RT::BYTES;
+  constexpr int MERGE = RB * Rows::template merge_floats<NW, 1>() * 4;
+  constexpr int STREAM = NW * NSTG * STAGE;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[STREAM > MERGE ? STREAM : MERGE];
+  __shared__ int meta_page[kMetaBlocks];
+  __shared__ float meta_k[kMetaBlocks], meta_v[kMetaBlocks];
+
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int item;
+  {
+    const int n = gridDim.x, x = blockIdx.x % 8, q = n / 8, rem = n % 8;
+    item = x * q + min(x, rem) + blockIdx.x / 8;
   }
+  const int bh = item / p.n_splits, split = item - bh * p.n_splits;
+  const int b = bh / p.Hkv, hk = bh - b * p.Hkv, G = p.G;
+  const int seq = seqs.seq[b], len = max(0, min(p.lens[seq], p.W * p.L));
+  // this workgroup's blocks: `chunk` of them, the last range whatever is left
+  const int n_blk = (len + 63) >> 6;
+  const int blk0 = min(n_blk, split * chunk), blk1 = split + 1 == p.n_splits ? n_blk : min(n_blk, blk0 + chunk);
+
+  bf16x8 qf[RB][KK];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = rb * 32 + (lane & 31);
+    const bf16_t* qp = p.q + row_offset(p.sq, b, hk, G, min(row, p.R - 1));
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      // steps 2 j and 2 j + 1: columns 32 j + 16 h + 0..7 and + 8..15; (D = 72) step 4: columns 64..71 and zeros
+      const int col = TAIL && kk == KK - 1 ? 64 : 32 * (kk / 2) + 16 * h + 8 * (kk & 1);
+      if (row < p.R && !(TAIL && kk == KK - 1 && h)) {
+        qf[rb][kk] = *reinterpret_cast<const bf16x8*>(qp + col);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[rb][kk][j] = (__bf16)0.f;
+      }
+    }
+  }
+  Rows rows[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) rows[rb].init();
+
+  unsigned char* mine = lds + wave * NSTG * STAGE;
+  const float c = p.scale_log2;
+  // this lane's part of the transposing reads: row and column within 32 keys x 32 columns
+  const int tr_row = 4 * h + (((lane & 15) >> 1) & 3) + 8 * ((lane & 15) >> 3), tr_col = 16 * ((lane >> 4) & 1) + 8 * (lane & 1);
+
+  for (int m0 = blk0; m0 < blk1; m0 += kMetaBlocks) {
+    const int m1 = min(blk1, m0 + kMetaBlocks);
+    if (m0 > blk0) __syncthreads();
+    for (int i = tid; i < m1 - m0; i += 64 * NW) {
+      const int blk = m0 + i;
+      const int w = p.per_page == 1 ? blk : (int)__umulhi((unsigned)blk, p.per_page_magic);
+      const long long at = ((long long)p.table[(long long)seq * p.W + w] * p.Hkv + hk) * p.per_page + (blk - w * p.per_page);
+      // (the page's block of this head; below 2^31: P H L / 64 is checked)
+      meta_page[i] = (int)at;
+      meta_k[i] = p.k_scales[at];
+      meta_v[i] = p.v_scales[at];
+    }
+    __syncthreads();
+    // Q is waited for here, not by the compiler's count inside the loop, which does not know of the loads into LDS
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[rb][kk]));
+    // units of 32 tokens of these blocks: every NW-th is this wave's
+    const int units = (min(len, m1 * 64) - m0 * 64 + 31) >> 5;
+    auto issue = [&](int u, int st) {
+      const long long at = ((long long)__builtin_amdgcn_readfirstlane(meta_page[u >> 1]) * 64 + 32 * (u & 1)) * D;
+      const int last = min(31, len - 1 - m0 * 64 - u * 32);
+      const unsigned to = lds_addr(mine) + st * STAGE;
+#pragma unroll
+      for (int it = 0; it < RT::ROUNDS; ++it) {
+        const unsigned src = RT::source(it, lane, last);
+        dma_lds_16_s(p.k_pages + at, src, __builtin_amdgcn_readfirstlane(to + it * 1024));
+        dma_lds_16_s(p.v_pages + at, src, __builtin_amdgcn_readfirstlane(to + RT::BYTES + it * 1024));
+      }
+    };
+    int ahead = 0, u_in = wave, st_in = 0, st = 0;
+#pragma unroll
+    for (int i = 0; i < NSTG - 1; ++i)
+      if (u_in < units) {
+        issue(u_in, st_in);
+        u_in += NW;
+        ++st_in;
+        ++ahead;
+      }
+    if (st_in == NSTG) st_in = 0;
+    for (int u = wave; u < units; u += NW) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage to be filled has been read
+      if (u_in < units) {
+        issue(u_in, st_in);
+        u_in += NW;
+        st_in = st_in + 1 == NSTG ? 0 : st_in + 1;
+        ++ahead;
+      }
+      --ahead;
+      wait_vmem_upto<LOADS, NSTG - 1>(ahead);
+      asm volatile("" ::: "memory");
+      const unsigned char* Kt = mine + st * STAGE;
+      const unsigned char* Vt = Kt + RT::BYTES;
+      const float ks = meta_k[u >> 1], vs = meta_v[u >> 1];
+      const int last = len - 1 - m0 * 64 - u * 32;  // last token of the unit, if below 31
+      // (D = 72: rows behind it hold whatever the page does)
+      const int krow = TAIL ? min(lane & 31, last) : lane & 31;
+      f32x16 s[RB][1];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) s[rb][0] = zero16();
+#pragma unroll
+      for (int j = 0; j < KK / 2; ++j) {
+        unsigned w[4];
+        if constexpr (TAIL) {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(Kt + krow * D + 32 * j + 16 * h);
+          const u32x2 y = *reinterpret_cast<const u32x2*>(Kt + krow * D + 32 * j + 16 * h + 8);
+          w[0] = x[0], w[1] = x[1], w[2] = y[0], w[3] = y[1];
+        } else {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(Kt + RT::off(krow, 32 * j + 16 * h));
+          w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+        }
+        const bf16x8 k0 = decode(w[0], w[1], ks), k1 = decode(w[2], w[3], ks);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          s[rb][0] = mfma32(k0, qf[rb][2 * j], s[rb][0]);
+          s[rb][0] = mfma32(k1, qf[rb][2 * j + 1], s[rb][0]);
+        }
+      }
+      if constexpr (TAIL) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(Kt + krow * D + 64);
+        const bf16x8 k0 = decode(h ? 0u : x[0], h ? 0u : x[1], ks);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[rb][0] = mfma32(k0, qf[rb][KK - 1], s[rb][0]);
+      }
+      const bool ragged = last < 31;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        if (ragged) Rows::hide(s[rb], 0, 0, last + 1, lane);
+        rows[rb].weigh(s[rb], c, lane);
+      }
+      // each V fragment is read and converted once for all row blocks
+      bf16x8 pb[RB][2];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) pb[rb][t] = pack8(s[rb][0], t);
+      auto read_v = [&](int row, int col) {
+        const unsigned char* at = Vt + (TAIL ? min(row, last) * D + col : RT::off(row, col));
+        const auto x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((MW_LDS i32x2*)(at));
+        return decode((unsigned)x[0], (unsigned)x[1], vs);
+      };
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const bf16x8 vf = read_v(16 * t + tr_row, 32 * db + tr_col);
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) rows[rb].o[db] = mfma32(vf, pb[rb][t], rows[rb].o[db]);
+        }
+      if constexpr (TAIL) {
+        // lane group g holds rows row(g % 2, 8 (g / 2) + j) of columns 64..71 (Tail72); its other eight are not kept
+        const int g = lane >> 4, i = lane & 15;
+        const bf16x8 vf = read_v(16 * (g & 1) + 4 * (g >> 1) + ((i >> 1) & 3) + 8 * (i >> 3), 64);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+          tail_operands(pb[rb][0], pb[rb][1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) rows[rb].ot[e] = mfma16(vf, pb[rb][e], rows[rb].ot[e]);
+        }
+      }
+      st = st + 1 == NSTG ? 0 : st + 1;
+    }
+  }
+
+  // the queued tokens' own keys, 32 at a time, by the waves of the first range in turn
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  if (split == 0) {
+    bf16_t* Vt = reinterpret_cast<bf16_t*>(mine);
+    const FragOffsets<D> fo(lane, 0);
+    const Tail72 ft(lane, 0);
+    const long long kbase = b * p.sk.b + hk * p.sk.h, vbase = b * p.sv.b + hk * p.sv.h;
+    for (int k0 = wave * 32; k0 < p.M; k0 += 32 * NW) {
+      const bf16_t* kp = p.k + kbase + (long long)min(k0 + (lane & 31), p.M - 1) * p.sk.t;
+      f32x16 s[RB][1];
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) s[rb][0] = zero16();
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const int col = TAIL && kk == KK - 1 ? 64 : 32 * (kk / 2) + 16 * h + 8 * (kk & 1);
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + col);  // (D = 72: Q is zero where h = 1 repeats column 64)
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[rb][0] = mfma32(kf, qf[rb][kk], s[rb][0]);
+      }
+#pragma unroll
+      for (int it = 0; it < (32 * D / 8 + 63) / 64; ++it) {
+        const int q = it * 64 + lane, r = q / (D / 8), slot = q - r * (D / 8);
+        if (r < 32)
+          *reinterpret_cast<u32x4*>(Vt + Tile<D>::off(r, slot * 8)) =
+              *reinterpret_cast<const u32x4*>(p.v + vbase + (long long)min(k0 + r, p.M - 1) * p.sv.t + slot * 8);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const int c0 = min(rb * 32 + (lane & 31), p.R - 1) / G / p.qlen;
+        const int hi = p.mode == ROWS_SEE_ALL ? p.M : min(p.M, (c0 + 1) * p.qlen), lo = p.mode == ROWS_SEE_OWN ? c0 * p.qlen : 0;
+        Rows::hide(s[rb], k0, lo, hi, lane);
+        rows[rb].weigh(s[rb], c, lane);
+        rows[rb].add(s[rb], [&](int, int t, int db) { return fo.tr8(Vt, 0, t, db); }, [&](int) { return ft.read(Vt, 0); });
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+
+  __syncthreads();
+  float* x = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) rows[rb].template merge<NW, 1>(wave, 0, lane, x + rb * Rows::template merge_floats<NW, 1>());
+  __syncthreads();
+  if (wave > 0) return;  // no barrier follows
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb)
+    if (rb * 32 < p.R) finish_rows<D, 32>(p, rows[rb], split, bh, b, hk, rb * 32, reinterpret_cast<bf16_t*>(lds), lane);
 }
 
 // Join of the key ranges' partials: with M the largest m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s

@@ -13,6 +13,14 @@ constexpr int kD = MW_ROWS_HEAD_DIM;
 
 namespace {
 
+hipError_t join_ranges(const RowsParams& p, hipStream_t stream) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.n_splits == 1) return e;
+  const long long threads = (long long)p.B * p.Hkv * p.R * (kD / 4);
+  hipLaunchKernelGGL(attn_rows_join_kernel<kD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
 template <bool PAGED, int NW, int BN, int KG, int WPS>
 hipError_t launch_tile(RowsParams p, const RowsSeqs<PAGED>& seqs, const RowsPlan& plan, hipStream_t stream) {
   constexpr int BM = 32 * NW / KG;
@@ -22,18 +30,30 @@ hipError_t launch_tile(RowsParams p, const RowsSeqs<PAGED>& seqs, const RowsPlan
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
   hipLaunchKernelGGL((attn_rows_kernel<kD, PAGED, NW, BN, KG, WPS>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p,
                      seqs);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.n_splits == 1) return e;
-  const long long threads = (long long)p.B * p.Hkv * p.R * (kD / 4);
-  hipLaunchKernelGGL(attn_rows_join_kernel<kD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, p);
-  return hipGetLastError();
+  return join_ranges(p, stream);
 }
+
+#ifdef MW_ROWS_PAGED
+// Four waves; units in flight a wave beside the one it works on: 3.
+template <int RB>
+hipError_t launch_pages(RowsParams p, const RowsSeqs<true>& seqs, const RowsPlan& plan, hipStream_t stream) {
+  p.n_splits = plan.n_splits;
+  const long long grid = (long long)p.B * p.Hkv * p.n_splits;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((attn_pages_kernel<kD, RB, 4, 4>), dim3((unsigned)grid), dim3(256), 0, stream, p, seqs, plan.chunk);
+  return join_ranges(p, stream);
+}
+#endif
 
 template <bool PAGED>
 hipError_t launch_rows(const RowsParams& p, const RowsSeqs<PAGED>& seqs, const RowsPlan& plan, hipStream_t stream) {
-  if (plan.bm == 32) return launch_tile<PAGED, 4, 32, 4, 2>(p, seqs, plan, stream);
+  if constexpr (PAGED) {
+    if (plan.chunk > 0) return p.R <= 32 ? launch_pages<1>(p, seqs, plan, stream) : launch_pages<2>(p, seqs, plan, stream);
+  } else {
+    if (plan.bm == 32) return launch_tile<PAGED, 4, 32, 4, 2>(p, seqs, plan, stream);
+  }
   if (plan.bm == 64) return launch_tile<PAGED, 4, 32, 2, 2>(p, seqs, plan, stream);
-  if (plan.bm == 128) return launch_tile<PAGED, 4, 64, 1, kD == 128 ? 2 : (kD == 64 && !PAGED ? 4 : 3)>(p, seqs, plan, stream);
+  if (plan.bm == 128) return launch_tile<PAGED, 4, 64, 1, kD == 128 || (kD == 72 && PAGED) ? 2 : 3>(p, seqs, plan, stream);
   return launch_tile<PAGED, 8, 64, 1, 1>(p, seqs, plan, stream);
 }
 
@@ -56,9 +76,19 @@ size_t rows_part_bytes(int D, int BHkv, int R, int n_splits) {
   return n_splits <= 1 ? 0 : (size_t)n_splits * BHkv * R * (D + 2) * sizeof(float);
 }
 
-RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws_bytes) {
-  (void)paged;
-  RowsPlan plan{128, 1};
+RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, long long all_blocks, size_t ws_bytes) {
+  RowsPlan plan{128, 1, 0};
+  auto fits = [&](long long ns) { return rows_part_bytes(D, BHkv, R, (int)ns) <= ws_bytes; };
+  if (paged && R <= 64) {
+    // attn_pages_kernel: ranges of equally many blocks, about one workgroup a CU, at least four blocks each
+    plan.bm = R <= 32 ? 32 : 64;
+    const long long longest = std::max(1LL, (keys + 63) / 64);
+    long long chunk = std::max(4LL, (all_blocks + 255) / 256);
+    while ((longest + chunk - 1) / chunk > 1 && !fits((longest + chunk - 1) / chunk)) chunk = chunk * 2;
+    plan.chunk = (int)chunk;
+    plan.n_splits = (int)((longest + chunk - 1) / chunk);
+    return plan;
+  }
   if (R <= 32) {
     plan.bm = 32;
   } else if (R <= 64 || (long long)BHkv * ((R + 127) / 128) < 256) {
@@ -67,7 +97,7 @@ RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws
   const long long wgs = (long long)BHkv * ((R + plan.bm - 1) / plan.bm);
   const long long steps = (keys + 127) / 128;
   long long ns = std::min({(512 + wgs - 1) / wgs, std::max(1LL, steps / 2), 64LL});
-  while (ns > 1 && rows_part_bytes(D, BHkv, R, (int)ns) > ws_bytes) --ns;
+  while (ns > 1 && !fits(ns)) --ns;
   plan.n_splits = (int)std::max(1LL, ns);
   return plan;
 }

@@ -348,11 +348,13 @@ struct RowsParams {
   int n_rtiles, n_splits;
   float* part;  // [n_splits][B Hkv][R][D] unnormalised O, then [n_splits][B Hkv][R][2] (m, l)
 };
-// How a call is divided: rows of a tile and key ranges.
+// How a call is divided: rows of a tile and key ranges; chunk > 0: ranges of that many blocks of 64 cached tokens (few
+// rows over pages, the last range takes what is left).
 struct RowsPlan {
-  int bm, n_splits;
+  int bm, n_splits, chunk;
 };
-RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws_bytes);
+// keys: the longest batch member's; all_blocks: blocks of 64 cached tokens of all members and key heads.
+RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, long long all_blocks, size_t ws_bytes);
 size_t rows_part_bytes(int D, int BHkv, int R, int n_splits);
 hipError_t launch_cross_64(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
 hipError_t launch_cross_72(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);

@@ -53,8 +53,8 @@ int check_sizes(const char* fn, int P, int H, int L, int D, int N, int W) {
   if (L % MW_PAGE_BLOCK) return fail(MW_EINVAL, "%s: L = %d is not a multiple of %d", fn, L, MW_PAGE_BLOCK);
   // (L up to 2^16: block numbers below 2^18 are then divided exactly by the high word of a product)
   if (P > (1 << 24) || N > (1 << 16) || L > (1 << 16) || H > (1 << 14) || (long long)W * L > kMaxT || (long long)N * W > (1LL << 28) ||
-      (long long)H * L * D > (1LL << 30))
-    return fail(MW_EUNSUPPORTED, "%s: P, N, H, L, W * L, N * W or H * L * D is too large", fn);
+      (long long)H * L * D > (1LL << 30) || (long long)P * H * (L / MW_PAGE_BLOCK) > 0x7fffffffLL)
+    return fail(MW_EUNSUPPORTED, "%s: P, N, H, L, W * L, N * W, H * L * D or P * H * L is too large", fn);
   return MW_OK;
 }
 
@@ -404,9 +404,16 @@ static int check_paged_call(const char* fn, const mw_kvpages* c, const int32_t* 
 }
 
 static RowsPlan paged_plan(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int tokens, size_t ws_bytes) {
-  long long keys = 0;
-  for (int i = 0; i < n_seqs; ++i) keys = std::max<long long>(keys, book(c).lens[seqs[i]]);
-  return rows_plan(c->D, true, n_seqs * c->H, tokens * (H / c->H), keys + tokens, ws_bytes);
+  const Book b = book(c);
+  const int R = tokens * (H / c->H);
+  long long longest = 0, blocks = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    const int len = b.lens[seqs[i]];
+    longest = std::max<long long>(longest, len);
+    blocks += (len + MW_PAGE_BLOCK - 1) / MW_PAGE_BLOCK;
+  }
+  // (few rows: the queued keys go along with the first range)
+  return rows_plan(c->D, true, n_seqs * c->H, R, R <= 64 ? longest : longest + tokens, blocks * c->H, ws_bytes);
 }
 
 size_t mw_chunk_attn_paged_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int n_queued,
