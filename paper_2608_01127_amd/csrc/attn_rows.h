@@ -587,6 +587,12 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
   finish_rows<D, BN>(p, rb, split, bh, b, hk, r0 + rw * 32, (half & 1 ? Vs : Ks)[half >> 1] + (rw - half * PER) * 32 * D, lane);
 }
 
+// Sequences of a call of few rows, and their key ranges: those of batch member b are numbers first[b] .. first[b + 1].
+struct PageRanges {
+  int seq[kMaxSeqs];
+  int first[kMaxSeqs + 1];
+};
+
 // Few rows over pages (RB blocks of 32 rows): bound by reading the codes, so nothing is shared and nothing waits but
 // for them.  Each of NW waves streams units of 32 tokens of its own, every NW-th of the workgroup's key range, through
 // NSTG private LDS stages: codes go there as they are (32 rows of a head are contiguous in a page), NSTG - 1 units
@@ -624,32 +630,44 @@ struct RawTile {  // 32 rows of D codes, 16-byte slots permuted so that row and 
 constexpr int kMetaBlocks = 256;  // blocks of 64 tokens whose page and scales are looked up at a time
 
 template <int D, int RB, int NW, int NSTG>
-__global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(RowsParams p, RowsSeqs<true> seqs, int chunk) {
+__global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(RowsParams p, PageRanges seqs, int chunk) {
   using RT = RawTile<D>;
   using Rows = RowBlock<D, 32>;
   constexpr int KK = Rows::KK, DB = Rows::DB, LOADS = 2 * RT::ROUNDS;
   constexpr bool TAIL = Rows::TAIL;
   static_assert(NSTG >= 2 && NSTG <= 4 && LOADS * (NSTG - 1) <= 63, "the wait counts the units in flight");
   constexpr int STAGE = 2 * RT::BYTES;
-  constexpr int MERGE = RB * Rows::template merge_floats<NW, 1>() * 4;
+  constexpr int MERGE = RB * NW * (DB * 16 + 2 + (TAIL ? 8 : 0)) * 64 * 4;
   constexpr int STREAM = NW * NSTG * STAGE;
   __shared__ __attribute__((aligned(16))) unsigned char lds[STREAM > MERGE ? STREAM : MERGE];
-  __shared__ int meta_page[kMetaBlocks];
+  __shared__ int meta_block[kMetaBlocks];
+  static_assert(64 * NW == kMetaBlocks, "a thread looks up one block");
   __shared__ float meta_k[kMetaBlocks], meta_v[kMetaBlocks];
 
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int item;
-  {
-    const int n = gridDim.x, x = blockIdx.x % 8, q = n / 8, rem = n % 8;
-    item = x * q + min(x, rem) + blockIdx.x / 8;
+  // Workgroup = (range number, key head).  No two read the same codes, so they go round the XCDs as they come.
+  const int range = blockIdx.x / p.Hkv, hk = blockIdx.x - range * p.Hkv;
+  int b = -1;  // the last member whose first range is not behind this one
+  for (int i = 0; i < p.B; i += 64) {
+    const int first = seqs.first[min(i + lane, p.B)];
+    b += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < p.B && first <= range));
   }
-  const int bh = item / p.n_splits, split = item - bh * p.n_splits;
-  const int b = bh / p.Hkv, hk = bh - b * p.Hkv, G = p.G;
-  const int seq = seqs.seq[b], len = max(0, min(p.lens[seq], p.W * p.L));
+  b = __builtin_amdgcn_readfirstlane(b);
+  const int split = range - seqs.first[b], n_ranges = seqs.first[b + 1] - seqs.first[b];
+  const int bh = b * p.Hkv + hk, G = p.G;
+  const int seq = seqs.seq[b];
+  // The pages of the range's first blocks are looked up before the length is known (an entry of the row is
+  // always readable; what lies behind the length is not used): one memory latency less before the codes stream.
+  auto entry = [&](int blk) {
+    const int w = p.per_page == 1 ? blk : (int)__umulhi((unsigned)blk, p.per_page_magic);
+    return make_int2(p.table[(long long)seq * p.W + min(w, p.W - 1)], blk - w * p.per_page);
+  };
+  int2 my_entry = entry(split * chunk + tid);
+  const int len = max(0, min(p.lens[seq], p.W * p.L));
   // this workgroup's blocks: `chunk` of them, the last range whatever is left
   const int n_blk = (len + 63) >> 6;
-  const int blk0 = min(n_blk, split * chunk), blk1 = split + 1 == p.n_splits ? n_blk : min(n_blk, blk0 + chunk);
+  const int blk0 = min(n_blk, split * chunk), blk1 = split + 1 == n_ranges ? n_blk : min(n_blk, blk0 + chunk);
 
   bf16x8 qf[RB][KK];
 #pragma unroll
@@ -679,16 +697,14 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
 
   for (int m0 = blk0; m0 < blk1; m0 += kMetaBlocks) {
     const int m1 = min(blk1, m0 + kMetaBlocks);
-    if (m0 > blk0) __syncthreads();
-    for (int i = tid; i < m1 - m0; i += 64 * NW) {
-      const int blk = m0 + i;
-      const int w = p.per_page == 1 ? blk : (int)__umulhi((unsigned)blk, p.per_page_magic);
-      const long long at = ((long long)p.table[(long long)seq * p.W + w] * p.Hkv + hk) * p.per_page + (blk - w * p.per_page);
-      // (the page's block of this head; below 2^31: P H L / 64 is checked)
-      meta_page[i] = (int)at;
-      meta_k[i] = p.k_scales[at];
-      meta_v[i] = p.v_scales[at];
+    if (m0 > blk0) {
+      __syncthreads();
+      my_entry = entry(m0 + tid);
     }
+    // (the page's block of this head: below 2^31, P H L / 64 is checked)
+    const int my_block = (int)(((long long)my_entry.x * p.Hkv + hk) * p.per_page + my_entry.y);
+    const bool known = tid < m1 - m0;
+    if (known) meta_block[tid] = my_block;
     __syncthreads();
     // Q is waited for here, not by the compiler's count inside the loop, which does not know of the loads into LDS
 #pragma unroll
@@ -698,7 +714,7 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
     // units of 32 tokens of these blocks: every NW-th is this wave's
     const int units = (min(len, m1 * 64) - m0 * 64 + 31) >> 5;
     auto issue = [&](int u, int st) {
-      const long long at = ((long long)__builtin_amdgcn_readfirstlane(meta_page[u >> 1]) * 64 + 32 * (u & 1)) * D;
+      const long long at = ((long long)__builtin_amdgcn_readfirstlane(meta_block[u >> 1]) * 64 + 32 * (u & 1)) * D;
       const int last = min(31, len - 1 - m0 * 64 - u * 32);
       const unsigned to = lds_addr(mine) + st * STAGE;
 #pragma unroll
@@ -708,6 +724,9 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
         dma_lds_16_s(p.v_pages + at, src, __builtin_amdgcn_readfirstlane(to + RT::BYTES + it * 1024));
       }
     };
+    // the blocks' scales, a thread each, ahead of the codes
+    dma_lds_4(p.k_scales + (known ? my_block : 0), lds_addr(meta_k) + wave * 256);
+    dma_lds_4(p.v_scales + (known ? my_block : 0), lds_addr(meta_v) + wave * 256);
     int ahead = 0, u_in = wave, st_in = 0, st = 0;
 #pragma unroll
     for (int i = 0; i < NSTG - 1; ++i)
@@ -718,6 +737,8 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
         ++ahead;
       }
     if (st_in == NSTG) st_in = 0;
+    wait_vmem_upto<LOADS, NSTG - 1>(ahead);  // the scales; the first codes are on their way
+    lds_barrier();
     for (int u = wave; u < units; u += NW) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage to be filled has been read
       if (u_in < units) {
@@ -841,21 +862,105 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
     }
   }
 
+  // Join of the waves' results: column block db of every row block (and the tail) is one wave's to add up, with the
+  // weights 2^(m_w - M), and to store.
   __syncthreads();
-  float* x = reinterpret_cast<float*>(lds);
+  float* x = reinterpret_cast<float*>(lds) + lane;
+  constexpr int N = DB * 16 + 2 + (TAIL ? 8 : 0);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) rows[rb].template merge<NW, 1>(wave, 0, lane, x + rb * Rows::template merge_floats<NW, 1>());
+  for (int rb = 0; rb < RB; ++rb) {
+    float* y = x + (rb * NW + wave) * N * 64;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[(db * 16 + i) * 64] = rows[rb].o[db][i];
+    y[DB * 16 * 64] = rows[rb].m;
+    y[(DB * 16 + 1) * 64] = rows[rb].l;
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[(DB * 16 + 2 + i) * 64] = rows[rb].ot[i / 4][i % 4];
+    }
+  }
   __syncthreads();
-  if (wave > 0) return;  // no barrier follows
+  static_assert(DB + TAIL <= NW, "a column block a wave");
+  if (wave >= DB + TAIL) return;  // no barrier follows
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-    if (rb * 32 < p.R) finish_rows<D, 32>(p, rows[rb], split, bh, b, hk, rb * 32, reinterpret_cast<bf16_t*>(lds), lane);
+  for (int rb = 0; rb < RB; ++rb) {
+    const float* y = x + rb * NW * N * 64;
+    float w[NW], M = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int g = 0; g < NW; ++g) {
+      w[g] = y[(g * N + DB * 16) * 64];
+      M = fmaxf(M, w[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < NW; ++g) {
+      w[g] = w[g] == -INFINITY ? 0.f : fast_exp2(w[g] - M);
+      l = fmaf(w[g], y[(g * N + DB * 16 + 1) * 64], l);
+    }
+    l = sum_halves(l);
+    const int row = rb * 32 + (lane & 31);
+    const bool one = p.n_splits == 1;
+    const float inv = one ? (l == 0.f ? 0.f : 1.f / l) : 1.f;  // a row that saw no key gives zeros
+    const long long prow = ((long long)split * p.B * p.Hkv + bh) * p.R;
+    auto put = [&](int r, int col, const f32x4& v) {  // four columns of row r
+      if (one) {
+        bf16x4 u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = to_bf16(v[j]);
+        *reinterpret_cast<bf16x4*>(p.o + row_offset(p.so, b, hk, G, r) + col) = u;
+      } else {
+        *reinterpret_cast<f32x4*>(p.part + (prow + r) * D + col) = v;
+      }
+    };
+    if (!TAIL || wave < DB) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v = zero4();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+          for (int g = 0; g < NW; ++g) v[j] = fmaf(w[g], y[(g * N + wave * 16 + 4 * q + j) * 64], v[j]);
+          v[j] *= inv;
+        }
+        if (row < p.R) put(row, wave * 32 + 8 * q + 4 * h, v);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 16 * e + (lane & 15);
+        f32x4 v = zero4();
+#pragma unroll
+        for (int g = 0; g < NW; ++g) {
+          const float wg = __shfl(w[g], r);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = fmaf(wg, y[(g * N + DB * 16 + 2 + 4 * e + j) * 64], v[j]);
+        }
+        const float iv = __shfl(inv, r);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] *= iv;
+        if (lane < 32 && rb * 32 + r < p.R) put(rb * 32 + r, 64 + 4 * (lane >> 4), v);
+      }
+    }
+    if (wave == 0 && lane < 32 && row < p.R) {
+      if (!one) {
+        float* ml = p.part + (long long)p.n_splits * p.B * p.Hkv * p.R * D + 2 * (prow + row);
+        ml[0] = M;
+        ml[1] = l;
+      } else if (p.lse != nullptr) {
+        const int t = row / G;
+        p.lse[((long long)b * p.Hkv * G + hk * G + (row - t * G)) * p.T + t] =
+            l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994530942f;
+      }
+    }
+  }
 }
 
 // Join of the key ranges' partials: with M the largest m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s
 // and LSE = (M + log2 of that sum) ln 2.  One thread for four columns of a row.
-template <int D>
-__global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsParams p) {
+// A call of few rows over pages (PAGES) has ranges of its own for each batch member.
+template <int D, bool PAGES>
+__global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsParams p, std::conditional_t<PAGES, PageRanges, int> seqs) {
   constexpr int TPR = D / 4;
   const long long rows = (long long)p.B * p.Hkv * p.R;
   const long long gid = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -865,15 +970,17 @@ __global__ __launch_bounds__(256) void attn_rows_join_kernel(RowsParams p) {
   const int bh = (int)(pr / p.R), r = (int)(pr - (long long)bh * p.R);
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
   const float* ml = p.part + (long long)p.n_splits * rows * D;
+  int n = p.n_splits;
+  if constexpr (PAGES) n = seqs.first[b + 1] - seqs.first[b];
   float M = -INFINITY, L = 0.f;
   f32x4 acc = zero4();
-  constexpr int U = 4;  // ranges in flight
-  for (int s0 = 0; s0 < p.n_splits; s0 += U) {
+  constexpr int U = 8;  // ranges in flight
+  for (int s0 = 0; s0 < n; s0 += U) {
     float mv[U], lv[U];
     f32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u < p.n_splits;
+      const bool in = s0 + u < n;
       const long long x = (long long)(in ? s0 + u : s0) * rows + pr;
       mv[u] = in ? ml[2 * x] : -INFINITY;
       lv[u] = ml[2 * x + 1];

@@ -353,15 +353,21 @@ struct RowsParams {
 struct RowsPlan {
   int bm, n_splits, chunk;
 };
-// keys: the longest batch member's; all_blocks: blocks of 64 cached tokens of all members and key heads.
-RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, long long all_blocks, size_t ws_bytes);
+// keys: the longest batch member's.
+RowsPlan rows_plan(int D, int BHkv, int R, long long keys, size_t ws_bytes);
+// Few rows over pages: `blocks` of 64 cached tokens of each sequence.
+constexpr int kPagesRows = 64;
+RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t ws_bytes);
 size_t rows_part_bytes(int D, int BHkv, int R, int n_splits);
 hipError_t launch_cross_64(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
 hipError_t launch_cross_72(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
 hipError_t launch_cross_128(const RowsParams& p, const RowsPlan& plan, hipStream_t stream);
-hipError_t launch_paged_64(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
-hipError_t launch_paged_72(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
-hipError_t launch_paged_128(const RowsParams& p, const int* seqs, const RowsPlan& plan, hipStream_t stream);
+hipError_t launch_paged_64(const RowsParams& p, const int* seqs, const int* blocks, const RowsPlan& plan,
+                           hipStream_t stream);
+hipError_t launch_paged_72(const RowsParams& p, const int* seqs, const int* blocks, const RowsPlan& plan,
+                           hipStream_t stream);
+hipError_t launch_paged_128(const RowsParams& p, const int* seqs, const int* blocks, const RowsPlan& plan,
+                           hipStream_t stream);
 
 // Backward of the cross attention (attn_cross_bwd.hip).
 struct CrossBwdParams {

@@ -403,24 +403,26 @@ static int check_paged_call(const char* fn, const mw_kvpages* c, const int32_t* 
   return MW_OK;
 }
 
-static RowsPlan paged_plan(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int tokens, size_t ws_bytes) {
+// blocks: room for MW_MAX_SEQS; the blocks of 64 cached tokens of each sequence.
+static RowsPlan paged_plan(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int tokens, size_t ws_bytes,
+                           int* blocks) {
   const Book b = book(c);
   const int R = tokens * (H / c->H);
-  long long longest = 0, blocks = 0;
+  int longest = 0;
   for (int i = 0; i < n_seqs; ++i) {
-    const int len = b.lens[seqs[i]];
-    longest = std::max<long long>(longest, len);
-    blocks += (len + MW_PAGE_BLOCK - 1) / MW_PAGE_BLOCK;
+    longest = std::max(longest, b.lens[seqs[i]]);
+    blocks[i] = (b.lens[seqs[i]] + MW_PAGE_BLOCK - 1) / MW_PAGE_BLOCK;
   }
-  // (few rows: the queued keys go along with the first range)
-  return rows_plan(c->D, true, n_seqs * c->H, R, R <= 64 ? longest : longest + tokens, blocks * c->H, ws_bytes);
+  if (R <= kPagesRows) return pages_plan(c->D, R, blocks, n_seqs, c->H, ws_bytes);
+  return rows_plan(c->D, n_seqs * c->H, R, (long long)longest + tokens, ws_bytes);
 }
 
 size_t mw_chunk_attn_paged_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int n_queued,
                                           int q_len) {
   if (check_paged_call("mw_chunk_attn_paged_workspace_size", c, seqs, n_seqs, H, n_queued, q_len)) return 0;
   const int tokens = n_queued * q_len;
-  const RowsPlan plan = paged_plan(c, seqs, n_seqs, H, tokens, (size_t)-1);
+  int blocks[MW_MAX_SEQS];
+  const RowsPlan plan = paged_plan(c, seqs, n_seqs, H, tokens, (size_t)-1, blocks);
   return rows_part_bytes(c->D, n_seqs * c->H, tokens * (H / c->H), plan.n_splits);
 }
 
@@ -479,11 +481,12 @@ int mw_chunk_attn_paged(const void* q, const void* k_new, const void* v_new, int
   p.per_page = c->L / MW_PAGE_BLOCK;
   p.per_page_magic = (unsigned)(((1ULL << 32) + p.per_page - 1) / p.per_page);  // (2^32 wraps to 0 at 1, which is not used)
   p.part = static_cast<float*>(workspace);
-  const RowsPlan plan = paged_plan(c, seqs, n_seqs, H, T, workspace != nullptr ? workspace_bytes : 0);
+  int blocks[MW_MAX_SEQS];
+  const RowsPlan plan = paged_plan(c, seqs, n_seqs, H, T, workspace != nullptr ? workspace_bytes : 0, blocks);
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  return hip_status(fn, D == 64   ? launch_paged_64(p, seqs, plan, hs)
-                        : D == 72 ? launch_paged_72(p, seqs, plan, hs)
-                                  : launch_paged_128(p, seqs, plan, hs));
+  return hip_status(fn, D == 64   ? launch_paged_64(p, seqs, blocks, plan, hs)
+                        : D == 72 ? launch_paged_72(p, seqs, blocks, plan, hs)
+                                  : launch_paged_128(p, seqs, blocks, plan, hs));
 }
 
 }  // extern "C"
