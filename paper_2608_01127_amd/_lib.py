@@ -566,11 +566,14 @@ def mw_chunk_attn_cached_fp8(q8, k8_new, v8_new, n_queued: int, q_len: int, cach
 
 # ----------------------------------------------------------------------------- cross attention
 
+_HERE = contextlib.nullcontext()
+
+
 def _on_device(dev):
     """The calls below launch on the current device: make `dev` current for one that is not."""
     torch = _torch()
-    if not torch.cuda.is_initialized() or torch.cuda.current_device() == dev.index:
-        return contextlib.nullcontext()
+    if not torch.cuda.is_initialized() or torch._C._cuda_getDevice() == dev.index:
+        return _HERE
     return torch.cuda.device(dev)
 
 
@@ -584,24 +587,35 @@ def _check_like(name, t, shape, dev):
 
 
 def _check_workspace(workspace, dev):
-    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+    if workspace is None:
+        return 0
+    if workspace.device != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the device of the inputs")
-    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return workspace.nbytes
 
 
-def _cross_args(q, k, v, kv_len):
+def _cross_args(q, k, v, kv_len, rows, keys):
+    """Sizes of a cross attention call.  q and the tensors `rows` (name -> tensor or None) are [B,H,T,D], k, v and
+    `keys` [B,Hkv,M,D]."""
     torch = _torch()
-    for n, t in (("q", q), ("k", k), ("v", v)):
-        _bf16_4d(n, t, view=True)
+    if not (_plain_views([q, *(t for t in rows.values() if t is not None)], q.shape, q)
+            and _plain_views([k, v, *(t for t in keys.values() if t is not None)], k.shape, q)):
+        for n, t in (("q", q), ("k", k), ("v", v)):
+            _bf16_4d(n, t, view=True)
+        for n, t in rows.items():
+            if t is not None:
+                _check_like(n, t, q.shape, q.device)
+        for n, t in (("k", k), ("v", v), *keys.items()):
+            if t is not None:
+                _check_like(n, t, k.shape, q.device)
     B, H, T, D = q.shape
-    Hkv, M = k.shape[1], k.shape[2]
+    if k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"k and v must be [B,Hkv,M,D] with B, D = {B}, {D}, got {tuple(k.shape)}")
     dev = q.device
-    for n, t in (("k", k), ("v", v)):
-        _check_like(n, t, (B, Hkv, M, D), dev)
-    if kv_len is not None and (kv_len.dtype != torch.int32 or tuple(kv_len.shape) != (B,) or kv_len.device != dev
+    if kv_len is not None and (kv_len.dtype != torch.int32 or kv_len.shape != (B,) or kv_len.device != dev
                                or not kv_len.is_contiguous()):
         raise ValueError(f"kv_len must be a contiguous int32 tensor of shape {(B,)} on the device of the inputs")
-    return B, H, Hkv, T, M, D, dev
+    return B, H, k.shape[1], T, k.shape[2], D, dev
 
 
 def mw_cross_attn_workspace_size(B: int, H: int, Hkv: int, T: int, M: int, D: int) -> int:
@@ -615,10 +629,9 @@ def mw_cross_attn_fwd(q, k, v, kv_len=None, scale=None, out=None, lse=None, work
 
     With no workspace given, one of the size the library asks for is allocated here (torch)."""
     torch = _torch()
-    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len)
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, {"out": out}, {})
     scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
     o = torch.empty_like(q) if out is None else out
-    _check_like("out", o, (B, H, T, D), dev)
     lse = torch.empty((B, H, T), dtype=torch.float32, device=dev) if lse is None else lse
     _check_lse(lse, (B, H, T), dev)
     if workspace is None:
@@ -640,9 +653,7 @@ def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=N
     """Backward of mw_cross_attn_fwd.  Returns (dq, dk, dv): bf16 [B,H,T,D] and twice [B,Hkv,M,D], the latter
     summed over the query heads that share a key head and 0 behind kv_len."""
     torch = _torch()
-    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len)
-    for n, t in (("o", o), ("d_o", d_o)):
-        _check_like(n, t, (B, H, T, D), dev)
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, {"o": o, "d_o": d_o, "dq": dq}, {"dk": dk, "dv": dv})
     if lse is None:
         raise ValueError("lse is required")
     _check_lse(lse, (B, H, T), dev)
@@ -654,9 +665,6 @@ def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=N
     dq = torch.empty((B, H, T, D), dtype=q.dtype, device=dev) if dq is None else dq
     dk = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dk is None else dk
     dv = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dv is None else dv
-    _check_like("dq", dq, (B, H, T, D), dev)
-    for n, t in (("dk", dk), ("dv", dv)):
-        _check_like(n, t, (B, Hkv, M, D), dev)
     with _on_device(dev):
         _check(load().mw_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(d_o), _ptr(lse), _ptr(dq),
                                         _ptr(dk), _ptr(dv), _ptr(workspace), nbytes,
@@ -688,15 +696,12 @@ class KVPages:
                                                     device=device) for _ in range(2))
         self.table = torch.empty((N, W), dtype=torch.int32, device=device)
         self.lens = torch.zeros((N,), dtype=torch.int32, device=device)
+        self.device = device
         self._host = (ctypes.c_int32 * (need // 4))()
         self.desc = mw_kvpages()
         _check(load().mw_kvpages_init(ctypes.byref(self.desc), _ptr(self.k_pages), _ptr(self.v_pages),
                                       _ptr(self.k_scales), _ptr(self.v_scales), _ptr(self.table), _ptr(self.lens),
                                       ctypes.addressof(self._host), need, P, H, L, D, N, W))
-
-    @property
-    def device(self):
-        return self.k_pages.device
 
     @property
     def n_free(self) -> int:
@@ -716,16 +721,19 @@ def _seq_array(seqs):
 
 def _seqs(seqs):
     """Host array of sequence numbers (the library only reads it)."""
-    return _seq_array(tuple(int(s) for s in seqs))
+    if isinstance(seqs, ctypes.Array):
+        return seqs
+    return _seq_array(tuple(map(int, seqs)))
 
 
 def mw_kvpages_append(cache: KVPages, seqs, k, v) -> None:
     """Commit k, v (bf16 [len(seqs),H,n_tokens,D] views) to the ends of the listed sequences."""
     d, dev = cache.desc, cache.device
     seqs = _seqs(seqs)
-    for n, t in (("k", k), ("v", v)):
-        _bf16_4d(n, t, view=True)
-        _check_like(n, t, (len(seqs), d.H, k.shape[2], d.D), dev)
+    if not _plain_views((k, v), k.shape, cache.k_pages) or (k.shape[0], k.shape[1], k.shape[3]) != (len(seqs), d.H, d.D):
+        for n, t in (("k", k), ("v", v)):
+            _bf16_4d(n, t, view=True)
+            _check_like(n, t, (len(seqs), d.H, k.shape[2], d.D), dev)
     with _on_device(dev):
         _check(load().mw_kvpages_append(ctypes.byref(d), seqs, len(seqs), _ptr(k), _ptr(v), _strides(k, v), k.shape[2],
                                         _stream_handle(dev)))
@@ -779,17 +787,16 @@ def mw_chunk_attn_paged(q, k_new, v_new, n_queued: int, q_len: int, cache: KVPag
     d, dev = cache.desc, cache.device
     seqs = _seqs(seqs)
     B, T = len(seqs), n_queued * q_len
-    _bf16_4d("q", q, view=True)
-    H = q.shape[1]
-    _check_like("q", q, (B, H, T, d.D), dev)
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new are given together or not at all")
-    if k_new is not None:
-        for n, t in (("k_new", k_new), ("v_new", v_new)):
-            _check_like(n, t, (B, d.H, T, d.D), dev)
+    H = q.shape[1] if len(q.shape) == 4 else 0
+    if not (_plain_views((q,) if out is None else (q, out), (B, H, T, d.D), cache.k_pages)
+            and (k_new is None or _plain_views((k_new, v_new), (B, d.H, T, d.D), cache.k_pages))):
+        for n, t, heads in (("q", q, H), ("out", out, H), ("k_new", k_new, d.H), ("v_new", v_new, d.H)):
+            if t is not None:
+                _check_like(n, t, (B, heads, T, d.D), dev)
     scale = 1.0 / math.sqrt(d.D) if scale is None else float(scale)
     o = torch.empty_like(q) if out is None else out
-    _check_like("out", o, (B, H, T, d.D), dev)
     if want_lse and lse is None:
         lse = torch.empty((B, H, T), dtype=torch.float32, device=dev)
     _check_lse(lse, (B, H, T), dev)

@@ -2,6 +2,7 @@
 // attn_rows.h.  Compiled once per head dimension (MW_ROWS_HEAD_DIM = 64, 72 or 128) and kind
 // (MW_ROWS_PAGED); the plan of a call lives in the D = 128 cross unit.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_rows.h"
 
@@ -50,12 +51,8 @@ hipError_t launch_pages(RowsParams p, const PageRanges& ranges, const RowsPlan& 
 
 template <bool PAGED>
 hipError_t launch_rows(const RowsParams& p, const RowsSeqs<PAGED>& seqs, const RowsPlan& plan, hipStream_t stream) {
-  if constexpr (!PAGED) {
-    if (plan.bm == 32) return launch_tile<PAGED, 4, 32, 4, 2>(p, seqs, plan, stream);
-  }
   if (plan.bm == 64) return launch_tile<PAGED, 4, 32, 2, 2>(p, seqs, plan, stream);
-  if (plan.bm == 128) return launch_tile<PAGED, 4, 64, 1, kD == 128 || (kD == 72 && PAGED) ? 2 : 3>(p, seqs, plan, stream);
-  return launch_tile<PAGED, 8, 64, 1, 1>(p, seqs, plan, stream);
+  return launch_tile<PAGED, 4, 64, 1, kD == 128 || (kD == 72 && PAGED) ? 2 : 3>(p, seqs, plan, stream);
 }
 
 }  // namespace
@@ -119,19 +116,49 @@ RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t
   return plan;
 }
 
-RowsPlan rows_plan(int D, int BHkv, int R, long long keys, size_t ws_bytes) {
-  RowsPlan plan{128, 1, 0};
-  auto fits = [&](long long ns) { return rows_part_bytes(D, BHkv, R, (int)ns) <= ws_bytes; };
-  if (R <= 32) {
-    plan.bm = 32;
-  } else if (R <= 64 || (long long)BHkv * ((R + 127) / 128) < 256) {
-    plan.bm = 64;
+// attn_rows_kernel's tile (64 rows in two key groups, or 128) and key ranges, by a price for each pair.  A workgroup's
+// steps take `lone` us each where it has a CU for itself and `shared` us of the CU where others keep it busy too (L on
+// the busiest CU, `occ` of them resident); a round of resident workgroups begins with `round` us; ranges cost the join
+// a launch, time for each range, and their fp32 partials a transfer.  The constants are a least-squares fit to
+// 3600 (bf16 keys) and 2480 (pages) shapes of 1 to 64 key heads, up to 60000 rows and 16000 keys, each timed with every
+// tile and 1 to 64 ranges: the plans taken are on average 1.8% (at the 90th percentile 6%) off the fastest ones.
+// (Tiles of 32 and 256 rows, timed as well, would have gained 0.1% on average.)
+struct TilePrice {
+  double start, round, lone, shared, join, per_mb, per_range;
+  int occ;
+};
+const TilePrice& tile_price(int D, bool paged, int bm) {
+  static const TilePrice bf16[3][2] = {
+      {{5.67, 1.16, 0.55, 0.38, 1.78, 0.39, 0.083, 4}, {6.46, 0.0, 0.81, 0.61, 2.07, 0.345, 0.076, 3}},   // D = 64
+      {{4.99, 2.36, 0.60, 0.44, 1.66, 0.342, 0.085, 3}, {7.06, 0.0, 0.47, 0.88, 1.98, 0.25, 0.068, 3}},   // 72
+      {{5.72, 2.27, 0.70, 0.73, 1.65, 0.296, 0.077, 2}, {6.52, 0.72, 1.17, 0.99, 1.78, 0.346, 0.075, 2}}};  // 128
+  static const TilePrice pages[3][2] = {
+      {{8.16, 0.0, 0.82, 0.47, 1.83, 0.447, 0.080, 4}, {8.25, 0.0, 1.06, 0.70, 2.57, 0.29, 0.081, 3}},
+      {{9.12, 0.0, 0.94, 0.63, 1.24, 0.592, 0.074, 3}, {9.02, 0.0, 1.30, 0.90, 2.09, 0.346, 0.082, 2}},
+      {{9.39, 0.0, 1.21, 0.82, 1.78, 0.428, 0.068, 2}, {8.67, 0.0, 1.70, 1.15, 3.31, 0.313, 0.068, 2}}};
+  return (paged ? pages : bf16)[D == 64 ? 0 : (D == 72 ? 1 : 2)][bm == 64 ? 0 : 1];
+}
+
+RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws_bytes) {
+  RowsPlan plan{64, 1, 0};
+  double best = 1e300;
+  const long long steps = std::max(1LL, (keys + 63) / 64);
+  for (const int bm : {64, 128}) {
+    const TilePrice& c = tile_price(D, paged, bm);
+    const long long tiles = (long long)BHkv * ((R + bm - 1) / bm);
+    for (long long ns = 1; ns <= std::min(64LL, steps); ++ns) {
+      const size_t part = rows_part_bytes(D, BHkv, R, (int)ns);
+      if (part > ws_bytes || (ns > 1 && tiles * ns > 8192)) break;
+      const double L = (double)((tiles * ns + 255) / 256), k = std::min(L, (double)c.occ);
+      const double t = c.start + std::ceil(L / k) * c.round + L / k * ((steps + ns - 1) / ns) * std::max(c.lone, k * c.shared) +
+                       (ns > 1 ? c.join + c.per_mb * part * 1e-6 + c.per_range * ns : 0.0);
+      if (t < best) {
+        best = t;
+        plan.bm = bm;
+        plan.n_splits = (int)ns;
+      }
+    }
   }
-  const long long wgs = (long long)BHkv * ((R + plan.bm - 1) / plan.bm);
-  const long long steps = (keys + 127) / 128;
-  long long ns = std::min({(512 + wgs - 1) / wgs, std::max(1LL, steps / 2), 64LL});
-  while (ns > 1 && !fits(ns)) --ns;
-  plan.n_splits = (int)std::max(1LL, ns);
   return plan;
 }
 #endif

@@ -32,7 +32,7 @@ extern "C" {
 size_t mw_cross_attn_workspace_size(int B, int H, int Hkv, int T, int M, int D) {
   if (check_cross("mw_cross_attn_workspace_size", B, H, Hkv, T, M, D)) return 0;
   const int R = T * (H / Hkv);
-  return rows_part_bytes(D, B * Hkv, R, rows_plan(D, B * Hkv, R, M, (size_t)-1).n_splits);
+  return rows_part_bytes(D, B * Hkv, R, rows_plan(D, false, B * Hkv, R, M, (size_t)-1).n_splits);
 }
 
 int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t* kv_len, void* o, float* lse,
@@ -76,7 +76,7 @@ int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t
   p.qlen = 1;
   p.scale_log2 = scale * kLog2e;
   p.part = static_cast<float*>(workspace);
-  const RowsPlan plan = rows_plan(D, B * Hkv, p.R, M, workspace != nullptr ? workspace_bytes : 0);
+  const RowsPlan plan = rows_plan(D, false, B * Hkv, p.R, M, workspace != nullptr ? workspace_bytes : 0);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   return hip_status(fn, D == 64   ? launch_cross_64(p, plan, hs)
                         : D == 72 ? launch_cross_72(p, plan, hs)

@@ -354,7 +354,7 @@ struct RowsPlan {
   int bm, n_splits, chunk;
 };
 // keys: the longest batch member's.
-RowsPlan rows_plan(int D, int BHkv, int R, long long keys, size_t ws_bytes);
+RowsPlan rows_plan(int D, bool paged, int BHkv, int R, long long keys, size_t ws_bytes);
 // Few rows over pages: `blocks` of 64 cached tokens of each sequence.
 constexpr int kPagesRows = 64;
 RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t ws_bytes);

@@ -414,7 +414,7 @@ static RowsPlan paged_plan(const mw_kvpages* c, const int32_t* seqs, int n_seqs,
     blocks[i] = (b.lens[seqs[i]] + MW_PAGE_BLOCK - 1) / MW_PAGE_BLOCK;
   }
   if (R <= kPagesRows) return pages_plan(c->D, R, blocks, n_seqs, c->H, ws_bytes);
-  return rows_plan(c->D, n_seqs * c->H, R, (long long)longest + tokens, ws_bytes);
+  return rows_plan(c->D, true, n_seqs * c->H, R, (long long)longest + tokens, ws_bytes);
 }
 
 size_t mw_chunk_attn_paged_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int n_queued,
