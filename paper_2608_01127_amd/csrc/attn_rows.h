@@ -109,20 +109,43 @@ struct RowBlock {
   template <bool MASKED, bool PRIO>
   __device__ __forceinline__ void step(const bf16_t* Kt, const bf16_t* Vt, const FragOffsets<D>& fo, const Tail72& ft,
                                        const bf16x8 (&qf)[KK], float c, int key0, int lo, int hi, int lane) {
+    // fragments read in groups ahead of their products: 1 to 2% faster, but at D = 64 over pages 3% slower
+    constexpr bool GROUPS = D != 64 || PRIO;
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) s[kb] = zero16();
+    // K fragments of two contraction steps at a time, read while the two before them multiply (as in add())
+    constexpr int STEP = GROUPS ? 2 : KK;
+    bf16x8 kf[2][STEP][KB];
+    auto read = [&](int g) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
+      for (int j = 0; j < STEP; ++j)
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) s[kb] = mfma32(fo.row8(Kt, kb * 32, kk), qf[kk], s[kb]);
+        for (int kb = 0; kb < KB; ++kb)
+          if (STEP * g + j < KK) kf[g & 1][j][kb] = fo.row8(Kt, kb * 32, STEP * g + j);
+    };
+    read(0);
+#pragma unroll
+    for (int g = 0; STEP * g < KK; ++g) {
+      if (STEP * (g + 1) < KK) read(g + 1);
+      if constexpr (GROUPS) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < STEP; ++j)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+          if (STEP * g + j < KK) s[kb] = mfma32(kf[g & 1][j][kb], qf[STEP * g + j], s[kb]);
+      if constexpr (GROUPS) __builtin_amdgcn_sched_barrier(0);
+    }
+    auto vf = [&](int kb, int t, int db) { return fo.tr8(Vt, kb * 32, t, db); };
+    bf16x8 ahead[DB];
+    ahead_of(ahead, 0, vf);
     if constexpr (MASKED) hide(s, key0, lo, hi, lane);
     // matrix phases go first: of two waves on a SIMD one is then in its softmax while the other multiplies (12 heads x
     // 19200 rows x 2048 keys, D = 128: 261 -> 246 us); with e4m3 tiles to convert it is 2% slower
     if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
     weigh(s, c, lane);
     if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
-    add(s, [&](int kb, int t, int db) { return fo.tr8(Vt, kb * 32, t, db); }, [&](int kb) { return ft.read(Vt, kb * 32); });
+    add<GROUPS>(s, ahead, vf, [&](int kb) { return ft.read(Vt, kb * 32); });
   }
 
   // Scores of keys that the row does not see: -inf.
@@ -173,19 +196,28 @@ struct RowBlock {
 
   // O^T += V^T P^T; the probabilities go to the matrix product in bf16 (their sum stays in 32 bits).  vf(kb, t, db):
   // V fragment of 16-key step t and column block db of key block kb; vt(kb): (TAIL) that of columns 64...
-  template <class VF, class VT>
-  __device__ __forceinline__ void add(const f32x16 (&s)[KB], VF vf, VT vt) {
+  // `ahead` holds the first step's fragments (ahead_of), read before the softmax.  With GROUPS each step's fragments
+  // are read while the one before it multiplies; left alone, the compiler reads a fragment right before its product.
+  template <class VF>
+  __device__ __forceinline__ static void ahead_of(bf16x8 (&v)[DB], int step, VF vf) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      bf16x8 p[2];
+    for (int db = 0; db < DB; ++db) v[db] = vf(step / 2, step % 2, db);
+  }
+  template <bool GROUPS, class VF, class VT>
+  __device__ __forceinline__ void add(const f32x16 (&s)[KB], bf16x8 (&ahead)[DB], VF vf, VT vt) {
+    bf16x8 v[2][DB], p[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        p[t] = pack8(s[kb], t);
+    for (int db = 0; db < DB; ++db) v[0][db] = ahead[db];
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] = mfma32(vf(kb, t, db), p[t], o[db]);
-      }
-      if constexpr (TAIL) {
-        const bf16x8 x = vt(kb);
+    for (int step = 0; step < 2 * KB; ++step) {
+      if (step + 1 < 2 * KB) ahead_of(v[(step + 1) & 1], step + 1, vf);
+      p[step & 1] = pack8(s[step / 2], step % 2);
+      if constexpr (GROUPS) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] = mfma32(v[step & 1][db], p[step & 1], o[db]);
+      if constexpr (GROUPS) __builtin_amdgcn_sched_barrier(0);
+      if (TAIL && step % 2) {
+        const bf16x8 x = vt(step / 2);
         tail_operands(p[0], p[1]);
 #pragma unroll
         for (int e = 0; e < 2; ++e) ot[e] = mfma16(x, p[e], ot[e]);
@@ -314,59 +346,62 @@ __device__ __forceinline__ bf16x8 decode(unsigned w0, unsigned w1, float scale) 
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A tile of 64 cached tokens of one head on its way into LDS: this thread's pieces of the K
-// and V codes in registers.  Pieces of 16 codes (8 at D = 72, whose 72-byte rows are only
-// 8-byte aligned), NT threads a round.
+// A tile of 64 cached tokens of one head on its way into LDS: this thread's pieces of 16 K and V codes in registers.
+// The tile's codes are contiguous in the page; NT threads a round.  D = 72: 288 pieces, the 32 that 256 threads leave
+// over of K and of V are the last wave's, K's by its first half; a piece may end in the next row, and so do its two
+// slots of the (dense) LDS tile.
 template <int D, int NT>
 struct CodeTile {
-  static constexpr int PC = D == 72 ? 8 : 16;  // codes per piece
-  static constexpr int PPR = D / PC;           // pieces per row
-  static constexpr int PIECES = 64 * PPR;
-  static constexpr int ROUNDS = (PIECES + NT - 1) / NT;
-  static constexpr bool WHOLE = PIECES % NT == 0;
-  unsigned k[ROUNDS][PC / 4], v[ROUNDS][PC / 4];
+  static constexpr bool ODD = D == 72;
+  static constexpr int PPR = D / 16;  // pieces per row (D = 64, 128)
+  static constexpr int ROUNDS = ODD ? 1 : 64 * PPR / NT;
+  static_assert(ODD ? NT == 256 : 64 * PPR % NT == 0, "whole rounds");
+  u32x4 k[ROUNDS], v[ROUNDS], rest;
   float ks, vs;
+  int last;
 
-  // Codes of the tile at `kp`, `vp` (row 0 of the tile in its page), of which rows 0..last
-  // hold tokens; `e`: index of the block's scales.
+  // The tile at `kp`, `vp` (row 0 of the tile in its page), of which rows 0..last hold tokens.  What is behind them
+  // is replaced: the last row again, or (D = 72) zeros.
   __device__ __forceinline__ void fetch(const uint8_t* kp, const uint8_t* vp, const float* k_scale,
-                                        const float* v_scale, int last, int tid, int vzero) {
-    ks = k_scale[vzero];
-    vs = v_scale[vzero];
+                                        const float* v_scale, int last_row, int tid) {
+    ks = *k_scale;
+    vs = *v_scale;
+    last = last_row;
+    if constexpr (ODD) {
+      k[0] = reinterpret_cast<const u32x4*>(kp)[tid];
+      v[0] = reinterpret_cast<const u32x4*>(vp)[tid];
+      if (tid >= 192) rest = reinterpret_cast<const u32x4*>((tid & 32) ? vp : kp)[256 + (tid & 31)];
+    } else {
 #pragma unroll
-    for (int it = 0; it < ROUNDS; ++it) {
-      const int p = it * NT + tid;
-      if (!WHOLE && p >= PIECES) break;
-      const int row = p / PPR, col = (p - row * PPR) * PC;
-      const int at = min(row, last) * D + col;
-      if constexpr (PC == 16) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(kp + at), b = *reinterpret_cast<const u32x4*>(vp + at);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          k[it][j] = a[j];
-          v[it][j] = b[j];
-        }
-      } else {
-        const u32x2 a = *reinterpret_cast<const u32x2*>(kp + at), b = *reinterpret_cast<const u32x2*>(vp + at);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          k[it][j] = a[j];
-          v[it][j] = b[j];
-        }
+      for (int it = 0; it < ROUNDS; ++it) {
+        const int p = it * NT + tid, row = p / PPR, at = min(row, last) * PPR + (p - row * PPR);
+        k[it] = reinterpret_cast<const u32x4*>(kp)[at];
+        v[it] = reinterpret_cast<const u32x4*>(vp)[at];
       }
+    }
+  }
+
+  // (D = 72) piece p of a tile into its two LDS slots
+  __device__ __forceinline__ void put(bf16_t* tile, int p, const u32x4& x, float scale) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const bool in = (2 * p + j) / 9 <= last;
+      *reinterpret_cast<bf16x8*>(tile + (2 * p + j) * 8) = decode(in ? x[2 * j] : 0u, in ? x[2 * j + 1] : 0u, scale);
     }
   }
 
   // The tile in bf16 into LDS rows row0.. of the K and V tiles.
   __device__ __forceinline__ void commit(bf16_t* Kt, bf16_t* Vt, int row0, int tid) const {
+    if constexpr (ODD) {
+      put(Kt + row0 * D, tid, k[0], ks);
+      put(Vt + row0 * D, tid, v[0], vs);
+      if (tid >= 192) put(((tid & 32) ? Vt : Kt) + row0 * D, 256 + (tid & 31), rest, (tid & 32) ? vs : ks);
+    } else {
 #pragma unroll
-    for (int it = 0; it < ROUNDS; ++it) {
-      const int p = it * NT + tid;
-      if (!WHOLE && p >= PIECES) break;
-      const int row = p / PPR, col = (p - row * PPR) * PC;
-      if constexpr (PC == 16) {
-        // a piece fills two neighbouring 16-byte slots: odd rows write the upper one first, so that two
-        // rows' writes together cover every bank
+      for (int it = 0; it < ROUNDS; ++it) {
+        const int p = it * NT + tid, row = p / PPR, col = (p - row * PPR) * 16;
+        // a piece fills two neighbouring 16-byte slots: odd rows write the upper one first, so that two rows'
+        // writes together cover every bank
         const bool up = row & 1;
         const unsigned k0 = k[it][0], k1 = k[it][1], k2 = k[it][2], k3 = k[it][3];
         const unsigned v0 = v[it][0], v1 = v[it][1], v2 = v[it][2], v3 = v[it][3];
@@ -375,10 +410,6 @@ struct CodeTile {
         *reinterpret_cast<bf16x8*>(Vt + first) = decode(up ? v2 : v0, up ? v3 : v1, vs);
         *reinterpret_cast<bf16x8*>(Kt + second) = decode(up ? k0 : k2, up ? k1 : k3, ks);
         *reinterpret_cast<bf16x8*>(Vt + second) = decode(up ? v0 : v2, up ? v1 : v3, vs);
-      } else {
-        const int at = Tile<D>::off(row0 + row, col);
-        *reinterpret_cast<bf16x8*>(Kt + at) = decode(k[it][0], k[it][1], ks);
-        *reinterpret_cast<bf16x8*>(Vt + at) = decode(v[it][0], v[it][1], vs);
       }
     }
   }
@@ -491,19 +522,16 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
     }
   };
   // Cached tokens of a step into registers (and from there into LDS).  Their pages are looked up one
-  // step before that.  The lookups and the scales go through vector loads: a scalar load in flight
-  // makes every wait for an LDS read a wait for it too.
+  // step before that.
   Codes codes[PAGED ? NB : 1];
-  int vzero;
-  asm volatile("v_mov_b32 %0, 0" : "=v"(vzero));
-  int page_v[PAGED ? NB : 1];
+  int page_of[PAGED ? NB : 1];
   auto block_at = [&](int x, int nb) { return min(x * NB + nb, (len - 1) >> 6); };  // one behind the last repeats it
   auto look = [&](int x) {
     if constexpr (PAGED) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const unsigned w = __umulhi((unsigned)block_at(x, nb), p.per_page_magic);
-        page_v[nb] = p.table[(long long)seq * p.W + (int)(p.per_page == 1 ? block_at(x, nb) : w) + vzero];
+        page_of[nb] = p.table[(long long)seq * p.W + (int)(p.per_page == 1 ? block_at(x, nb) : w)];
       }
     }
   };
@@ -513,9 +541,9 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
       for (int nb = 0; nb < NB; ++nb) {
         const int blk = block_at(x, nb);
         const int off = p.per_page == 1 ? 0 : blk - (int)__umulhi((unsigned)blk, p.per_page_magic) * p.per_page;
-        const long long head = (long long)__builtin_amdgcn_readfirstlane(page_v[nb]) * p.Hkv + hk;
+        const long long head = (long long)page_of[nb] * p.Hkv + hk;
         const long long e = head * p.per_page + off, at = e * (64 * D);
-        codes[nb].fetch(p.k_pages + at, p.v_pages + at, p.k_scales + e, p.v_scales + e, len - 1 - 64 * blk, tid, vzero);
+        codes[nb].fetch(p.k_pages + at, p.v_pages + at, p.k_scales + e, p.v_scales + e, len - 1 - 64 * blk, tid);
       }
     }
   };
@@ -860,7 +888,10 @@ __global__ __launch_bounds__(64 * NW, RB == 1 ? 2 : 1) void attn_pages_kernel(Ro
         const int hi = p.mode == ROWS_SEE_ALL ? p.M : min(p.M, (c0 + 1) * p.qlen), lo = p.mode == ROWS_SEE_OWN ? c0 * p.qlen : 0;
         Rows::hide(s[rb], k0, lo, hi, lane);
         rows[rb].weigh(s[rb], c, lane);
-        rows[rb].add(s[rb], [&](int, int t, int db) { return fo.tr8(Vt, 0, t, db); }, [&](int) { return ft.read(Vt, 0); });
+        auto vf = [&](int, int t, int db) { return fo.tr8(Vt, 0, t, db); };
+        bf16x8 ahead[DB];
+        Rows::ahead_of(ahead, 0, vf);
+        rows[rb].template add<false>(s[rb], ahead, vf, [&](int) { return ft.read(Vt, 0); });
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }

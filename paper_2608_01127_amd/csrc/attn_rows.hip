@@ -120,22 +120,22 @@ RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t
 // steps take `lone` us each where it has a CU for itself and `shared` us of the CU where others keep it busy too (L on
 // the busiest CU, `occ` of them resident); a round of resident workgroups begins with `round` us; ranges cost the join
 // a launch, time for each range, and their fp32 partials a transfer.  The constants are a least-squares fit to
-// 3600 (bf16 keys) and 2480 (pages) shapes of 1 to 64 key heads, up to 60000 rows and 16000 keys, each timed with every
-// tile and 1 to 64 ranges: the plans taken are on average 1.8% (at the 90th percentile 6%) off the fastest ones.
-// (Tiles of 32 and 256 rows, timed as well, would have gained 0.1% on average.)
+// 2600 (bf16 keys) and 2200 (pages) shapes of 1 to 64 key heads, up to 60000 rows and 16000 keys, each timed with both
+// tiles and 1 to 64 ranges: the plans taken are on average 1.4% and 2.0% (at the 90th percentile 6%) off the fastest.
+// (Tiles of 32 and 256 rows, timed in another such run, would have gained 0.1%.)
 struct TilePrice {
   double start, round, lone, shared, join, per_mb, per_range;
   int occ;
 };
 const TilePrice& tile_price(int D, bool paged, int bm) {
   static const TilePrice bf16[3][2] = {
-      {{5.67, 1.16, 0.55, 0.38, 1.78, 0.39, 0.083, 4}, {6.46, 0.0, 0.81, 0.61, 2.07, 0.345, 0.076, 3}},   // D = 64
-      {{4.99, 2.36, 0.60, 0.44, 1.66, 0.342, 0.085, 3}, {7.06, 0.0, 0.47, 0.88, 1.98, 0.25, 0.068, 3}},   // 72
-      {{5.72, 2.27, 0.70, 0.73, 1.65, 0.296, 0.077, 2}, {6.52, 0.72, 1.17, 0.99, 1.78, 0.346, 0.075, 2}}};  // 128
+      {{4.38, 2.45, 0.52, 0.365, 1.72, 0.363, 0.088, 4}, {6.04, 0.53, 0.76, 0.57, 1.92, 0.333, 0.081, 3}},   // D = 64
+      {{4.56, 2.77, 0.62, 0.413, 1.72, 0.308, 0.089, 3}, {7.32, 0.0, 0.48, 0.87, 2.05, 0.226, 0.073, 3}},    // 72
+      {{5.78, 2.36, 0.70, 0.721, 1.71, 0.281, 0.074, 2}, {6.46, 1.03, 1.14, 0.91, 1.85, 0.343, 0.071, 2}}};  // 128
   static const TilePrice pages[3][2] = {
-      {{8.16, 0.0, 0.82, 0.47, 1.83, 0.447, 0.080, 4}, {8.25, 0.0, 1.06, 0.70, 2.57, 0.29, 0.081, 3}},
-      {{9.12, 0.0, 0.94, 0.63, 1.24, 0.592, 0.074, 3}, {9.02, 0.0, 1.30, 0.90, 2.09, 0.346, 0.082, 2}},
-      {{9.39, 0.0, 1.21, 0.82, 1.78, 0.428, 0.068, 2}, {8.67, 0.0, 1.70, 1.15, 3.31, 0.313, 0.068, 2}}};
+      {{7.71, 0.0, 0.83, 0.47, 2.05, 0.447, 0.087, 4}, {7.65, 0.0, 1.05, 0.68, 2.85, 0.291, 0.090, 3}},
+      {{9.41, 0.0, 0.90, 0.54, 1.62, 0.444, 0.078, 3}, {9.25, 0.0, 1.17, 0.87, 2.16, 0.333, 0.077, 2}},
+      {{8.86, 0.0, 1.18, 0.83, 2.12, 0.401, 0.078, 2}, {8.77, 0.0, 1.50, 1.10, 3.53, 0.307, 0.071, 2}}};
   return (paged ? pages : bf16)[D == 64 ? 0 : (D == 72 ? 1 : 2)][bm == 64 ? 0 : 1];
 }
 
