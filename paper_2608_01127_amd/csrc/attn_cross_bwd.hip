@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
   if (k0 < n) {
     bf16x8 kf[KK], vf[KK];
     const bf16_t* vfrag = Vs + (kw * VL * 64 + lane) * 8;
-    {
+    auto load_keys = [&] {
       const long long kr = min(key, n - 1);
       const bf16_t* ka = p.k + b * p.sk.b + hk * p.sk.h + kr * p.sk.t + 8 * (lane >> 5);
       const bf16_t* va = p.v + b * p.sv.b + hk * p.sv.h + kr * p.sv.t + 8 * (lane >> 5);
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
         }
         if (kk < VL && qg == 0) *reinterpret_cast<bf16x8*>(Vs + ((kw * VL + kk) * 64 + lane) * 8) = vf[kk];
       }
-    }
+    };
     const FragOffsets<D> fo(lane, gq * D);
     const Tail72 ft(lane, gq * D);
     const RowOffsets<D, BS, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
@@ -147,11 +147,15 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
       }
     };
     const float c = p.scale_log2;
+    // Matrix phases go first where a step is matrix products only (24 heads on 8, 9600 rows x 2048 keys, D = 64: the whole
+    // backward 487 -> 468 us; D = 128, 12 heads: 429 -> 422 us); with the tail's lane exchanges, D = 72, it is 1% slower.
+    constexpr bool PRIO = !TAIL;
     auto step = [&](auto ragged, int r0, int buf) {
 #pragma unroll
       for (int qb = 0; qb < BM / 32; ++qb) {
         // the dP products start from -Delta of their rows
         f32x16 s = zero16(), dp;
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][gq + qb * 32 + 8 * g + 4 * (lane >> 5)]);
@@ -164,6 +168,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
           const bf16x8 vk = kk < VL ? *reinterpret_cast<const bf16x8*>(vfrag + kk * 512) : vf[kk];
           dp = mfma32(fo.row8(Os[buf], qb * 32, kk), vk, dp);
         }
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int rr = gq + qb * 32 + 8 * g + 4 * (lane >> 5);
@@ -179,6 +184,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
         }
         // P, then dS, to the matrix products in bf16
         bf16x8 h[2] = {pack8(s, 0), pack8(s, 1)};
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -204,7 +210,8 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
       }
     };
     if (beg < end) {
-      stage(beg, 0);
+      stage(beg, 0);  // ahead of the keys, whose V fragments are waited for on their way into LDS
+      load_keys();
       wait_vmem();
       __syncthreads();
       int buf = 0;
@@ -213,6 +220,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
         for (; r0 < stop; r0 += BS) {
           if (r0 + BS < end) stage(r0 + BS, buf ^ 1);
           if (k0 + kw * 32 < n) step(ragged, r0, buf);
+          if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
           wait_vmem();
           __syncthreads();
           buf ^= 1;
@@ -317,7 +325,29 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
   const int rt = x - split * n_rtiles;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv, G = p.G, R = p.R;
-  const int row = rt * BM + wave * 32 + (lane & 31), rc = min(row, R - 1), n = valid_keys(p, b);
+  const int row = rt * BM + wave * 32 + (lane & 31), rc = min(row, R - 1);
+  // This row's Q, dO and O, asked for before anything that waits (the number of keys, the first keys): their latencies
+  // then pass together.
+  bf16x8 qf[KK], of[KK], y[KK];
+  {
+    const bf16_t* qa = p.q + row_offset(p.sq, b, hk, G, rc) + 8 * (lane >> 5);
+    const bf16_t* da = p.d_o + row_offset(p.sdo, b, hk, G, rc) + 8 * (lane >> 5);
+    const bf16_t* oa = p.o + row_offset(p.so, b, hk, G, rc) + 8 * (lane >> 5);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
+        of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
+        y[kk] = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
+        qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = y[kk][j] = (__bf16)0.f;
+      }
+    }
+  }
+  const int row_t = rc / G;
+  const float lse = p.lse[((long long)b * p.Hkv * G + hk * G + (rc - row_t * G)) * p.T + row_t];
+  const int n = valid_keys(p, b);
   f32x16 dq[DB];
   f32x4 tail[2] = {zero4(), zero4()};
 #pragma unroll
@@ -327,34 +357,6 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
   const int beg = (int)((long long)steps * split / p.n_ranges) * BN;
   const int end = min(n, (int)((long long)steps * (split + 1) / p.n_ranges) * BN);
   if (n > 0) {
-    bf16x8 qf[KK], of[KK];
-    const bf16_t* qa = p.q + row_offset(p.sq, b, hk, G, rc) + 8 * (lane >> 5);
-    const bf16_t* da = p.d_o + row_offset(p.sdo, b, hk, G, rc) + 8 * (lane >> 5);
-    const bf16_t* oa = p.o + row_offset(p.so, b, hk, G, rc) + 8 * (lane >> 5);
-    float dot = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
-        qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
-        of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
-        const bf16x8 y = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[j], dot);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = (__bf16)0.f;
-      }
-    }
-    const float ndlt = -sum_halves(dot), c = p.scale_log2;
-    const int t = rc / G;
-    const float lse2 = p.lse[((long long)b * p.Hkv * G + hk * G + (rc - t * G)) * p.T + t] * 1.4426950408889634f;
-    if (split == 0 && lane < 32 && row < R) {
-      p.delta[(long long)bh * R + row] = ndlt;
-      p.lse2[(long long)bh * R + row] = lse2;
-    }
-    f32x16 nd;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) nd[i] = ndlt;
     const FragOffsets<D> fo(lane, 0);
     const Tail72 ft(lane, 0);
     const long long kb = b * p.sk.b + hk * p.sk.h, vb = b * p.sv.b + hk * p.sv.h;
@@ -370,6 +372,20 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
         }, tid);
       }
     };
+    if (beg < end) stage(beg, 0);
+    float dot = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[kk][j], dot);
+    const float ndlt = -sum_halves(dot), c = p.scale_log2, lse2 = lse * 1.4426950408889634f;
+    if (split == 0 && lane < 32 && row < R) {
+      p.delta[(long long)bh * R + row] = ndlt;
+      p.lse2[(long long)bh * R + row] = lse2;
+    }
+    f32x16 nd;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) nd[i] = ndlt;
     auto step = [&](auto ragged, int k0, int buf) {
 #pragma unroll
       for (int kq = 0; kq < BN / 32; ++kq) {
@@ -401,7 +417,6 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
         }
       }
     };
-    if (beg < end) stage(beg, 0);
     wait_vmem();
     __syncthreads();
     int buf = 0, k0 = beg;
@@ -513,7 +528,7 @@ hipError_t MW_CAT(launch_cross_bwd_, MW_CROSS_HEAD_DIM)(const CrossBwdParams& p,
                      n_rtiles);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  e = p.M <= 64 ? launch_dkdv<2, 4, 32, kD == 128 ? 7 : 0>(p, stream) : launch_dkdv<4, 2, 32, kD == 128 ? 6 : 0>(p, stream);
+  e = p.key_waves == 2 ? launch_dkdv<2, 4, 32, kD == 128 ? 7 : 0>(p, stream) : launch_dkdv<4, 2, 32, kD == 128 ? 6 : 0>(p, stream);
   if (e != hipSuccess || (p.n_slices == 1 && p.n_ranges == 1)) return e;
   const long long bhkv = (long long)p.B * p.Hkv;
   const long long n_kv = p.n_slices > 1 ? (bhkv * p.M * (kD / 4) + 255) / 256 : 0;
@@ -523,17 +538,65 @@ hipError_t MW_CAT(launch_cross_bwd_, MW_CROSS_HEAD_DIM)(const CrossBwdParams& p,
 }
 
 #if MW_CROSS_HEAD_DIM == 128
-// Slices of the rows: workgroups of eight waves for about one a CU, of at least two steps.
-int cross_bwd_slices(int D, int BHkv, int R, int M) {
-  (void)D;
-  const long long tiles = (long long)BHkv * (M <= 64 ? 1 : (M + 127) / 128);
-  return (int)std::max(1LL, std::min({256 / tiles, (long long)R / 128, 64LL}));
+// Key waves and row slices of the dK/dV kernel and key ranges of the dQ kernel, by a price for each choice.  A round of
+// the workgroups that are resident together begins with `begin` us; a step of 64 keys (or 32 * 8 / key waves rows) takes
+// `lone` us where a workgroup has its CU for itself and `shared` us of the CU for each where it has not.  The join costs a
+// launch, its partials' transfer and time for each slice and range.  The constants are a least-squares fit to 55160
+// timings of 5712 shapes (1 to 64 key heads, up to 60000 rows and 12000 keys): the plans taken are on average 0.6% (at
+// the 90th percentile 2.3%) off the fastest; one dK/dV workgroup and two dQ workgroups a CU as a rule were 5% (12%).
+struct BwdPrice {
+  int occ_q, occ_k;
+  double begin_q, lone_q, shared_q, begin_k, lone_k[2], shared_k[2];  // [0]: two key waves, [1]: four
+  double join, per_mb, per_part;
+};
+const BwdPrice& bwd_price(int D) {
+  static const BwdPrice d64 = {3, 2, 8.16, 1.11, 0.81, 4.92, {1.32, 0.97}, {1.32, 0.94}, 2.79, 0.379, 0.124};
+  static const BwdPrice d72 = {3, 1, 9.17, 1.33, 0.97, 4.14, {1.49, 1.15}, {1.49, 1.15}, 2.77, 0.268, 0.103};
+  static const BwdPrice d128 = {2, 1, 10.52, 1.76, 1.39, 5.42, {2.16, 1.61}, {2.16, 1.61}, 3.69, 0.321, 0.101};
+  return D == 64 ? d64 : (D == 72 ? d72 : d128);
 }
-// Key ranges of the dQ kernel: workgroups of four waves for about two a CU, of at least two steps.
-int cross_bwd_ranges(int D, int BHkv, int R, int M) {
-  (void)D;
-  const long long tiles = (long long)BHkv * ((R + 127) / 128);
-  return (int)std::max(1LL, std::min({512 / tiles, (long long)M / 128, 64LL}));
+
+// Time of `n` workgroups of `steps` steps each.
+double rounds_us(long long n, long long steps, int occ, double begin, double lone, double shared) {
+  const double busiest = (double)((n + 255) / 256), k = std::min(busiest, (double)occ);
+  return busiest / k * (begin + steps * std::max(lone, k * shared));
+}
+
+CrossBwdPlan cross_bwd_plan(int D, int BHkv, int R, int M) {
+  const BwdPrice& c = bwd_price(D);
+  // the best without and with parts, of either kernel
+  struct Best {
+    double us = 1e300;
+    int parts = 1, key_waves = 4;
+  } dq[2], dkv[2];
+  const auto offer = [](Best& x, double us, int parts, int key_waves) {
+    if (us < x.us) x = {us, parts, key_waves};
+  };
+  const long long q_steps = (M + 63) / 64, q_tiles = (long long)BHkv * ((R + 127) / 128);
+  const double q_mb = (double)BHkv * R * D * 4e-6, kv_mb = (double)BHkv * M * D * 8e-6;
+  for (int n = 1; n <= std::min(64LL, q_steps); ++n) {
+    const double t = rounds_us(q_tiles * n, (q_steps + n - 1) / n, c.occ_q, c.begin_q, c.lone_q, c.shared_q);
+    offer(dq[n > 1], n > 1 ? t + n * (c.per_mb * q_mb + c.per_part) : t, n, 0);
+  }
+  for (const int kw : {2, 4}) {
+    const int rows = 32 * (8 / kw), i = kw / 2 - 1;
+    const long long steps = (R + rows - 1) / rows, tiles = (long long)BHkv * ((M + 32 * kw - 1) / (32 * kw));
+    for (int n = 1; n <= std::min(64LL, steps); ++n) {
+      const double t = rounds_us(tiles * n, (steps + n - 1) / n, c.occ_k, c.begin_k, c.lone_k[i], c.shared_k[i]);
+      offer(dkv[n > 1], n > 1 ? t + n * (c.per_mb * kv_mb + c.per_part) : t, n, kw);
+    }
+  }
+  CrossBwdPlan plan{4, 1, 1};
+  double best = 1e300;
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j) {
+      const double t = dq[i].us + dkv[j].us + (i + j > 0 ? c.join : 0.0);
+      if (t < best) {
+        best = t;
+        plan = {dkv[j].key_waves, dkv[j].parts, dq[i].parts};
+      }
+    }
+  return plan;
 }
 #endif
 

@@ -86,15 +86,14 @@ int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t
 // Workspace of the backward: row terms (two fp32 a row), the fp32 dK and dV of the slices, the fp32 dQ of the
 // key ranges.
 struct CrossBwdLayout {
-  int n_slices, n_ranges;
+  CrossBwdPlan plan;
   size_t rows, part, part_q;  // bytes of one row term, of the slices and of the ranges
   CrossBwdLayout(int B, int H, int Hkv, int T, int M, int D) {
     const int R = T * (H / Hkv);
-    n_slices = cross_bwd_slices(D, B * Hkv, R, M);
-    n_ranges = cross_bwd_ranges(D, B * Hkv, R, M);
+    plan = cross_bwd_plan(D, B * Hkv, R, M);
     rows = round256((size_t)B * H * T * sizeof(float));
-    part = n_slices > 1 ? round256((size_t)n_slices * 2 * B * Hkv * M * D * sizeof(float)) : 0;
-    part_q = n_ranges > 1 ? round256((size_t)n_ranges * B * H * T * D * sizeof(float)) : 0;
+    part = plan.n_slices > 1 ? round256((size_t)plan.n_slices * 2 * B * Hkv * M * D * sizeof(float)) : 0;
+    part_q = plan.n_ranges > 1 ? round256((size_t)plan.n_ranges * B * H * T * D * sizeof(float)) : 0;
   }
   size_t bytes() const { return 2 * rows + part + part_q; }
 };
@@ -159,8 +158,9 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
   p.T = T;
   p.R = T * p.G;
   p.M = M;
-  p.n_slices = lay.n_slices;
-  p.n_ranges = lay.n_ranges;
+  p.key_waves = lay.plan.key_waves;
+  p.n_slices = lay.plan.n_slices;
+  p.n_ranges = lay.plan.n_ranges;
   p.scale = scale;
   p.scale_log2 = scale * kLog2e;
   hipStream_t hs = static_cast<hipStream_t>(stream);

@@ -387,11 +387,14 @@ struct CrossBwdParams {
   float* part_q;  // n_ranges > 1: [n_ranges][B Hkv][R][D] fp32 dQ of a range of the keys
   Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   int B, Hkv, G, T, R, M;
-  int n_slices, n_ranges;
+  int key_waves, n_slices, n_ranges;
   float scale, scale_log2;
 };
-int cross_bwd_slices(int D, int BHkv, int R, int M);
-int cross_bwd_ranges(int D, int BHkv, int R, int M);
+// Waves over the keys of a dK/dV workgroup, slices of the rows there, key ranges of the dQ kernel.
+struct CrossBwdPlan {
+  int key_waves, n_slices, n_ranges;
+};
+CrossBwdPlan cross_bwd_plan(int D, int BHkv, int R, int M);
 hipError_t launch_cross_bwd_64(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_72(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_128(const CrossBwdParams& p, hipStream_t stream);
