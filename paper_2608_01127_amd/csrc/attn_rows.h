@@ -105,12 +105,18 @@ struct RowBlock {
   }
 
   // One step of BN staged keys; `key0` + i is the place of key i, and (MASKED) a row sees
-  // places lo <= place < hi.
-  template <bool MASKED, bool PRIO>
-  __device__ __forceinline__ void step(const bf16_t* Kt, const bf16_t* Vt, const FragOffsets<D>& fo, const Tail72& ft,
+  // places lo <= place < hi.  `mid` is called between the scores and the softmax.
+  //
+  // Matrix phases go first: of two waves on a SIMD one is then in its softmax while the other multiplies (12 heads x
+  // 19200 rows x 2048 keys, D = 128: 261 -> 246 us).  Over pages (CODES) the conversion of the next tile, in `mid`, and
+  // what lies between two steps come last as well (12 heads x 2400 rows over 15000 cached tokens: D = 128 327 -> 300 us,
+  // D = 64 214 -> 177 us; with the conversion in front of the step 316 and 208); with bf16 keys, whose steps are staged
+  // by a few instructions, that is 5% slower.
+  template <bool MASKED, bool CODES, class Mid>
+  __device__ __forceinline__ void step(Mid mid, const bf16_t* Kt, const bf16_t* Vt, const FragOffsets<D>& fo, const Tail72& ft,
                                        const bf16x8 (&qf)[KK], float c, int key0, int lo, int hi, int lane) {
-    // fragments read in groups ahead of their products: 1 to 2% faster, but at D = 64 over pages 3% slower
-    constexpr bool GROUPS = D != 64 || PRIO;
+    // fragments read in groups ahead of their products: 1 to 2% faster, but at D = 64 over pages up to 7% slower
+    constexpr bool GROUPS = D != 64 || !CODES;
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) s[kb] = zero16();
@@ -124,6 +130,7 @@ struct RowBlock {
         for (int kb = 0; kb < KB; ++kb)
           if (STEP * g + j < KK) kf[g & 1][j][kb] = fo.row8(Kt, kb * 32, STEP * g + j);
     };
+    if constexpr (CODES) __builtin_amdgcn_s_setprio(1);
     read(0);
 #pragma unroll
     for (int g = 0; STEP * g < KK; ++g) {
@@ -140,12 +147,12 @@ struct RowBlock {
     bf16x8 ahead[DB];
     ahead_of(ahead, 0, vf);
     if constexpr (MASKED) hide(s, key0, lo, hi, lane);
-    // matrix phases go first: of two waves on a SIMD one is then in its softmax while the other multiplies (12 heads x
-    // 19200 rows x 2048 keys, D = 128: 261 -> 246 us); with e4m3 tiles to convert it is 2% slower
-    if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_s_setprio(0);
+    mid();
     weigh(s, c, lane);
-    if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_s_setprio(1);
     add<GROUPS>(s, ahead, vf, [&](int kb) { return ft.read(Vt, kb * 32); });
+    if constexpr (CODES) __builtin_amdgcn_s_setprio(0);
   }
 
   // Scores of keys that the row does not see: -inf.
@@ -586,16 +593,18 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
         const bool more = i + 1 < end;
         if (!PAGED && more) next = place(i + 1);
         const bool direct = more && (!PAGED || next < 0);
-        if (direct) {
-          stage_new(~next * BK, buf ^ 1);
-        } else if (more) {
-          commit(buf ^ 1);
-        }
-        if (PAGED && after >= 0) fetch(after);
-        if (PAGED && later >= 0) look(later);
+        if (direct) stage_new(~next * BK, buf ^ 1);
+        auto mid = [&] {
+          if constexpr (PAGED) {
+            if (more && !direct) commit(buf ^ 1);
+            if (after >= 0) fetch(after);
+            if (later >= 0) look(later);
+          }
+        };
         const bool old = PAGED && x >= 0;
         const int k0 = (old ? x : ~x) * BK + kg * BN;
-        rb.template step<decltype(masked)::value, !PAGED>(Ks[buf], Vs[buf], fo, ft, qf, c, k0, old ? 0 : lo, old ? len : hi, lane);
+        rb.template step<decltype(masked)::value, PAGED>(mid, Ks[buf], Vs[buf], fo, ft, qf, c, k0, old ? 0 : lo,
+                                                         old ? len : hi, lane);
         if (direct) wait_vmem();
         lds_barrier();
         buf ^= 1;

@@ -120,8 +120,8 @@ RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t
 // steps take `lone` us each where it has a CU for itself and `shared` us of the CU where others keep it busy too (L on
 // the busiest CU, `occ` of them resident); a round of resident workgroups begins with `round` us; ranges cost the join
 // a launch, time for each range, and their fp32 partials a transfer.  The constants are a least-squares fit to
-// 2600 (bf16 keys) and 2200 (pages) shapes of 1 to 64 key heads, up to 60000 rows and 16000 keys, each timed with both
-// tiles and 1 to 64 ranges: the plans taken are on average 1.4% and 2.0% (at the 90th percentile 6%) off the fastest.
+// 2600 (bf16 keys) and 3100 (pages) shapes of 1 to 64 key heads, up to 60000 rows and 16000 keys, each timed with both
+// tiles and 1 to 64 ranges: the plans taken are on average 1.4% and 1.3% (at the 90th percentile 6% and 5%) off the fastest.
 // (Tiles of 32 and 256 rows, timed in another such run, would have gained 0.1%.)
 struct TilePrice {
   double start, round, lone, shared, join, per_mb, per_range;
@@ -133,9 +133,9 @@ const TilePrice& tile_price(int D, bool paged, int bm) {
       {{4.56, 2.77, 0.62, 0.413, 1.72, 0.308, 0.089, 3}, {7.32, 0.0, 0.48, 0.87, 2.05, 0.226, 0.073, 3}},    // 72
       {{5.78, 2.36, 0.70, 0.721, 1.71, 0.281, 0.074, 2}, {6.46, 1.03, 1.14, 0.91, 1.85, 0.343, 0.071, 2}}};  // 128
   static const TilePrice pages[3][2] = {
-      {{7.71, 0.0, 0.83, 0.47, 2.05, 0.447, 0.087, 4}, {7.65, 0.0, 1.05, 0.68, 2.85, 0.291, 0.090, 3}},
-      {{9.41, 0.0, 0.90, 0.54, 1.62, 0.444, 0.078, 3}, {9.25, 0.0, 1.17, 0.87, 2.16, 0.333, 0.077, 2}},
-      {{8.86, 0.0, 1.18, 0.83, 2.12, 0.401, 0.078, 2}, {8.77, 0.0, 1.50, 1.10, 3.53, 0.307, 0.071, 2}}};
+      {{8.71, 0.0, 0.73, 0.436, 1.67, 0.456, 0.070, 4}, {8.88, 0.0, 0.98, 0.636, 2.40, 0.307, 0.070, 3}},
+      {{9.63, 0.0, 0.91, 0.583, 1.01, 0.602, 0.065, 3}, {9.44, 0.0, 1.16, 0.81, 2.02, 0.357, 0.069, 2}},
+      {{10.05, 0.0, 1.04, 0.729, 1.42, 0.435, 0.062, 2}, {9.77, 0.0, 1.39, 1.01, 2.88, 0.319, 0.055, 2}}};
   return (paged ? pages : bf16)[D == 64 ? 0 : (D == 72 ? 1 : 2)][bm == 64 ? 0 : 1];
 }
 
