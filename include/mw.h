@@ -454,8 +454,9 @@ int mw_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t
                       const mw_strides* strides, int B, int H, int Hkv, int T, int M, int D, float scale,
                       void* workspace, size_t workspace_bytes, mw_stream_t stream);
 
-/* Bytes of device workspace mw_cross_attn_bwd needs: two fp32 for each row, and the
- * fp32 dK and dV of the slices the rows are cut into. */
+/* Bytes of device workspace mw_cross_attn_bwd needs: two fp32 for each row, the fp32
+ * dK and dV of the slices the rows are cut into, and the fp32 dQ of the ranges the
+ * keys are cut into. */
 size_t mw_cross_attn_bwd_workspace_size(int B, int H, int Hkv, int T, int M, int D);
 
 /* Backward of mw_cross_attn_fwd for the loss sum(dO * O): dQ, and dK and dV summed
@@ -496,8 +497,10 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
  * table and lengths is written by the calls' kernels in stream order, so the calls on
  * one cache go to one stream (or streams that wait for each other), from one thread
  * at a time, and with the stream's device current.  Pages are taken lowest index first.
- * Operations that change a cache must run outside HIP graph capture; a captured
- * mw_chunk_attn_paged reads the table and lengths as they are when it is replayed.
+ * Operations that change a cache refuse a stream under HIP graph capture (MW_EINVAL); a
+ * captured mw_chunk_attn_paged reads the table and lengths as they are when it is
+ * replayed.  After MW_EHIP from an operation the device's copy of the lists it names
+ * is undefined.
  * ---------------------------------------------------------------------- */
 typedef struct {
   void* k_pages;   /* e4m3 [P, H, L, D] */
@@ -572,6 +575,7 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
  *                by H / cache->H query heads each
  * k_new, v_new : bf16 [n_seqs, cache->H, n_queued * q_len, D], or both NULL: the
  *                cached tokens alone (O = 0, LSE = -inf where there are none)
+ *                (a value that a row does not see weighs 0 there: it has to be finite)
  * lse          : fp32 [n_seqs, H, n_queued * q_len], or NULL
  * workspace    : optional, as in mw_chunk_attn_cached; sized for the sequences'
  *                present lengths by mw_chunk_attn_paged_workspace_size

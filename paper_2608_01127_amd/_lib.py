@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import functools
 import math
+import operator
 import os
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -708,10 +709,18 @@ class KVPages:
         return _check(load().mw_kvpages_n_free(ctypes.byref(self.desc)))
 
     def len(self, seq: int) -> int:
-        return _check(load().mw_kvpages_len(ctypes.byref(self.desc), int(seq)))
+        return _check(load().mw_kvpages_len(ctypes.byref(self.desc), _int32(seq)))
 
     def page_of(self, seq: int, index: int) -> int:
-        return _check(load().mw_kvpages_page_of(ctypes.byref(self.desc), int(seq), int(index)))
+        return _check(load().mw_kvpages_page_of(ctypes.byref(self.desc), _int32(seq), _int32(index)))
+
+
+def _int32(x) -> int:
+    """An integer that a C int holds (ctypes takes any and keeps its low bits)."""
+    x = operator.index(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{x} is out of range")
+    return x
 
 
 @functools.lru_cache(maxsize=512)
@@ -723,7 +732,7 @@ def _seqs(seqs):
     """Host array of sequence numbers (the library only reads it)."""
     if isinstance(seqs, ctypes.Array):
         return seqs
-    return _seq_array(tuple(map(int, seqs)))
+    return _seq_array(tuple(map(_int32, seqs)))
 
 
 def mw_kvpages_append(cache: KVPages, seqs, k, v) -> None:
@@ -742,13 +751,13 @@ def mw_kvpages_append(cache: KVPages, seqs, k, v) -> None:
 def mw_kvpages_fork(cache: KVPages, src: int, dst: int) -> None:
     """Make the empty sequence dst a branch of src that shares its pages."""
     with _on_device(cache.device):
-        _check(load().mw_kvpages_fork(ctypes.byref(cache.desc), int(src), int(dst), _stream_handle(cache.device)))
+        _check(load().mw_kvpages_fork(ctypes.byref(cache.desc), _int32(src), _int32(dst), _stream_handle(cache.device)))
 
 
 def mw_kvpages_copy(cache: KVPages, src: int, dst: int) -> None:
     """Make the empty sequence dst a copy of src in pages of its own."""
     with _on_device(cache.device):
-        _check(load().mw_kvpages_copy(ctypes.byref(cache.desc), int(src), int(dst), _stream_handle(cache.device)))
+        _check(load().mw_kvpages_copy(ctypes.byref(cache.desc), _int32(src), _int32(dst), _stream_handle(cache.device)))
 
 
 def mw_kvpages_free(cache: KVPages, seqs) -> None:
@@ -761,7 +770,7 @@ def mw_kvpages_free(cache: KVPages, seqs) -> None:
 def mw_kvpages_evict(cache: KVPages, seq: int, first_page: int, n_pages: int) -> None:
     """Drop the full pages [first_page, first_page + n_pages) of a sequence."""
     with _on_device(cache.device):
-        _check(load().mw_kvpages_evict(ctypes.byref(cache.desc), int(seq), int(first_page), int(n_pages),
+        _check(load().mw_kvpages_evict(ctypes.byref(cache.desc), _int32(seq), _int32(first_page), _int32(n_pages),
                                        _stream_handle(cache.device)))
 
 

@@ -18,6 +18,8 @@
 
 using namespace mw;
 
+static_assert(kMaxSeqs == MW_MAX_SEQS, "the kernels' arguments hold the sequences of a call");
+
 namespace {
 
 struct Book {
@@ -82,6 +84,18 @@ int check_seqs(const char* fn, const mw_kvpages* c, const int32_t* seqs, int n, 
     for (int j = 0; distinct && j < i; ++j)
       if (seqs[j] == seqs[i]) return fail(MW_EINVAL, "%s: sequence %d is listed twice", fn, seqs[i]);
   }
+  return MW_OK;
+}
+
+// A recorded operation would run again with the pages and places of its first time, which the books no longer match.
+int check_not_captured(const char* fn, mw_stream_t stream) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &status) != hipSuccess) {
+    (void)hipGetLastError();  // (the launch reports it)
+    return MW_OK;
+  }
+  if (status != hipStreamCaptureStatusNone)
+    return fail(MW_EINVAL, "%s: the stream is being captured into a graph; the call changes host state", fn);
   return MW_OK;
 }
 
@@ -165,6 +179,7 @@ int mw_kvpages_append(mw_kvpages* c, const int32_t* seqs, int n_seqs, const void
   int st = check_pages(fn, c);
   if (!st) st = check_seqs(fn, c, seqs, n_seqs, true);
   if (!st) st = check_ptrs(fn, {{"k", k}, {"v", v}});
+  if (!st) st = check_not_captured(fn, stream);
   if (st) return st;
   if (n_tokens < 1) return fail(MW_EINVAL, "%s: n_tokens must be >= 1", fn);
   if (n_tokens > kMaxT) return fail(MW_EUNSUPPORTED, "%s: too many tokens", fn);
@@ -245,10 +260,11 @@ int mw_kvpages_append(mw_kvpages* c, const int32_t* seqs, int n_seqs, const void
   return hip_status(fn, e);
 }
 
-static int check_empty_pair(const char* fn, const mw_kvpages* c, int src, int dst) {
+static int check_empty_pair(const char* fn, const mw_kvpages* c, int src, int dst, mw_stream_t stream) {
   int st = check_pages(fn, c);
   if (!st) st = check_seq(fn, c, src);
   if (!st) st = check_seq(fn, c, dst);
+  if (!st) st = check_not_captured(fn, stream);
   if (st) return st;
   if (src == dst) return fail(MW_EINVAL, "%s: source and destination are both sequence %d", fn, src);
   if (book(c).lens[dst] != 0)
@@ -258,7 +274,7 @@ static int check_empty_pair(const char* fn, const mw_kvpages* c, int src, int ds
 
 int mw_kvpages_fork(mw_kvpages* c, int src, int dst, mw_stream_t stream) {
   const char* fn = "mw_kvpages_fork";
-  const int st = check_empty_pair(fn, c, src, dst);
+  const int st = check_empty_pair(fn, c, src, dst, stream);
   if (st) return st;
   const Book b = book(c);
   const int len = b.lens[src], n = pages_of(c, len);
@@ -276,7 +292,7 @@ int mw_kvpages_fork(mw_kvpages* c, int src, int dst, mw_stream_t stream) {
 
 int mw_kvpages_copy(mw_kvpages* c, int src, int dst, mw_stream_t stream) {
   const char* fn = "mw_kvpages_copy";
-  const int st = check_empty_pair(fn, c, src, dst);
+  const int st = check_empty_pair(fn, c, src, dst, stream);
   if (st) return st;
   const Book b = book(c);
   const int len = b.lens[src], n = pages_of(c, len);
@@ -306,6 +322,7 @@ int mw_kvpages_free(mw_kvpages* c, const int32_t* seqs, int n_seqs, mw_stream_t 
   const char* fn = "mw_kvpages_free";
   int st = check_pages(fn, c);
   if (!st) st = check_seqs(fn, c, seqs, n_seqs, true);
+  if (!st) st = check_not_captured(fn, stream);
   if (st) return st;
   const Book b = book(c);
   SeqArgs a;
@@ -325,6 +342,7 @@ int mw_kvpages_evict(mw_kvpages* c, int seq, int first_page, int n_pages, mw_str
   const char* fn = "mw_kvpages_evict";
   int st = check_pages(fn, c);
   if (!st) st = check_seq(fn, c, seq);
+  if (!st) st = check_not_captured(fn, stream);
   if (st) return st;
   const Book b = book(c);
   const int len = b.lens[seq], used = pages_of(c, len);
@@ -346,7 +364,8 @@ int mw_kvpages_evict(mw_kvpages* c, int seq, int first_page, int n_pages, mw_str
 
 int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream) {
   const char* fn = "mw_kvpages_compact";
-  const int st = check_pages(fn, c);
+  int st = check_pages(fn, c);
+  if (!st) st = check_not_captured(fn, stream);
   if (st) return st;
   const Book b = book(c);
   const int live = c->P - b.head[2];

@@ -488,6 +488,33 @@ def test_captured_calls_follow_the_cache(mw):
         assert torch.allclose(again.float(), o.float(), atol=2.0 ** -7 * 4)
 
 
+def test_operations_refuse_a_stream_under_capture(mw):
+    """They change the books on the host, which a replay does not; a refusal leaves the cache and the capture alone."""
+    import torch
+    H, L, D = 2, 64, 64
+    cache, model = filled(mw, H, L, D, [200, 0, 0], seed=4)
+    k, v = randn((1, H, 5, D), 1), randn((1, H, 5, D), 2)
+    x = torch.zeros(64, device="cuda")
+    free = cache.n_free
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for op in (lambda: mw.mw_kvpages_append(cache, [0], k, v), lambda: mw.mw_kvpages_fork(cache, 0, 1),
+                   lambda: mw.mw_kvpages_copy(cache, 0, 1), lambda: mw.mw_kvpages_free(cache, [0]),
+                   lambda: mw.mw_kvpages_evict(cache, 0, 0, 1), lambda: mw.mw_kvpages_compact(cache)):
+            with pytest.raises(mw.MWError, match="captured"):
+                op()
+        x += 1
+    for n in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x, torch.full_like(x, n + 1.0))
+    assert cache.n_free == free and cache.len(0) == 200 and cache.len(1) == 0
+    model.verify()
+    mw.mw_kvpages_append(cache, [0], k, v)  # and outside a capture they run as before
+    assert cache.len(0) == 205
+
+
 # ------------------------------------------------------------------------------- together
 
 @pytest.mark.parametrize("D", [64, 128])

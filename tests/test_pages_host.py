@@ -132,3 +132,12 @@ def test_python_class_refuses_sizes_before_it_allocates(bad):
     if not torch.cuda.is_available():
         with pytest.raises(mw.MWError):
             mw.KVPages(*bad, device="cpu")
+
+
+def test_sequence_numbers_that_a_c_int_does_not_hold_are_refused():
+    """ctypes would keep the low 32 bits: 2^32 would name sequence 0."""
+    for f in (lambda s: _lib._seqs([s]), _lib._int32):
+        for bad, kind in ((1 << 32, ValueError), (-(1 << 31) - 1, ValueError), (1.5, TypeError)):
+            with pytest.raises(kind):
+                f(bad)
+    assert list(_lib._seqs([0, 255])) == [0, 255] and _lib._int32(-1) == -1
