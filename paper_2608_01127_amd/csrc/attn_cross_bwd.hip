@@ -5,7 +5,7 @@
 // shared heads are sums over more rows and need nothing else.
 //
 //   dQ kernel    : a wave owns 32 rows and walks the keys; it has the rows' dO in registers, so it also
-//                  forms Delta (and LSE log2 e) for the other kernel.  Few rows over many keys: the keys are cut
+//                  forms Delta (and LSE log2 e) for the other kernel; where one step holds all keys, as sum_j P_j dP_j.  Few rows over many keys: the keys are cut
 //                  into ranges that leave fp32 dQ.
 //   dK/dV kernel : a wave owns 32 keys and walks rows staged in LDS.  The rows are many and the keys few, so the
 //                  rows of a key tile are cut into slices that fill the card and leave fp32 dK, dV.
@@ -378,8 +378,33 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
       for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[kk][j], dot);
-    const float ndlt = -sum_halves(dot), c = p.scale_log2, lse2 = lse * 1.4426950408889634f;
-    if (split == 0 && lane < 32 && row < R) {
+    float ndlt = -sum_halves(dot);
+    const float c = p.scale_log2, lse2 = lse * 1.4426950408889634f;
+    wait_vmem();
+    __syncthreads();
+    // Keys of a single step: Delta = sum_j P_j dP_j of the probabilities at hand.  rowsum(dO O) has O's rounding to bf16,
+    // which next to few keys' dP - Delta is no longer small (2 keys: dK 0.0043 off, relative to its norm; so 0.0023,
+    // which is the rounding of dS and of dK itself; from 64 keys on it is below a tenth of those).
+    const bool few = n <= BN;
+    if (few && beg < end) {
+      float sum = 0.f;
+#pragma unroll 1
+      for (int kq = 0; kq < BN / 32; ++kq) {
+        f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = mfma32(fo.row8(Ks[0], kq * 32, kk), qf[kk], s);
+          dp = mfma32(fo.row8(Vs[0], kq * 32, kk), of[kk], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool in = kq * 32 + acc_row(i, lane) < n;
+          sum = fmaf(in ? fast_exp2(fmaf(s[i], c, -lse2)) : 0.f, in ? dp[i] : 0.f, sum);
+        }
+      }
+      ndlt = -sum_halves(sum);
+    }
+    if ((few ? beg < end : split == 0) && lane < 32 && row < R) {
       p.delta[(long long)bh * R + row] = ndlt;
       p.lse2[(long long)bh * R + row] = lse2;
     }
@@ -417,8 +442,6 @@ __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p
         }
       }
     };
-    wait_vmem();
-    __syncthreads();
     int buf = 0, k0 = beg;
     auto run = [&](auto ragged, int stop) {
       for (; k0 < stop; k0 += BN) {

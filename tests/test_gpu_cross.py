@@ -235,3 +235,31 @@ def test_side_stream_and_graph_replays(mw):
         for x in outs:
             for a, b in zip(x, eager):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("M,lens", [(2, None), (5, None), (40, None), (64, None), (1000, [2, 900]), (1000, [64, 7])])
+def test_gradients_of_few_states_keep_their_precision(mw, D, M, lens):
+    """Next to a few states' dP - Delta the rounding of O to bf16 would not be small, so Delta must not come from it.
+    What is left is the rounding of dS and that of the gradient itself: relative errors of at most 2^-8 each, spread
+    over their interval, so 2^-8 / sqrt(3) in the mean square at most and sqrt(2) of that together, for sums of
+    independent terms (random inputs) too."""
+    import torch
+    B, H, T = 2, 3, 700
+    n = lens or [M, M]
+    q, do = randn((B, H, T, D), 1), randn((B, H, T, D), 2)
+    k, v = randn((B, H, M, D), 3), randn((B, H, M, D), 4)
+    kv_len = torch.tensor(n, dtype=torch.int32, device="cuda")
+    o, lse = mw.mw_cross_attn_fwd(q, k, v, kv_len=kv_len)
+    got = dict(zip(("dq", "dk", "dv"), mw.mw_cross_attn_bwd(q, k, v, o, do, lse, kv_len=kv_len)))
+    for b in range(B):
+        q64, k64, v64, d64 = (x[b].double().cpu() for x in (q, k[:, :, :n[b]], v[:, :, :n[b]], do))
+        kt, vt = k64.transpose(1, 2).contiguous(), v64.transpose(1, 2).contiguous()
+        P = torch.softmax(q64 @ kt / math.sqrt(D), -1)
+        dP = d64 @ vt
+        dS = P * (dP - (P * dP).sum(-1, keepdim=True)) / math.sqrt(D)
+        want = dict(dq=dS @ k64, dk=dS.transpose(1, 2).contiguous() @ q64, dv=P.transpose(1, 2).contiguous() @ d64)
+        for name, w in want.items():
+            g = got[name][b].double().cpu()
+            g = g if name == "dq" else g[:, :n[b]]
+            assert (g - w).norm() <= 2.0 ** -8 * math.sqrt(2 / 3) * w.norm(), (name, b, ((g - w).norm() / w.norm()).item())
