@@ -38,7 +38,7 @@ hipError_t launch_tile(RowsParams p, const RowsSeqs<PAGED>& seqs, const RowsPlan
 
 #ifdef MW_ROWS_PAGED
 // Four waves; two stages a wave leave room for two workgroups a CU, whose prologues and ends overlap (with four stages
-// and one workgroup: one token of 8 sequences over up to 15840 tokens 28.2 us for 26.2, in two rounds 39 for 31).
+// and one workgroup: one token of 8 sequences over up to 15840 tokens 27.3 us for 25.2, in two rounds 34.8 for 27.5).
 template <int RB>
 hipError_t launch_pages(RowsParams p, const PageRanges& ranges, const RowsPlan& plan, hipStream_t stream) {
   p.n_splits = plan.n_splits;
@@ -83,7 +83,7 @@ size_t rows_part_bytes(int D, int BHkv, int R, int n_splits) {
 // attn_pages_kernel's ranges, of `chunk` blocks.  A call takes about as long as the workgroups of the busiest CU (L of
 // them) take to stream their ranges, one after another or side by side, each beside its range as long as nine blocks:
 // one token of 8 sequences of up to 248 blocks (4 key heads), us for chunks of 8 | 16 | 24 | 32 blocks (L = 3, 2, 2, 1)
-// 31.0 | 27.1 | 31.1 | 26.2; 64 rows of 16 heads over 248 (L = 2, 1, 1, 1) 37.7 | 28.5 | 33.3 | 38.1.
+// 31.3 | 27.5 | 30.9 | 25.3; 64 rows of 16 heads over 248 (L = 2, 1, 1, 1) 38.7 | 29.2 | 34.0 | 38.7.
 RowsPlan pages_plan(int D, int R, const int* blocks, int n_seqs, int Hkv, size_t ws_bytes) {
   RowsPlan plan{0, 1, 1};
   long long longest = 1;
