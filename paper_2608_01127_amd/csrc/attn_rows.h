@@ -444,18 +444,18 @@ __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, R
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % NWR, kg = wave / NWR;
-  // Consecutive workgroups are dealt to the 8 XCDs in turn: each gets one contiguous range of
-  // (head, key range, row tile), so that a head's keys stay in one L2.
+  // Consecutive workgroups are dealt to the 8 XCDs in turn: each gets one contiguous range of (key head, key range,
+  // batch member, row tile).  The row tiles of a range share one L2; members, whose lengths differ, take turns, or the
+  // XCDs with the long ones would finish last (members one after another: 8 chunks of 600 rows, 2 x 12 heads over 14700
+  // and 11025 cached tokens 1120 us, so 1037; 3 x 16 heads x 999 rows over 3601, 3001 and 2401, D = 72, 125 and 111).
   int item;
   {
     const int n = gridDim.x, x = blockIdx.x % 8, q = n / 8, rem = n % 8;
     item = x * q + min(x, rem) + blockIdx.x / 8;
   }
-  const int per_head = p.n_rtiles * p.n_splits;
-  const int bh = item / per_head;
-  const int in_head = item - bh * per_head;
-  const int split = in_head / p.n_rtiles, rt = p.n_rtiles - 1 - (in_head - split * p.n_rtiles);  // late rows see more
-  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const int group = item / p.n_rtiles, rt = p.n_rtiles - 1 - (item - group * p.n_rtiles);  // late rows see more
+  const int range = group / p.B, b = group - range * p.B;
+  const int hk = range / p.n_splits, split = range - hk * p.n_splits, bh = b * p.Hkv + hk;
   const int G = p.G;
   const int r0 = rt * BM;
 
