@@ -595,28 +595,29 @@ def _check_workspace(workspace, dev):
     return workspace.nbytes
 
 
-def _cross_args(q, k, v, kv_len, rows, keys):
-    """Sizes of a cross attention call.  q and the tensors `rows` (name -> tensor or None) are [B,H,T,D], k, v and
-    `keys` [B,Hkv,M,D]."""
+def _cross_args(q, k, v, kv_len, rows, keys, named):
+    """Sizes of a cross attention call.  `rows` are its [B,H,T,D] tensors, `keys` its [B,Hkv,M,D] ones; named() gives
+    what of them is neither q, k nor v by name (or None), for the errors."""
     torch = _torch()
-    if not (_plain_views([q, *(t for t in rows.values() if t is not None)], q.shape, q)
-            and _plain_views([k, v, *(t for t in keys.values() if t is not None)], k.shape, q)):
+    if not (_plain_views(rows, q.shape, q) and _plain_views(keys, k.shape, q)):
         for n, t in (("q", q), ("k", k), ("v", v)):
             _bf16_4d(n, t, view=True)
-        for n, t in rows.items():
+        like_q, like_k = named()
+        for n, t in like_q.items():
             if t is not None:
                 _check_like(n, t, q.shape, q.device)
-        for n, t in (("k", k), ("v", v), *keys.items()):
+        for n, t in (("k", k), ("v", v), *like_k.items()):
             if t is not None:
                 _check_like(n, t, k.shape, q.device)
     B, H, T, D = q.shape
-    if k.shape[0] != B or k.shape[3] != D:
+    Bk, Hkv, M, Dk = k.shape
+    if Bk != B or Dk != D:
         raise ValueError(f"k and v must be [B,Hkv,M,D] with B, D = {B}, {D}, got {tuple(k.shape)}")
     dev = q.device
-    if kv_len is not None and (kv_len.dtype != torch.int32 or kv_len.shape != (B,) or kv_len.device != dev
+    if kv_len is not None and (kv_len.dtype is not torch.int32 or kv_len.shape != (B,) or kv_len.device != dev
                                or not kv_len.is_contiguous()):
         raise ValueError(f"kv_len must be a contiguous int32 tensor of shape {(B,)} on the device of the inputs")
-    return B, H, k.shape[1], T, k.shape[2], D, dev
+    return B, H, Hkv, T, M, D, dev
 
 
 def mw_cross_attn_workspace_size(B: int, H: int, Hkv: int, T: int, M: int, D: int) -> int:
@@ -630,7 +631,8 @@ def mw_cross_attn_fwd(q, k, v, kv_len=None, scale=None, out=None, lse=None, work
 
     With no workspace given, one of the size the library asks for is allocated here (torch)."""
     torch = _torch()
-    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, {"out": out}, {})
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, (q,) if out is None else (q, out), (k, v),
+                                             lambda: ({"out": out}, {}))
     scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
     o = torch.empty_like(q) if out is None else out
     lse = torch.empty((B, H, T), dtype=torch.float32, device=dev) if lse is None else lse
@@ -654,7 +656,9 @@ def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=N
     """Backward of mw_cross_attn_fwd.  Returns (dq, dk, dv): bf16 [B,H,T,D] and twice [B,Hkv,M,D], the latter
     summed over the query heads that share a key head and 0 behind kv_len."""
     torch = _torch()
-    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, {"o": o, "d_o": d_o, "dq": dq}, {"dk": dk, "dv": dv})
+    B, H, Hkv, T, M, D, dev = _cross_args(q, k, v, kv_len, (q, o, d_o) if dq is None else (q, o, d_o, dq),
+                                          (k, v, *(t for t in (dk, dv) if t is not None)),
+                                          lambda: ({"o": o, "d_o": d_o, "dq": dq}, {"dk": dk, "dv": dv}))
     if lse is None:
         raise ValueError("lse is required")
     _check_lse(lse, (B, H, T), dev)
