@@ -263,3 +263,10 @@ def test_gradients_of_few_states_keep_their_precision(mw, D, M, lens):
             g = got[name][b].double().cpu()
             g = g if name == "dq" else g[:, :n[b]]
             assert (g - w).norm() <= 2.0 ** -8 * math.sqrt(2 / 3) * w.norm(), (name, b, ((g - w).norm() / w.norm()).item())
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("M,lens", [(300, [290, 41]), (64, [64, 64])])
+def test_rows_that_fill_the_card(mw, D, M, lens):
+    """Several rounds of the largest row tiles, whole key steps and partly filled ones, members of unlike lengths."""
+    verify(mw, 2, 6, 3, 9001, M, D, lens=lens, layout="bthd", seed=40 + M)
