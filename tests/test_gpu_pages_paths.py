@@ -82,6 +82,61 @@ def test_as_many_members_as_a_call_may_name(mw, B, D, ql, H):
     attend(mw, cache, model, seqs[::-1], 1, ql, H, 0, seed=B + 1, split=False, layout="bthd")
 
 
+def pages_plan(D, R, blocks, Hkv, ws=1 << 62):
+    fn = mw_lib.load()["_ZN2mw10pages_planEiiPKiiim"]  # mw::pages_plan(int, int, const int*, int, int, size_t)
+    fn.restype = Plan
+    fn.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_int), ctypes.c_int, ctypes.c_int, ctypes.c_size_t]
+    return fn(D, R, (ctypes.c_int * len(blocks))(*blocks), len(blocks), Hkv, ws)
+
+
+@pytest.mark.parametrize("n", [32, 63, 64, 65, 128, 256])
+@pytest.mark.parametrize("D,R", [(64, 1), (72, 4), (128, 1)])
+def test_one_long_member_is_cut_however_many_short_ones_there_are(n, D, R):
+    plan = pages_plan(D, R, [2] * (n // 2) + [248] + [2] * (n - n // 2 - 1), 16)
+    assert plan.n_splits >= 4 and plan.n_splits == -(-248 // plan.chunk)
+    assert pages_plan(D, R, [2] * (n - 1) + [248], 16, 0).n_splits == 1  # without a workspace
+
+
+@pytest.mark.parametrize("n", [64, 128, 256])
+def test_members_of_one_length_that_fill_the_card_are_not_cut(n):
+    for blocks in (1, 3, 4, 100, 248):
+        assert pages_plan(128, 1, [blocks] * n, 16).n_splits == 1
+    assert pages_plan(128, 1, [0] * n, 16).n_splits == 1
+
+
+@pytest.mark.parametrize("blocks", [[250000] + [1] * 255, [250000] * 2, [5], [0, 0], [4, 1]])
+@pytest.mark.parametrize("Hkv,R", [(1, 64), (16, 64), (3, 1)])
+def test_partials_of_long_members_stay_within_a_gibibyte(blocks, Hkv, R):
+    plan = pages_plan(128, R, blocks, Hkv)
+    assert 1 <= plan.chunk and plan.n_splits == max(1, -(-max(blocks) // plan.chunk))
+    assert plan.n_splits == 1 or plan.n_splits * len(blocks) * Hkv * R * 130 * 4 <= 1 << 30
+
+
+def test_a_workspace_of_the_size_asked_for_gets_the_plan_it_was_asked_for():
+    import random
+    rng = random.Random(1)
+    for _ in range(400):
+        D, R, Hkv = rng.choice([64, 72, 128]), rng.choice([1, 5, 32, 64]), rng.choice([1, 3, 16])
+        top = int(2 ** rng.uniform(0, 18))
+        blocks = [rng.choice([top, rng.randint(0, top), 1]) for _ in range(int(2 ** rng.uniform(0, 8)))]
+        free = pages_plan(D, R, blocks, Hkv)
+        exact = free.n_splits * len(blocks) * Hkv * R * (D + 2) * 4 if free.n_splits > 1 else 0
+        for ws in (exact, exact + 100):
+            plan = pages_plan(D, R, blocks, Hkv, ws)
+            assert (plan.n_splits, plan.chunk) == (free.n_splits, free.chunk), (D, R, Hkv, blocks)
+        less = pages_plan(D, R, blocks, Hkv, exact // 2)
+        assert less.n_splits == 1 or less.n_splits * len(blocks) * Hkv * R * (D + 2) * 4 <= exact // 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,ql,Hkv", [(64, 1, 16), (72, 8, 16), (128, 33, 16)])
+def test_one_long_member_among_many_short_ones(mw, D, ql, Hkv):
+    cache, model = filled(mw, Hkv, 64, D, [7000, 70, 0, 130], seed=D)
+    seqs = [1, 2, 3] * 10 + [0] + [3, 1, 2] * 11
+    assert mw.mw_chunk_attn_paged_workspace_size(cache, seqs, Hkv, 1, ql) > 0
+    attend(mw, cache, model, seqs, 1, ql, Hkv, 0, seed=D)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n", [32, 33, 70])
 @pytest.mark.parametrize("D", [64, 72])
