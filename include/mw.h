@@ -434,7 +434,7 @@ int mw_chunk_attn_cached_fp8(const void* q8, const void* k8_new, const void* v8_
  * A batch member without a state (kv_len[b] <= 0) has O = 0 and LSE = -inf.
  *
  * q, o     : bf16 [B, H, T, D];  k, v : bf16 [B, Hkv, M, D]
- * kv_len   : int32 [B] in device memory, or NULL.  Values are taken as at most M.
+ * kv_len   : int32 [B] in device memory, 16-byte aligned, or NULL.  Values are taken as at most M.
  *            States behind kv_len[b] are not read: they may hold anything.
  * lse      : fp32 [B, H, T], or NULL
  * strides  : 4 entries, for q, k, v, o (NULL = all contiguous).  A k or v stride
@@ -446,7 +446,8 @@ int mw_chunk_attn_cached_fp8(const void* q8, const void* k8_new, const void* v8_
  * Arithmetic as in mw_block_causal_attn_fwd.  The calling thread's current device
  * must be the device of the stream and of the tensors.
  * Errors: MW_EINVAL (null q, k, v or o, sizes < 1, H not a multiple of Hkv, scale
- * not finite and > 0, the stride checks of mw_strides), MW_EALIGN,
+ * not finite and > 0, the stride checks of mw_strides), MW_EALIGN (any pointer, kv_len,
+ * lse and workspace among them, or a stride),
  * MW_EUNSUPPORTED (D; T * H / Hkv or M above 2^24), MW_EHIP.
  * ---------------------------------------------------------------------- */
 size_t mw_cross_attn_workspace_size(int B, int H, int Hkv, int T, int M, int D);

@@ -620,14 +620,20 @@ def _cross_args(q, k, v, kv_len, rows, keys, named):
     return B, H, Hkv, T, M, D, dev
 
 
+def _aligned(kv_len):
+    """kv_len, or a copy of one whose first entry is not on 16 bytes, as the library wants it: a slice of a longer
+    list of lengths.  (A sum, not a clone: a kernel, which a captured graph repeats over the list's new values.)"""
+    return kv_len if kv_len is None or kv_len.data_ptr() % 16 == 0 else kv_len + 0
+
+
 def mw_cross_attn_workspace_size(B: int, H: int, Hkv: int, T: int, M: int, D: int) -> int:
     return int(load().mw_cross_attn_workspace_size(B, H, Hkv, T, M, D))
 
 
 def mw_cross_attn_fwd(q, k, v, kv_len=None, scale=None, out=None, lse=None, workspace=None):
     """Cross attention forward.  q: bf16 [B,H,T,D]; k, v: bf16 [B,Hkv,M,D] with Hkv dividing H (views with a
-    contiguous head dimension are read in place); kv_len: int32 [B] on the GPU, the valid states of each batch
-    member (None: all M).  Returns (o, lse).
+    contiguous head dimension are read in place); kv_len: int32 [B] on the GPU (a slice of a
+    longer list too), the valid states of each batch member (None: all M).  Returns (o, lse).
 
     With no workspace given, one of the size the library asks for is allocated here (torch)."""
     torch = _torch()
@@ -641,6 +647,7 @@ def mw_cross_attn_fwd(q, k, v, kv_len=None, scale=None, out=None, lse=None, work
         need = mw_cross_attn_workspace_size(B, H, Hkv, T, M, D)
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
     nbytes = _check_workspace(workspace, dev)
+    kv_len = _aligned(kv_len)
     with _on_device(dev):
         _check(load().mw_cross_attn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(lse),
                                         _strides(q, k, v, o), B, H, Hkv, T, M, D, scale, _ptr(workspace), nbytes,
@@ -670,6 +677,7 @@ def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=N
     dq = torch.empty((B, H, T, D), dtype=q.dtype, device=dev) if dq is None else dq
     dk = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dk is None else dk
     dv = torch.empty((B, Hkv, M, D), dtype=q.dtype, device=dev) if dv is None else dv
+    kv_len = _aligned(kv_len)
     with _on_device(dev):
         _check(load().mw_cross_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(kv_len), _ptr(o), _ptr(d_o), _ptr(lse), _ptr(dq),
                                         _ptr(dk), _ptr(dv), _ptr(workspace), nbytes,
