@@ -576,7 +576,7 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
  *                by H / cache->H query heads each
  * k_new, v_new : bf16 [n_seqs, cache->H, n_queued * q_len, D], or both NULL: the
  *                cached tokens alone (O = 0, LSE = -inf where there are none)
- *                (a value that a row does not see weighs 0 there: it has to be finite)
+ *                (a key or value that a row does not see weighs 0 there, and has to be finite)
  * lse          : fp32 [n_seqs, H, n_queued * q_len], or NULL
  * workspace    : optional, as in mw_chunk_attn_cached; sized for the sequences'
  *                present lengths by mw_chunk_attn_paged_workspace_size

@@ -75,8 +75,8 @@ __device__ __forceinline__ void add_groups(f32x16 (&acc)[N], int group, int slot
 // BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
 // first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
 // the registers).  Lanes behind the last key repeat it and store zeros.
-// Bound by the matrix units' share of a SIMD's two waves and by LDS reads (48% and 36% of the time busy): 12 heads x
-// 19200 rows x 512 keys, D = 128: 129 us, 934 TF.
+// Bound by the matrix units' share of a SIMD's two waves and by LDS reads (48% and 35% of the time busy): 12 heads x
+// 19200 rows x 512 keys, D = 128: 127 to 130 us, 930 to 954 TF.
 template <int D, int NWK, int QG, int BM, int VL>
 __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdParams p, int n_ktiles) {
   constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
@@ -316,8 +316,8 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
 }
 
 // dQ: NW waves of 32 rows each (Q and dO fragments, dQ^T in registers), walking the keys of range `split`, BN a step.
-// Few keys a row and long prologues (Q, dO and O of every row are read once): the same 12 heads 116 us, 776 TF, the
-// matrix units busy 40% of it.
+// Few keys a row and long prologues (Q, dO and O of every row are read once): the same 12 heads 115 us, 790 TF, the
+// matrix units busy 41% of it.  (D = 72 at three waves a SIMD spills six registers, 28 bytes a lane.)
 template <int D, int NW, int BN, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void cross_dq_kernel(CrossBwdParams p, int n_rtiles) {
   constexpr int BM = 32 * NW, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;

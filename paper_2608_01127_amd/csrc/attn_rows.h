@@ -6,11 +6,15 @@
 // of one tile: row r of key head hk is token r / G of query head hk G + r % G.  With one
 // token and G heads a tile then reads the keys once for all of them.
 //
-// Keys.  A workgroup visits key steps of BK keys: first the cached tokens of its
-// sequence (PAGED), then the bf16 keys (the states, or the queued tokens' own keys).
-// Each kind starts a step of its own and its last step may be partly filled; rows of a
-// staged tile behind the last key repeat it, so that nothing behind the data is read and
-// the masked products meet finite values.
+// Keys.  A workgroup visits key steps of BK keys: cached tokens of its sequence (PAGED) and
+// bf16 keys (the states, or the queued tokens' own keys).  Each kind starts a step of its
+// own and its last step may be partly filled.  The steps that every row sees whole come
+// first, cached ones, then bf16 ones; then the partly filled cached step and the bf16 steps
+// that some rows see in part.  Rows of a staged tile behind the last key repeat it (codes at
+// D = 72: zeros), so that nothing behind the data is read and the masked products meet
+// finite values.  D = 72 contracts 80 columns: the last eight of a key row in LDS are the
+// next row's first ones, against zeros in Q, so that a key a row does not see has to be
+// finite as its value has.
 //
 // Cached tokens are e4m3 codes with a power-of-two scale for each 64 tokens and head: a
 // step never straddles a page, and a code times its scale is exact in bf16, so a tile is
@@ -424,9 +428,10 @@ struct CodeTile {
 
 // NW waves in KG key groups of NW / KG waves of 32 rows each; a step stages KG * BN keys,
 // of which a group takes its BN.  WPS: waves per SIMD the registers are allocated for.
-// Bound by a SIMD's two or three waves: of a step's time the matrix unit is busy 40 to 50%, the vector unit (softmax;
-// over pages the conversion too) 46%, and they overlap only between waves.  12 heads x 19200 rows x 2048 keys, D = 128:
-// 240 us, 1007 TF (a plain product of 8192^3: 1246); 16 heads x 4800 rows over 15000 cached tokens 852 us, 914 TF.
+// Bound by a SIMD's two or three waves: over long keys the matrix units are busy 40 to 53% of the time, and waves at work
+// on a vector or matrix instruction (softmax; over pages the conversion too) 45 to 51% of a SIMD; the two overlap only
+// between waves.  12 heads x 19200 rows x 2048 keys, D = 128: 240 to 245 us, 990 to 1007 TF (a plain product of 8192^3:
+// 1246); 16 heads x 4800 rows, one chunk that sees 15000 cached tokens and itself, 852 to 879 us, 886 to 914 TF.
 template <int D, bool PAGED, int NW, int BN, int KG, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, RowsSeqs<PAGED> seqs) {
   constexpr int NWR = NW / KG, BM = 32 * NWR, NT = 64 * NW, BK = BN * KG, NB = BK / 64;

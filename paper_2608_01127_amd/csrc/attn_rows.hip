@@ -37,8 +37,9 @@ hipError_t launch_tile(RowsParams p, const RowsSeqs<PAGED>& seqs, const RowsPlan
 }
 
 #ifdef MW_ROWS_PAGED
-// Four waves; two stages a wave leave room for two workgroups a CU, whose prologues and ends overlap (with four stages
-// and one workgroup: one token of 8 sequences over up to 15840 tokens 27.3 us for 25.2, in two rounds 34.8 for 27.5).
+// Four waves; up to 32 rows (RB = 1) two stages a wave leave room for two workgroups a CU, whose prologues and ends
+// overlap (with four stages and one workgroup: one token of 8 sequences over up to 15840 tokens 27.3 us for 25.2, in two
+// rounds 34.8 for 27.5).  RB = 2 is compiled for one: at D = 128 it takes 443 registers and 135 KB of LDS for the join.
 template <int RB>
 hipError_t launch_pages(RowsParams p, const PageRanges& ranges, const RowsPlan& plan, hipStream_t stream) {
   p.n_splits = plan.n_splits;
@@ -52,6 +53,7 @@ hipError_t launch_pages(RowsParams p, const PageRanges& ranges, const RowsPlan& 
 template <bool PAGED>
 hipError_t launch_rows(const RowsParams& p, const RowsSeqs<PAGED>& seqs, const RowsPlan& plan, hipStream_t stream) {
   if (plan.bm == 64) return launch_tile<PAGED, 4, 32, 2, 2>(p, seqs, plan, stream);
+  // (bf16 keys at D = 72: three waves a SIMD spill five registers, 24 bytes a lane)
   return launch_tile<PAGED, 4, 64, 1, kD == 128 || (kD == 72 && PAGED) ? 2 : 3>(p, seqs, plan, stream);
 }
 
