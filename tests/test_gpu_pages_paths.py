@@ -129,6 +129,43 @@ def test_a_workspace_of_the_size_asked_for_gets_the_plan_it_was_asked_for():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("ql,flags", [(1, 0), (1, 1), (3, 0), (3, 1)])
+def test_as_many_queued_chunks_as_a_call_may_have(mw, D, ql, flags):
+    cache, model = filled(mw, 1, 64, D, [90, 0, 64], seed=D)
+    attend(mw, cache, model, [0, 1, 2], 64, ql, 1, flags, seed=ql)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("rows", [1, 40, 100])
+def test_a_smaller_workspace_gives_fewer_ranges(mw, D, rows):
+    """Down to one byte less than two ranges take; the results stay within their bounds, and what lies behind the
+    workspace is left as it was."""
+    import torch
+    n = 5000
+    cache, model = filled(mw, 1, 64, D, [n], seed=D)
+    q = randn((1, 1, rows, D), 1)
+    k, v = (t[None] for t in model.values(0))
+    kb, vb = k.bfloat16(), v.bfloat16()  # exact: codes times powers of two
+    none = torch.zeros((1, 1), dtype=torch.bool, device="cuda")
+    want = attention64(q[0, 0], k[0, 0], v[0, 0], none, 1 / math.sqrt(D))
+    one = rows * (D + 2) * 4  # bytes of one range
+    for need, call in ((mw.mw_chunk_attn_paged_workspace_size(cache, [0], 1, 1, rows),
+                        lambda ws, lse: mw.mw_chunk_attn_paged(q, None, None, 1, rows, cache, [0], lse=lse, workspace=ws)[0]),
+                       (mw.mw_cross_attn_workspace_size(1, 1, 1, rows, n, D),
+                        lambda ws, lse: mw.mw_cross_attn_fwd(q, kb, vb, lse=lse, workspace=ws)[0])):
+        assert need >= 4 * one and need % one == 0
+        for size in (need, need - 1, need // 2, 2 * one, 2 * one - 1):
+            buf = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+            lse = torch.empty((1, 1, rows), device="cuda")
+            o = call(buf[:size], lse)
+            check(f"o with {size} of {need} bytes", o[0, 0], *want["o"])
+            check(f"lse with {size} of {need} bytes", lse[0, 0], *want["lse"])
+            assert bool((buf[size:] == 0xA5).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("D,ql,Hkv", [(64, 1, 16), (72, 8, 16), (128, 33, 16)])
 def test_one_long_member_among_many_short_ones(mw, D, ql, Hkv):
     cache, model = filled(mw, Hkv, 64, D, [7000, 70, 0, 130], seed=D)
