@@ -430,7 +430,7 @@ struct CodeTile {
 // of which a group takes its BN.  WPS: waves per SIMD the registers are allocated for.
 // Bound by a SIMD's two or three waves: over long keys the matrix units are busy 40 to 53% of the time, and waves at work
 // on a vector or matrix instruction (softmax; over pages the conversion too) 45 to 51% of a SIMD; the two overlap only
-// between waves.  12 heads x 19200 rows x 2048 keys, D = 128: 240 to 245 us, 990 to 1007 TF (a plain product of 8192^3:
+// between waves.  12 heads x 19200 rows x 2048 keys, D = 128: 240 to 245 us, 987 to 1007 TF (a plain product of 8192^3:
 // 1246); 16 heads x 4800 rows, one chunk that sees 15000 cached tokens and itself, 852 to 879 us, 886 to 914 TF.
 template <int D, bool PAGED, int NW, int BN, int KG, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void attn_rows_kernel(RowsParams p, RowsSeqs<PAGED> seqs) {
