@@ -54,7 +54,7 @@ typedef enum {
   MW_EINVAL = -1,        /* null pointer, non-positive size, inconsistent sizes */
   MW_EUNSUPPORTED = -2,  /* head dimension other than 64, 72 or 128, or a limit exceeded */
   MW_EALIGN = -3,        /* a pointer that is not 16-byte aligned */
-  MW_EFULL = -4,         /* append to a ring whose slots are all live, or with too few free pages */
+  MW_EFULL = -4,         /* append to a ring whose slots are all live; too few free pages */
   MW_EEMPTY = -5,        /* evict more chunks (or full pages) than are live */
   MW_EHIP = -6           /* the HIP runtime reported an error at launch */
 } mw_status;
@@ -476,6 +476,134 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
                       float scale, mw_stream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Packed sequences: attention of sequences of different lengths that lie one behind
+ * the other, without padding (clips or prompts of a batch; grouped heads).
+ *
+ * Sequence s has the queries cu_q[s] .. cu_q[s + 1] - 1 and the keys cu_k[s] ..
+ * cu_k[s + 1] - 1 (device arrays of N + 1 int32, not decreasing, within [0, total_q]
+ * and [0, total_k]; cu_k may be cu_q; sequences may be empty).  Its nq queries are
+ * the last of its nk tokens: query i has the place p = i + nk - nq and sees key j iff
+ *     p >= 0  and  floor(j / chunk_len) <= floor(p / chunk_len)
+ * (chunk_len = 1: token-causal; chunk_len >= nk: every query of a place >= 0 sees every
+ * key).  With nq = nk this is mw_block_causal_attn_* for each sequence; with nq < nk
+ * the newest tokens attend to all before them: nq = 1 is the single token of a
+ * generation step.  A query that sees no key has O = 0 and LSE = -inf.  H query heads
+ * share Hkv key heads (Hkv divides H): query head h reads key head h / (H / Hkv).
+ *
+ * mw_packed is a batch's plan: which workgroup takes which tiles, worked out on the
+ * device from cu_q and cu_k by mw_packed_init, for any number of calls on tensors of
+ * these sizes.  The plan buffer (16-byte aligned, mw_packed_plan_bytes) holds copies of
+ * all that the calls read; cu_q and cu_k are not read again.  New lengths: call
+ * mw_packed_init again (in stream order; it may be recorded into a graph, as the calls
+ * may).  Lengths out of order or out of range lead to undefined results, but not to
+ * accesses outside of the tensors.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const int32_t* cu_q;
+  const int32_t* cu_k;
+  int32_t* plan;
+  int N, total_q, total_k, H, Hkv, D, chunk_len;
+  int backward; /* 1: planned for the backward too */
+} mw_packed;
+
+/* Bytes of a plan (0 for sizes out of range). */
+size_t mw_packed_plan_bytes(int N, int total_q, int total_k, int H, int Hkv, int D, int chunk_len, int backward);
+
+/* Plan a batch.  backward != 0: also its backward.
+ * Errors: MW_EINVAL (null, sizes < 1, H not a multiple of Hkv, plan too small), MW_EALIGN
+ * (plan on 16 bytes, cu_q and cu_k on 4), MW_EUNSUPPORTED (D; N > 2^16, H > 2^14, total_q *
+ * H / Hkv or total_k above 2^24), MW_EHIP. */
+int mw_packed_init(mw_packed* p, const int32_t* cu_q, const int32_t* cu_k, int32_t* plan, size_t plan_bytes, int N,
+                   int total_q, int total_k, int H, int Hkv, int D, int chunk_len, int backward, mw_stream_t stream);
+
+/* Forward.
+ * q, o     : bf16 [total_q, H, D];  k, v : bf16 [total_k, Hkv, D]
+ * lse      : fp32 [H, total_q]
+ * workspace: at least mw_packed_attn_workspace_size(p) bytes (0: none is needed): fp32
+ *            partial results of tiles that are cut along the keys, in calls of few rows
+ * strides  : 4 entries, for q, k, v, o (NULL = all contiguous): h and t as in mw_strides,
+ *            t the stride of the tokens; b is not used
+ * Rows of o and lse behind the last sequence are left as they were, and tokens behind it
+ * are not read.  A key or value that a row does not see weighs 0 there, and has to be finite;
+ * those of other sequences may hold anything.
+ * Arithmetic as in mw_block_causal_attn_fwd.  The calling thread's current device must be
+ * the device of the stream and of the tensors.
+ * Errors: MW_EINVAL (null, p not initialised, workspace too small, scale not finite and
+ * > 0, the stride checks of mw_strides), MW_EALIGN, MW_EHIP. */
+size_t mw_packed_attn_workspace_size(const mw_packed* p);
+int mw_packed_attn_fwd(const void* q, const void* k, const void* v, const mw_packed* p, void* o, float* lse, float scale,
+                       void* workspace, size_t workspace_bytes, const mw_strides* strides, mw_stream_t stream);
+
+/* Backward for the loss sum(dO * O): dQ, and dK and dV summed over the query heads that
+ * share a key head; 0 where nothing was seen.
+ * q, k, v, p, o, lse : as given to and left by the forward (p planned with backward)
+ * d_o, dq : bf16 [total_q, H, D];  dk, dv : bf16 [total_k, Hkv, D], written (not accumulated);
+ *           rows behind the last sequence are left as they were
+ * workspace : mw_packed_attn_bwd_workspace_size(p) bytes: two fp32 for each row, and the
+ *           fp32 gradients of cut tiles
+ * strides : 8 entries, for q, k, v, o, d_o, dq, dk, dv (NULL = all contiguous)
+ * The result is deterministic (no atomics).
+ * Errors: as the forward, plus MW_EINVAL for a batch planned without its backward. */
+size_t mw_packed_attn_bwd_workspace_size(const mw_packed* p);
+int mw_packed_attn_bwd(const void* q, const void* k, const void* v, const void* o, const void* d_o, const float* lse,
+                       const mw_packed* p, void* dq, void* dk, void* dv, float scale, void* workspace,
+                       size_t workspace_bytes, const mw_strides* strides, mw_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions of queries and keys, in one call for both.
+ *
+ * A band is dim_count dimensions of the head from dim_offset on, in pairs: interleaved
+ * (2 i, 2 i + 1), as in mw_rope, or halves (i, i + dim_count / 2).  Pair i of a token at
+ * position p on the band's axis turns by p f_i radians and grows by gain:
+ *     y_a = gain (x_a cos - x_b sin),  y_b = gain (x_b cos + x_a sin)
+ *     f_i = theta^(-2 i / dim_count)
+ * and for contexts longer than the trained ones, with factor s != 1,
+ *     f_i (r + (1 - r) / s),  r = (trained_len f_i / 2 pi - turns_lo) / (turns_hi - turns_lo)
+ * held in [0, 1] (r = 0, positions divided by s, where turns_hi = turns_lo): pairs that turn
+ * often within the trained length keep their frequency, slow ones are stretched.
+ * Dimensions of no band are copied.  Several bands have the axes of a video's tokens (time,
+ * height, width).
+ * ---------------------------------------------------------------------- */
+#define MW_MAX_ROPE_BANDS 4
+#define MW_MAX_ROPE_PAIRS 64
+typedef struct {
+  int dim_offset, dim_count;   /* even; bands do not share dimensions */
+  double theta;                /* > 0 */
+  int axis;                    /* which of the positions (0 .. MW_MAX_ROPE_BANDS - 1) */
+  double factor;               /* > 0; 1: frequencies as they are */
+  double trained_len, turns_lo, turns_hi;
+} mw_rope_band;
+/* Bands as the calls take them: plain data, filled by mw_rope_bands_init. */
+typedef struct {
+  int n_bands, n_pairs, n_axes, halves;
+  float gain;
+  int dim_offset[MW_MAX_ROPE_BANDS], dim_count[MW_MAX_ROPE_BANDS];
+  uint8_t axis[MW_MAX_ROPE_PAIRS];
+  double freq[MW_MAX_ROPE_PAIRS]; /* turns of a pair per position, f_i / 2 pi */
+} mw_rope_bands;
+
+/* halves: 1 or 0 (interleaved).  Host only.  Errors: MW_EINVAL. */
+int mw_rope_bands_init(mw_rope_bands* out, const mw_rope_band* bands, int n_bands, int halves, float gain);
+
+/* Apply to q and k (inverse = 0), or its transpose, the turn back with the same gain
+ * (inverse = 1): the gradients of q and k from those of the outputs.
+ * q, q_out : bf16 [B, H, T, D];  k, k_out : bf16 [B, Hkv, T, D], or both NULL
+ *            (an output may be its input, with the same strides; else they must not overlap)
+ * positions: device integers of pos_bytes = 4 or 8 bytes, any value; of axis a, member b and
+ *            token t at a * pos_strides->h + b * pos_strides->b + t * pos_strides->t (in
+ *            integers; strides of 0 share them); or NULL: first + t (bands of one axis)
+ * strides  : 4 entries, for q, k, q_out, k_out (NULL = all contiguous)
+ * D        : 64, 72 or 128.
+ * Arithmetic: the turns in 64 bits, sine, cosine and products in 32, outputs rounded to bf16
+ * (nearest even) once.  The calling thread's current device must be the device of the stream
+ * and of the tensors.
+ * Errors: MW_EINVAL (null, bands not initialised or beyond D, sizes < 1, several axes
+ * without positions), MW_EALIGN, MW_EUNSUPPORTED (D; T > 2^24, B * T >= 2^30, H > 2^14), MW_EHIP. */
+int mw_rope_apply(const void* q, const void* k, void* q_out, void* k_out, const mw_rope_bands* bands, const void* positions,
+                  int pos_bytes, const mw_strides* pos_strides, int64_t first, int inverse, const mw_strides* strides, int B,
+                  int H, int Hkv, int T, int D, mw_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * Paged 8-bit cache with a scale for each block of tokens and head.
  *
  * A pool of P pages of L tokens each holds the keys and values of up to N
@@ -565,6 +693,41 @@ int mw_kvpages_evict(mw_kvpages* c, int seq, int first_page, int n_pages, mw_str
  * be given back or lent out).  Returns the number of pages moved, or a negative status.
  * Errors: MW_EINVAL, MW_EHIP. */
 int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
+
+/* Attention weight that each cached token of the listed sequences (n_seqs different ones)
+ * gets from the queries of a call of mw_chunk_attn_paged, summed over rows and heads:
+ *     weights[s][j] (+)= sum_{h, t} exp(scale q[b, h, t] . k_j - lse[b, h, t]),  s = seqs[b]
+ * q       : bf16 [n_seqs, H, T, D] view (strides: 1 entry, NULL = contiguous) and
+ * lse     : fp32 [n_seqs, H, T] as given to and left by that call, over the same cached tokens
+ *           (a row of LSE -inf weighs nothing)
+ * weights : fp32 [N, W * L], a row for each sequence; entries behind its length are left as
+ *           they were.  add = 1: added to what is there; 0: written.  They are the caller's: fork,
+ *           copy, free and evict do not move them.
+ * workspace: mw_kvpages_weigh_workspace_size(...) bytes, or NULL: the rows of a call are then not
+ *           divided among workgroups.
+ * Products as in mw_chunk_attn_paged, sums in fp32, deterministic.
+ * Refuses a stream under HIP graph capture (the host's lengths size the call).
+ * Errors: MW_EINVAL (also a sequence listed twice), MW_EALIGN, MW_EUNSUPPORTED, MW_EHIP. */
+size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T);
+int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const void* q, const float* lse, int H, int T,
+                     float* weights, int add, float scale, void* workspace, size_t workspace_bytes, const mw_strides* strides,
+                     mw_stream_t stream);
+
+/* Drop the lightest tokens of the listed sequences (n_seqs different ones), so that n_keep
+ * stay: the first `first`, the last `recent`, and of the others the heaviest by their row of
+ * weights (of equal ones those in front; a NaN is the lightest), in their order.  Sequences of
+ * at most n_keep tokens are left alone.  What stays is copied into new pages, taken before
+ * the old ones are given back, but for the whole pages of the first `first` tokens, which stay
+ * (and stay shared).  A block's new scale is the least that holds its tokens; codes are rounded
+ * again as RNE_e4m3(value / scale), which changes only codes that become subnormal.  The
+ * row of weights is moved alike; entries from n_keep up to the old length become 0.
+ * weights  : fp32 [N, W * L];  workspace: mw_kvpages_evict_weighted_workspace_size(...) bytes
+ * The tokens' keys stay as committed.  All or nothing.
+ * Errors: MW_EINVAL (n_keep < 1, first + recent > n_keep, a sequence listed twice, workspace too
+ * small), MW_EALIGN, MW_EFULL (too few free pages), MW_EUNSUPPORTED, MW_EHIP. */
+size_t mw_kvpages_evict_weighted_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int n_keep, int first);
+int mw_kvpages_evict_weighted(mw_kvpages* c, const int32_t* seqs, int n_seqs, float* weights, int n_keep, int first,
+                              int recent, void* workspace, size_t workspace_bytes, mw_stream_t stream);
 
 /* Cached chunk attention over the pages: batch member b attends to the tokens of
  * sequence seqs[b] (host array, n_seqs <= MW_MAX_SEQS entries, repeats allowed) and

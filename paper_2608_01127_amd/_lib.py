@@ -31,6 +31,8 @@ MW_MAX_QUEUED = 64
 MW_MAX_SLOTS = 128
 MW_PAGE_BLOCK = 64
 MW_MAX_SEQS = 256
+MW_MAX_ROPE_BANDS = 4
+MW_MAX_ROPE_PAIRS = 64
 
 STATUS_NAMES = {0: "MW_OK", -1: "MW_EINVAL", -2: "MW_EUNSUPPORTED", -3: "MW_EALIGN", -4: "MW_EFULL",
                 -5: "MW_EEMPTY", -6: "MW_EHIP"}
@@ -64,6 +66,25 @@ class mw_rope(ctypes.Structure):
     _fields_ = [("dim_offset", ctypes.c_int), ("dim_count", ctypes.c_int), ("theta", ctypes.c_float)]
 
 
+class mw_rope_band(ctypes.Structure):
+    _fields_ = [("dim_offset", ctypes.c_int), ("dim_count", ctypes.c_int), ("theta", ctypes.c_double), ("axis", ctypes.c_int),
+                ("factor", ctypes.c_double), ("trained_len", ctypes.c_double), ("turns_lo", ctypes.c_double),
+                ("turns_hi", ctypes.c_double)]
+
+
+class mw_rope_bands(ctypes.Structure):
+    _fields_ = [("n_bands", ctypes.c_int), ("n_pairs", ctypes.c_int), ("n_axes", ctypes.c_int), ("halves", ctypes.c_int),
+                ("gain", ctypes.c_float), ("dim_offset", ctypes.c_int * MW_MAX_ROPE_BANDS),
+                ("dim_count", ctypes.c_int * MW_MAX_ROPE_BANDS), ("axis", ctypes.c_uint8 * MW_MAX_ROPE_PAIRS),
+                ("freq", ctypes.c_double * MW_MAX_ROPE_PAIRS)]
+
+
+class mw_packed(ctypes.Structure):
+    _fields_ = [("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("plan", ctypes.c_void_p), ("N", ctypes.c_int),
+                ("total_q", ctypes.c_int), ("total_k", ctypes.c_int), ("H", ctypes.c_int), ("Hkv", ctypes.c_int),
+                ("D", ctypes.c_int), ("chunk_len", ctypes.c_int), ("backward", ctypes.c_int)]
+
+
 class mw_strides(ctypes.Structure):
     _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
 
@@ -89,6 +110,8 @@ _cache_p = ctypes.POINTER(mw_kvcache)
 _str_p = ctypes.POINTER(mw_strides)
 _pages_p = ctypes.POINTER(mw_kvpages)
 _seq_p = ctypes.POINTER(ctypes.c_int32)
+_packed_p = ctypes.POINTER(mw_packed)
+_bands_p = ctypes.POINTER(mw_rope_bands)
 SIGNATURES = {
     "mw_last_error": ([], ctypes.c_char_p),
     "mw_version": ([], _i),
@@ -132,6 +155,18 @@ SIGNATURES = {
     "mw_kvpages_compact": ([_pages_p, _vp], _i),
     "mw_chunk_attn_paged_workspace_size": ([_pages_p, _seq_p] + [_i] * 4, _sz),
     "mw_chunk_attn_paged": ([_vp] * 3 + [_i, _i, _pages_p, _seq_p] + [_i] * 3 + [_vp, _vp, _f, _vp, _sz, _str_p, _vp], _i),
+    "mw_packed_plan_bytes": ([_i] * 8, _sz),
+    "mw_packed_init": ([_packed_p, _vp, _vp, _vp, _sz] + [_i] * 8 + [_vp], _i),
+    "mw_packed_attn_workspace_size": ([_packed_p], _sz),
+    "mw_packed_attn_fwd": ([_vp] * 3 + [_packed_p, _vp, _vp, _f, _vp, _sz, _str_p, _vp], _i),
+    "mw_packed_attn_bwd_workspace_size": ([_packed_p], _sz),
+    "mw_packed_attn_bwd": ([_vp] * 6 + [_packed_p] + [_vp] * 3 + [_f, _vp, _sz, _str_p, _vp], _i),
+    "mw_rope_bands_init": ([_bands_p, ctypes.POINTER(mw_rope_band), _i, _i, _f], _i),
+    "mw_rope_apply": ([_vp] * 4 + [_bands_p, _vp, _i, _str_p, ctypes.c_int64, _i, _str_p] + [_i] * 5 + [_vp], _i),
+    "mw_kvpages_weigh_workspace_size": ([_pages_p, _seq_p, _i, _i, _i], _sz),
+    "mw_kvpages_weigh": ([_pages_p, _seq_p, _i, _vp, _vp, _i, _i, _vp, _i, _f, _vp, _sz, _str_p, _vp], _i),
+    "mw_kvpages_evict_weighted_workspace_size": ([_pages_p, _seq_p, _i, _i, _i], _sz),
+    "mw_kvpages_evict_weighted": ([_pages_p, _seq_p, _i, _vp, _i, _i, _i, _vp, _sz, _vp], _i),
     "mw_sched_num_ticks": ([ctypes.POINTER(mw_sched_config)], ctypes.c_int64),
     "mw_sched_plan": ([ctypes.POINTER(mw_sched_config), ctypes.c_int64, ctypes.POINTER(mw_sched_tick)], _i),
 }
@@ -686,6 +721,190 @@ def mw_cross_attn_bwd(q, k, v, o, d_o, lse, kv_len=None, scale=None, workspace=N
     return dq, dk, dv
 
 
+# ----------------------------------------------------------------------------- packed sequences
+
+class Packed:
+    """Plan of a batch of sequences that lie one behind the other: cu_q int32 [N+1] on the GPU, the places where their
+    queries begin (and the last one ends) among total_q tokens; cu_k and total_k those of their keys (default: the
+    same).  H query heads share Hkv key heads of width D; chunk_len as in mw_block_causal_attn_fwd (1: token-causal).
+    backward=True plans the backward too.
+
+    update() plans again, over new contents of cu_q and cu_k; it may be captured into a graph.
+    Wraps the mw_packed descriptor.
+    """
+
+    def __init__(self, cu_q, total_q: int, H: int, Hkv: int, D: int, chunk_len: int = 1, cu_k=None, total_k=None,
+                 backward: bool = False):
+        torch = _torch()
+        self.cu_q, self.cu_k = cu_q, cu_q if cu_k is None else cu_k
+        total_k = total_q if total_k is None else total_k
+        for n, t in (("cu_q", self.cu_q), ("cu_k", self.cu_k)):
+            if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] < 2 or not t.is_contiguous() or t.device.type != "cuda":
+                raise ValueError(f"{n} must be a contiguous int32 tensor of N + 1 entries on a GPU")
+        if self.cu_k.shape != cu_q.shape or self.cu_k.device != cu_q.device:
+            raise ValueError("cu_q and cu_k must have the same length and device")
+        self.device = cu_q.device
+        self._sizes = (cu_q.shape[0] - 1, *map(_int32, (total_q, total_k, H, Hkv, D, chunk_len)), int(bool(backward)))
+        self.q_shape, self.k_shape = (self._sizes[1], H, D), (self._sizes[2], Hkv, D)
+        self.lse_shape = (H, self._sizes[1])
+        need = int(load().mw_packed_plan_bytes(*self._sizes))
+        self.plan = torch.empty(need // 4, dtype=torch.int32, device=self.device)
+        self.desc = mw_packed()
+        if need == 0:  # sizes out of range: the library says which
+            _check(load().mw_packed_init(ctypes.byref(self.desc), _ptr(self.cu_q), _ptr(self.cu_k), 16, 0, *self._sizes, None))
+        self.update()
+
+    def update(self) -> None:
+        with _on_device(self.device):
+            _check(load().mw_packed_init(ctypes.byref(self.desc), _ptr(self.cu_q), _ptr(self.cu_k), _ptr(self.plan),
+                                         self.plan.nbytes, *self._sizes, _stream_handle(self.device)))
+
+
+def _check_packed(pack: Packed, queries, keys):
+    """Tensors by name: bf16 views [total_q,H,D] and [total_k,Hkv,D] on the batch's device."""
+    bf16, index = _torch().bfloat16, pack.device.index
+    for shape, named in ((pack.q_shape, queries), (pack.k_shape, keys)):
+        for n, t in named:
+            if t is None:
+                continue
+            if t.dtype is not bf16:
+                raise TypeError(f"{n} must be bfloat16, got {t.dtype}")
+            if t.shape != shape:
+                raise ValueError(f"{n} must have shape {shape}, got {tuple(t.shape)}")
+            if t.get_device() != index:
+                raise ValueError("all tensors must be on the GPU of the batch")
+            if t.stride(2) != 1:
+                raise ValueError(f"{n} must have a contiguous last (head) dimension")
+
+
+def _packed_strides(*ts):
+    return _strides_array(*[(0, s[1], s[0]) for s in (t.stride() for t in ts)])
+
+
+def mw_packed_attn_workspace_size(pack: Packed) -> int:
+    return int(load().mw_packed_attn_workspace_size(ctypes.byref(pack.desc)))
+
+
+def mw_packed_attn_fwd(q, k, v, pack: Packed, scale=None, out=None, lse=None, workspace=None):
+    """Attention of packed sequences.  q: bf16 [total_q,H,D]; k, v: bf16 [total_k,Hkv,D] (views with a contiguous head
+    dimension are read in place).  Returns (o, lse): bf16 like q and fp32 [H,total_q]; rows behind the last
+    sequence are not written.
+
+    With no workspace given, one of the size the library asks for is allocated here (torch)."""
+    torch = _torch()
+    _check_packed(pack, (("q", q), ("out", out)), (("k", k), ("v", v)))
+    dev = pack.device
+    scale = 1.0 / math.sqrt(pack.desc.D) if scale is None else float(scale)
+    o = torch.empty_like(q) if out is None else out
+    lse = torch.empty(pack.lse_shape, dtype=torch.float32, device=dev) if lse is None else lse
+    _check_lse(lse, pack.lse_shape, dev)
+    if workspace is None:
+        need = mw_packed_attn_workspace_size(pack)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    nbytes = _check_workspace(workspace, dev)
+    with _on_device(dev):
+        _check(load().mw_packed_attn_fwd(_ptr(q), _ptr(k), _ptr(v), ctypes.byref(pack.desc), _ptr(o), _ptr(lse), scale,
+                                         _ptr(workspace), nbytes, _packed_strides(q, k, v, o), _stream_handle(dev)))
+    return o, lse
+
+
+def mw_packed_attn_bwd_workspace_size(pack: Packed) -> int:
+    need = int(load().mw_packed_attn_bwd_workspace_size(ctypes.byref(pack.desc)))
+    if need == 0:
+        _check(MW_EINVAL)  # (planned without the backward)
+    return need
+
+
+def mw_packed_attn_bwd(q, k, v, o, d_o, lse, pack: Packed, scale=None, workspace=None, dq=None, dk=None, dv=None):
+    """Backward of mw_packed_attn_fwd, for a batch planned with backward=True.  Returns (dq, dk, dv): bf16 [total_q,H,D]
+    and twice [total_k,Hkv,D], the latter summed over the query heads that share a key head."""
+    torch = _torch()
+    _check_packed(pack, (("q", q), ("o", o), ("d_o", d_o), ("dq", dq)), (("k", k), ("v", v), ("dk", dk), ("dv", dv)))
+    dev = pack.device
+    if lse is None:
+        raise ValueError("lse is required")
+    _check_lse(lse, pack.lse_shape, dev)
+    scale = 1.0 / math.sqrt(pack.desc.D) if scale is None else float(scale)
+    if workspace is None:
+        workspace = torch.empty(mw_packed_attn_bwd_workspace_size(pack), dtype=torch.uint8, device=dev)
+    nbytes = _check_workspace(workspace, dev)
+    # (a gradient of keys shared between heads does not share their strides)
+    dq = torch.empty(pack.q_shape, dtype=q.dtype, device=dev) if dq is None else dq
+    dk = torch.empty(pack.k_shape, dtype=q.dtype, device=dev) if dk is None else dk
+    dv = torch.empty(pack.k_shape, dtype=q.dtype, device=dev) if dv is None else dv
+    with _on_device(dev):
+        _check(load().mw_packed_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(d_o), _ptr(lse), ctypes.byref(pack.desc),
+                                         _ptr(dq), _ptr(dk), _ptr(dv), scale, _ptr(workspace), nbytes,
+                                         _packed_strides(q, k, v, o, d_o, dq, dk, dv), _stream_handle(dev)))
+    return dq, dk, dv
+
+
+# ----------------------------------------------------------------------------- rotary positions
+
+def rope_bands(bands, halves: bool = False, gain: float = 1.0) -> mw_rope_bands:
+    """Bands of the head for mw_rope_apply (see include/mw.h): dicts of dim_offset and dim_count, and optionally theta
+    (10000), axis (0), factor (1), trained_len, turns_lo and turns_hi.  halves: pairs (i, i + dim_count/2), else
+    (2i, 2i+1)."""
+    arr = (mw_rope_band * max(1, len(bands)))()
+    for x, b in zip(arr, bands):
+        b = {"theta": 1e4, "axis": 0, "factor": 1.0, "trained_len": 0.0, "turns_lo": 0.0, "turns_hi": 0.0, **b}
+        for n, v in b.items():
+            if n not in dict(mw_rope_band._fields_):
+                raise ValueError(f"a band has no {n}")
+            setattr(x, n, _int32(v) if n in ("dim_offset", "dim_count", "axis") else float(v))
+    out = mw_rope_bands()
+    _check(load().mw_rope_bands_init(ctypes.byref(out), arr, len(bands), int(bool(halves)), float(gain)))
+    return out
+
+
+def mw_rope_apply(q, k, bands: mw_rope_bands, positions=None, first: int = 0, inverse: bool = False, q_out=None, k_out=None):
+    """Rotary positions applied to q (bf16 [B,H,T,D]) and k (bf16 [B,Hkv,T,D], or None), or with inverse=True taken
+    back, which gives the gradients of q and k from those of the outputs.  positions: int32 or int64 on the GPU, [T] or
+    [B,T], for bands of several axes [axes,T] or [axes,B,T]; None: first, first + 1, ...  Views with a contiguous
+    head dimension are read and written in place; an output may be its input.  Returns (q_out, k_out)."""
+    torch = _torch()
+    B, H, T, D = q.shape if len(q.shape) == 4 else (0, 0, 0, 0)
+    dev = q.device
+    Hkv = 0
+    ts = [q] if q_out is None else [q, q_out]
+    if not _plain_views(ts, q.shape, q):
+        _bf16_4d("q", q, view=True)
+        _check_like("q_out", ts[-1], q.shape, dev)
+    if k is not None:
+        shape = (B, k.shape[1] if len(k.shape) == 4 else 0, T, D)
+        Hkv = shape[1]
+        ts = [k] if k_out is None else [k, k_out]
+        if not _plain_views(ts, shape, q):
+            _check_like("k", k, shape, dev)
+            _check_like("k_out", ts[-1], shape, dev)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    pos_strides, pos_bytes = None, 0
+    if positions is not None:
+        p, axes = positions, bands.n_axes
+        if p.dtype not in (torch.int32, torch.int64) or p.device != dev:
+            raise ValueError("positions must be int32 or int64 on the device of q")
+        s, shape = p.stride(), tuple(p.shape)
+        if axes > 1:
+            if shape not in ((axes, T), (axes, B, T)):
+                raise ValueError(f"positions must be [axes,T] or [axes,B,T] = {(axes, B, T)}, got {shape}")
+            pos_strides = _strides_array((s[1] if len(s) == 3 else 0, s[0], s[-1]))
+        else:
+            if shape not in ((T,), (B, T)):
+                raise ValueError(f"positions must be [T] or [B,T] = {(B, T)}, got {shape}")
+            pos_strides = _strides_array((s[0] if len(s) == 2 else 0, 0, s[-1]))
+        pos_bytes = p.element_size()
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    if k is not None and k_out is None:
+        k_out = torch.empty_like(k)
+    ks = (q, q_out) if k is None else (k, k_out)
+    with _on_device(dev):
+        _check(load().mw_rope_apply(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), ctypes.byref(bands), _ptr(positions), pos_bytes,
+                                    pos_strides, operator.index(first), int(bool(inverse)), _strides(q, ks[0], q_out, ks[1]),
+                                    B, H, Hkv, T, D, _stream_handle(dev)))
+    return q_out, k_out
+
+
 # ----------------------------------------------------------------------------- paged 8-bit cache
 
 class KVPages:
@@ -790,6 +1009,69 @@ def mw_kvpages_compact(cache: KVPages) -> int:
     """Move live pages to the front of the pool; returns how many moved."""
     with _on_device(cache.device):
         return _check(load().mw_kvpages_compact(ctypes.byref(cache.desc), _stream_handle(cache.device)))
+
+
+def mw_kvpages_weigh_workspace_size(cache: KVPages, seqs, H: int, T: int) -> int:
+    seqs = _seqs(seqs)
+    return int(load().mw_kvpages_weigh_workspace_size(ctypes.byref(cache.desc), seqs, len(seqs), _int32(H), _int32(T)))
+
+
+def _check_weights(cache: KVPages, weights):
+    d = cache.desc
+    if weights.dtype is not _torch().float32 or weights.shape != (d.N, d.W * d.L) or not weights.is_contiguous():
+        raise ValueError(f"weights must be a contiguous fp32 tensor of shape {(d.N, d.W * d.L)}, got {weights.dtype} "
+                         f"{tuple(weights.shape)}")
+    if weights.device != cache.device:
+        raise ValueError("weights must be on the device of the cache")
+
+
+def mw_kvpages_weigh(cache: KVPages, seqs, q, lse, weights, add: bool = True, scale=None, workspace=None) -> None:
+    """Sum, over the rows and heads of a mw_chunk_attn_paged call, of the attention weight that each cached token of the
+    listed sequences got, into weights (fp32 [N, W*L], a row for each sequence): added, or (add=False) written.
+    q: bf16 [len(seqs),H,T,D] and lse: fp32 [len(seqs),H,T], as given to and left by that call.
+
+    With no workspace given, one of the size the library asks for is allocated here (torch)."""
+    torch = _torch()
+    d, dev = cache.desc, cache.device
+    seqs = _seqs(seqs)
+    if not _plain_views((q,), q.shape, cache.k_pages) or (q.shape[0], q.shape[3]) != (len(seqs), d.D):
+        _bf16_4d("q", q, view=True)
+        _check_like("q", q, (len(seqs), *q.shape[1:3], d.D), dev)
+    B, H, T, _ = q.shape
+    if lse is None:
+        raise ValueError("lse is required")
+    _check_lse(lse, (B, H, T), dev)
+    _check_weights(cache, weights)
+    if workspace is None:
+        need = mw_kvpages_weigh_workspace_size(cache, seqs, H, T)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    nbytes = _check_workspace(workspace, dev)
+    scale = 1.0 / math.sqrt(d.D) if scale is None else float(scale)
+    with _on_device(dev):
+        _check(load().mw_kvpages_weigh(ctypes.byref(d), seqs, B, _ptr(q), _ptr(lse), H, T, _ptr(weights), int(bool(add)), scale,
+                                       _ptr(workspace), nbytes, _strides(q), _stream_handle(dev)))
+
+
+def mw_kvpages_evict_weighted_workspace_size(cache: KVPages, seqs, n_keep: int, first: int = 0) -> int:
+    seqs = _seqs(seqs)
+    return int(load().mw_kvpages_evict_weighted_workspace_size(ctypes.byref(cache.desc), seqs, len(seqs), _int32(n_keep),
+                                                               _int32(first)))
+
+
+def mw_kvpages_evict_weighted(cache: KVPages, seqs, weights, n_keep: int, first: int = 0, recent: int = 0,
+                              workspace=None) -> None:
+    """Drop the lightest tokens of the listed sequences by their rows of weights (fp32 [N, W*L], moved alike), so that
+    n_keep stay: the first `first`, the last `recent` and the heaviest of the others, in their order."""
+    dev = cache.device
+    seqs = _seqs(seqs)
+    _check_weights(cache, weights)
+    if workspace is None:
+        need = mw_kvpages_evict_weighted_workspace_size(cache, seqs, n_keep, first)
+        workspace = _torch().empty(max(16, need), dtype=_torch().uint8, device=dev)
+    nbytes = _check_workspace(workspace, dev)
+    with _on_device(dev):
+        _check(load().mw_kvpages_evict_weighted(ctypes.byref(cache.desc), seqs, len(seqs), _ptr(weights), _int32(n_keep),
+                                                _int32(first), _int32(recent), _ptr(workspace), nbytes, _stream_handle(dev)))
 
 
 def mw_chunk_attn_paged_workspace_size(cache: KVPages, seqs, H: int, n_queued: int, q_len: int) -> int:

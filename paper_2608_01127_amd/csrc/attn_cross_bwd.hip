@@ -34,43 +34,6 @@ __device__ __forceinline__ int xcd_range(int id, int n) {
   return x * q + min(x, rem) + id / 8;
 }
 
-// LDS of the dK/dV kernel: Q and dO tiles of BS rows, LSE and -Delta of those rows (two stages each), then VL V
-// fragments of each key wave.
-template <int D, int NWK, int QG, int BM, int VL>
-struct CrossLds {
-  static constexpr int NT = 64 * NWK * QG, BS = BM * QG;
-  static constexpr int TE = stage_elems<D, BS, NT>();
-  static constexpr int RT = BS < 64 ? 64 : BS;
-  static constexpr int STAGES = 2 * 2 * TE * 2 + 2 * 2 * RT * 4;
-  static constexpr int MERGE = QG == 1 ? 0 : (QG / 2) * NWK * (D / 32 + (D % 32 != 0)) * 16 * 64 * 4;
-  static constexpr int BYTES = STAGES + NWK * VL * 1024 > MERGE ? STAGES + NWK * VL * 1024 : MERGE;
-};
-
-// Sum of the row groups' tiles in group 0, through LDS: in each round the upper half of the groups hands its tiles
-// to the lower half (a fixed order).  Every wave calls it after the last read of `x`.
-template <int G, int NWK, int N>
-__device__ __forceinline__ void add_groups(f32x16 (&acc)[N], int group, int slot, int lane, float* x) {
-#pragma unroll
-  for (int half = G / 2; half >= 1; half >>= 1) {
-    __syncthreads();
-    if (group >= half && group < 2 * half) {
-      float* y = x + ((group - half) * NWK + slot) * N * 1024 + lane;
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[(n * 16 + i) * 64] = acc[n][i];
-    }
-    __syncthreads();
-    if (group < half) {
-      const float* y = x + (group * NWK + slot) * N * 1024 + lane;
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[n][i] += y[(n * 16 + i) * 64];
-    }
-  }
-}
-
 // dK/dV: NWK key waves of 32 keys each (K fragments, dK^T and dV^T in registers) in QG row groups; a step stages
 // BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
 // first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
@@ -82,7 +45,7 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void cross_dkdv_kernel(CrossBwdPa
   constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
   static_assert(16 * VL <= D, "the V fragments in LDS have no columns past D");
-  using LD = CrossLds<D, NWK, QG, BM, VL>;
+  using LD = KeyTileLds<D, NWK, QG, BM, VL>;
   constexpr int TE = LD::TE, RT = LD::RT;
   __shared__ __attribute__((aligned(16))) unsigned char lds[LD::BYTES];
   bf16_t(*Qs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);

@@ -1,0 +1,530 @@
+// Backward of the packed attention (gfx950): with P recomputed from Q, K and the forward's LSE,
+//   dV = sum_r P_r^T dO_r,  dP = dO V^T,  Delta = rowsum(dO O),  dS = P (dP - Delta),
+//   dQ = scale dS K,  dK = scale sum_r dS_r^T Q_r
+// over the rows r of a key head (attn_packed.hip).
+//
+//   dQ kernel    : a wave owns 32 rows and walks the keys they see; it forms Delta (and LSE log2 e) for the other one.
+//   dK/dV kernel : a wave owns 32 keys and walks the rows that see them, staged in LDS.
+//   join kernel  : adds the parts of tiles that the plan has cut, in their order.  No atomics.
+#include <algorithm>
+#include <type_traits>
+
+#include "attn_packed.h"
+
+namespace mw {
+
+namespace {
+
+constexpr int kD = MW_PACKED_HEAD_DIM;
+
+// Byte offsets, from the step's first row, of the pieces this thread stages of ROWS rows of a key head's G query heads
+// (StagePlan's pieces; G divides ROWS and a step begins with a token's first row).
+template <int D, int ROWS, int NT>
+struct GroupOffsets {
+  unsigned off[StagePlan<D, ROWS, NT>::ROUNDS];
+  __device__ __forceinline__ GroupOffsets(const Strides& s, int G, int tid) {
+    using SP = StagePlan<D, ROWS, NT>;
+#pragma unroll
+    for (int it = 0; it < SP::ROUNDS; ++it) {
+      const int ci0 = it * NT + tid;
+      const int ci = (SP::PIECES % NT == 0 || ci0 < SP::PIECES) ? ci0 : 0;
+      const int row = ci / SP::SLOTS, ls = (ci % SP::SLOTS) ^ Tile<D>::swz(row);
+      const int t = (unsigned)row / (unsigned)G;
+      off[it] = (unsigned)((t * s.t + (row - t * G) * s.h) * 2 + ls * 16);
+    }
+  }
+  __device__ __forceinline__ void stage(bf16_t* lds_tile, const bf16_t* first_row, int tid) const {
+#pragma unroll
+    for (int it = 0; it < StagePlan<D, ROWS, NT>::ROUNDS; ++it)
+      dma_lds_16_s(first_row, off[it], lds_addr(lds_tile) + it * NT * 16 + wave_stage_off(tid));
+  }
+};
+
+// dK/dV: NWK key waves of 32 keys each (K fragments, dK^T and dV^T in registers) in QG row groups; a step stages
+// BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
+// first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
+// the registers).  Lanes behind the last key repeat it and store nothing.
+template <int D, int NWK, int QG, int BM, int VL>
+__global__ __launch_bounds__(64 * NWK * QG, 2) void packed_dkdv_kernel(PackedBwdParams p) {
+  constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
+  constexpr bool TAIL = D % 32 != 0;
+  static_assert(16 * VL <= D, "the V fragments in LDS have no columns past D");
+  using LD = KeyTileLds<D, NWK, QG, BM, VL>;
+  constexpr int TE = LD::TE, RT = LD::RT;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[LD::BYTES];
+  bf16_t(*Qs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);
+  bf16_t(*Os)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds + 4 * TE);
+  float(*lse_s)[RT] = reinterpret_cast<float(*)[RT]>(lds + 8 * TE);
+  float(*dlt_s)[RT] = reinterpret_cast<float(*)[RT]>(lds + 8 * TE + 8 * RT);
+  bf16_t* Vs = reinterpret_cast<bf16_t*>(lds + LD::STAGES);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kw = wave % NWK, qg = wave / NWK, gq = qg * BM;
+  int hk;
+  PackedItem it;
+  if (!work_item(p.list_k, p.Hkv, hk, it)) return;
+  const int G = p.G, R = it.nq * G, n = it.nk, L = p.L;
+  const int k0 = it.tile * BN, key = k0 + kw * 32 + (lane & 31);
+  f32x16 dk[DB], dv[DB];
+  f32x4 tail[4] = {zero4(), zero4(), zero4(), zero4()};  // (TAIL) dV^T, dK^T of keys 0..15 and 16..31
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dk[db] = dv[db] = zero16();
+
+  if (it.beg < it.end) {
+    // the first row that sees this lane's key; from `all` on every row sees every key of the tile
+    const int first = max(0, (int)((unsigned)min(key, n - 1) / (unsigned)L) * L - (n - it.nq)) * G;
+    const int all = max(0, (int)((unsigned)(min(k0 + BN, n) - 1) / (unsigned)L) * L - (n - it.nq)) * G;
+    bf16x8 kf[KK], vf[KK];
+    const bf16_t* vfrag = Vs + (kw * VL * 64 + lane) * 8;
+    auto load_keys = [&] {
+      const long long kr = it.k0 + min(key, n - 1);
+      const bf16_t* ka = p.k + hk * p.sk.h + kr * p.sk.t + 8 * (lane >> 5);
+      const bf16_t* va = p.v + hk * p.sv.h + kr * p.sv.t + 8 * (lane >> 5);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
+          kf[kk] = *reinterpret_cast<const bf16x8*>(ka + 16 * kk);
+          vf[kk] = *reinterpret_cast<const bf16x8*>(va + 16 * kk);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) kf[kk][j] = vf[kk][j] = (__bf16)0.f;
+        }
+        if (kk < VL && qg == 0) *reinterpret_cast<bf16x8*>(Vs + ((kw * VL + kk) * 64 + lane) * 8) = vf[kk];
+      }
+    };
+    const FragOffsets<D> fo(lane, gq * D);
+    const Tail72 ft(lane, gq * D);
+    const GroupOffsets<D, BS, NT> go_q(p.sq, G, tid), go_o(p.sdo, G, tid);
+    const long long row_base = ((long long)hk * p.total_q + it.q0) * G;
+    const float* lse2 = p.lse2 + row_base;
+    const float* dlt = p.delta + row_base;
+    const int beg = it.beg * BS, end = min(R, it.end * BS);
+    auto stage = [&](int r0, int buf) {  // rows behind the sequence's last one repeat it
+      if (p.grouped && r0 + BS <= R) {
+        const long long t = it.q0 + (G == 1 ? r0 : r0 / G);
+        go_q.stage(Qs[buf], p.q + (long long)hk * G * p.sq.h + t * p.sq.t, tid);
+        go_o.stage(Os[buf], p.d_o + (long long)hk * G * p.sdo.h + t * p.sdo.t, tid);
+      } else {
+        stage_rows_direct<D, BS, NT>(Qs[buf], [&](int r) { return p.q + packed_offset(p.sq, hk, G, it.q0, min(r0 + r, R - 1)); },
+                                     tid);
+        stage_rows_direct<D, BS, NT>(Os[buf],
+                                     [&](int r) { return p.d_o + packed_offset(p.sdo, hk, G, it.q0, min(r0 + r, R - 1)); }, tid);
+      }
+#pragma unroll
+      for (int c = wave; c < 2 * (RT / 64); c += NW) {
+        const int part = c % (RT / 64);
+        if (c < RT / 64) {
+          stage_f32x64_direct(lse_s[buf] + 64 * part, lse2, r0 + 64 * part, R, lane);
+        } else {
+          stage_f32x64_direct(dlt_s[buf] + 64 * part, dlt, r0 + 64 * part, R, lane);
+        }
+      }
+    };
+    const float c = p.scale_log2;
+    constexpr bool PRIO = !TAIL;  // matrix phases go first
+    auto step = [&](auto masked, int r0, int buf) {
+#pragma unroll
+      for (int qb = 0; qb < BM / 32; ++qb) {
+        // the dP products start from -Delta of their rows
+        f32x16 s = zero16(), dp;
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 d4 = *reinterpret_cast<const f32x4*>(&dlt_s[buf][gq + qb * 32 + 8 * g + 4 * (lane >> 5)]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dp[4 * g + j] = d4[j];
+        }
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = mfma32(fo.row8(Qs[buf], qb * 32, kk), kf[kk], s);
+          const bf16x8 vk = kk < VL ? *reinterpret_cast<const bf16x8*>(vfrag + kk * 512) : vf[kk];
+          dp = mfma32(fo.row8(Os[buf], qb * 32, kk), vk, dp);
+        }
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int rr = gq + qb * 32 + 8 * g + 4 * (lane >> 5);
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(&lse_s[buf][rr]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 4 * g + j;
+            float pv = fast_exp2(fmaf(s[i], c, -l4[j]));
+            if constexpr (decltype(masked)::value) pv = ((r0 + rr + j >= first) & (r0 + rr + j < R)) ? pv : 0.f;
+            s[i] = pv;
+            dp[i] *= pv;
+          }
+        }
+        // P, then dS, to the matrix products in bf16
+        bf16x8 h[2] = {pack8(s, 0), pack8(s, 1)};
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) dv[db] = mfma32(fo.tr8(Os[buf], qb * 32, t, db), h[t], dv[db]);
+        if constexpr (TAIL) {
+          tail_operands(h[0], h[1]);
+          const bf16x8 x = ft.read(Os[buf], qb * 32);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) tail[e] = mfma16(x, h[e], tail[e]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          h[t] = pack8(dp, t);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) dk[db] = mfma32(fo.tr8(Qs[buf], qb * 32, t, db), h[t], dk[db]);
+        }
+        if constexpr (TAIL) {
+          tail_operands(h[0], h[1]);
+          const bf16x8 x = ft.read(Qs[buf], qb * 32);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) tail[2 + e] = mfma16(x, h[e], tail[2 + e]);
+        }
+      }
+    };
+    stage(beg, 0);  // ahead of the keys, whose V fragments are waited for on their way into LDS
+    load_keys();
+    wait_vmem();
+    __syncthreads();
+    int buf = 0, r0 = beg;
+    auto run = [&](auto masked, int stop) {
+      for (; r0 < stop; r0 += BS) {
+        if (r0 + BS < end) stage(r0 + BS, buf ^ 1);
+        if (k0 + kw * 32 < n) step(masked, r0, buf);
+        if constexpr (PRIO) __builtin_amdgcn_s_setprio(0);
+        wait_vmem();
+        __syncthreads();
+        buf ^= 1;
+      }
+    };
+    run(std::true_type{}, min(end, (all + BS - 1) / BS * BS));
+    run(std::false_type{}, min(end, R / BS * BS));
+    run(std::true_type{}, end);
+  }
+
+  if constexpr (QG > 1) {
+    float* m = reinterpret_cast<float*>(lds);
+    add_groups<QG, NWK>(dv, qg, kw, lane, m);
+    add_groups<QG, NWK>(dk, qg, kw, lane, m);
+    if constexpr (TAIL) {
+      f32x16 rest[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) rest[0][i] = tail[i / 4][i % 4];
+      add_groups<QG, NWK>(rest, qg, kw, lane, m);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tail[i / 4][i % 4] = rest[0][i];
+    }
+    if (qg > 0) return;  // no barrier follows
+  }
+  if (it.slot >= 0) {
+    constexpr int HALF = BN * D;
+    float* pk = p.part_k + ((long long)it.slot * p.Hkv + hk) * 2 * HALF;  // dK; dV behind it
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int kr = kw * 32 + 16 * e + (lane & 15);
+        if (lane < 32 && k0 + kr < n) {
+          float* x = pk + kr * D + 64 + 4 * (lane >> 4);
+          *reinterpret_cast<f32x4*>(x) = tail[2 + e];
+          *reinterpret_cast<f32x4*>(x + HALF) = tail[e];
+        }
+      }
+    }
+    if (key >= n) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 wk, wv;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          wk[j] = dk[db][4 * g + j];
+          wv[j] = dv[db][4 * g + j];
+        }
+        float* x = pk + (key - k0) * D + db * 32 + 8 * g + 4 * (lane >> 5);
+        *reinterpret_cast<f32x4*>(x) = wk;
+        *reinterpret_cast<f32x4*>(x + HALF) = wv;
+      }
+    return;
+  }
+  if constexpr (TAIL) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int kr = k0 + kw * 32 + 16 * e + (lane & 15), col = 64 + 4 * (lane >> 4);
+      if (lane < 32 && kr < n) {
+        bf16x4 wk, wv;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          wk[j] = to_bf16(tail[2 + e][j] * p.scale);
+          wv[j] = to_bf16(tail[e][j]);
+        }
+        *reinterpret_cast<bf16x4*>(p.dk + hk * p.sdk.h + (long long)(it.k0 + kr) * p.sdk.t + col) = wk;
+        *reinterpret_cast<bf16x4*>(p.dv + hk * p.sdv.h + (long long)(it.k0 + kr) * p.sdv.t + col) = wv;
+      }
+    }
+  }
+  if (key >= n) return;
+  bf16_t* dkr = p.dk + hk * p.sdk.h + (long long)(it.k0 + key) * p.sdk.t;
+  bf16_t* dvr = p.dv + hk * p.sdv.h + (long long)(it.k0 + key) * p.sdv.t;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      bf16x4 wk, wv;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        wk[j] = to_bf16(dk[db][4 * g + j] * p.scale);
+        wv[j] = to_bf16(dv[db][4 * g + j]);
+      }
+      const int col = db * 32 + 8 * g + 4 * (lane >> 5);
+      *reinterpret_cast<bf16x4*>(dkr + col) = wk;
+      *reinterpret_cast<bf16x4*>(dvr + col) = wv;
+    }
+}
+
+// dQ: NW waves of 32 rows each (Q and dO fragments, dQ^T in registers), walking the keys, BN a step.
+template <int D, int NW, int BN, int WPS>
+__global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams p) {
+  constexpr int BM = 32 * NW, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
+  constexpr bool TAIL = D % 32 != 0;
+  constexpr int TE = stage_elems<D, BN, NT>();
+  __shared__ __attribute__((aligned(16))) bf16_t lds[2][2][TE];
+  bf16_t(*Ks)[TE] = lds[0];
+  bf16_t(*Vs)[TE] = lds[1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int hk;
+  PackedItem it;
+  if (!work_item(p.list_q, p.Hkv, hk, it)) return;
+  const int G = p.G, R = it.nq * G, n = it.nk, r0 = it.tile * BM;
+  const int row = r0 + wave * 32 + (lane & 31), rc = min(row, R - 1);
+  // This row's Q, dO and O, asked for before anything that waits: their latencies then pass together.
+  bf16x8 qf[KK], of[KK], y[KK];
+  {
+    const bf16_t* qa = p.q + packed_offset(p.sq, hk, G, it.q0, rc) + 8 * (lane >> 5);
+    const bf16_t* da = p.d_o + packed_offset(p.sdo, hk, G, it.q0, rc) + 8 * (lane >> 5);
+    const bf16_t* oa = p.o + packed_offset(p.so, hk, G, it.q0, rc) + 8 * (lane >> 5);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
+        of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
+        y[kk] = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
+        qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = y[kk][j] = (__bf16)0.f;
+      }
+    }
+  }
+  const int row_t = rc / G;
+  const float lse = p.lse[(long long)(hk * G + (rc - row_t * G)) * p.total_q + it.q0 + row_t];
+  const int hi = sees(rc, G, it.nq, n, p.L), hi_all = sees(r0, G, it.nq, n, p.L);
+  f32x16 dq[DB];
+  f32x4 tail[2] = {zero4(), zero4()};
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dq[db] = zero16();
+  const bf16_t* k0p = p.k + (long long)it.k0 * p.sk.t + hk * p.sk.h;
+  const bf16_t* v0p = p.v + (long long)it.k0 * p.sv.t + hk * p.sv.h;
+  const FragOffsets<D> fo(lane, 0);
+  const Tail72 ft(lane, 0);
+  const RowOffsets<D, BN, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
+  auto stage = [&](int i, int buf) {  // keys behind the sequence's last one repeat it
+    const long long k0 = (long long)i * BN;
+    if (k0 + BN <= n) {
+      stage_rows_s<D, BN, NT>(Ks[buf], k0p + k0 * p.sk.t, ro_k, tid);
+      stage_rows_s<D, BN, NT>(Vs[buf], v0p + k0 * p.sv.t, ro_v, tid);
+    } else {
+      stage_kv_rows_direct<D, BN, NT>(Ks[buf], Vs[buf], [&](int r) -> RowPair {
+        const long long j = min(k0 + r, (long long)n - 1);
+        return {k0p + j * p.sk.t, v0p + j * p.sv.t};
+      }, tid);
+    }
+  };
+  if (it.beg < it.end) stage(it.beg, 0);
+  float dot = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[kk][j], dot);
+  float ndlt = -sum_halves(dot);
+  const float c = p.scale_log2, lse2 = lse * 1.4426950408889634f;
+  wait_vmem();
+  __syncthreads();
+  // Rows of few keys: Delta = sum_j P_j dP_j of the probabilities at hand.  rowsum(dO O) has O's rounding to bf16, which
+  // next to few keys' dP - Delta is not small (cross_dq_kernel); a tile whose first row sees at most a step of
+  // keys is walked twice.
+  if (hi_all <= BN && it.slot < 0 && it.beg < it.end) {
+    float sum = 0.f;
+    for (int i = it.beg; i < it.end; ++i) {
+      if (i > it.beg) {
+        stage(i, 0);
+        wait_vmem();
+        __syncthreads();
+      }
+#pragma unroll 1
+      for (int kq = 0; kq < BN / 32; ++kq) {
+        f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = mfma32(fo.row8(Ks[0], kq * 32, kk), qf[kk], s);
+          dp = mfma32(fo.row8(Vs[0], kq * 32, kk), of[kk], dp);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const bool in = i * BN + kq * 32 + acc_row(j, lane) < hi;
+          sum = fmaf(in ? fast_exp2(fmaf(s[j], c, -lse2)) : 0.f, in ? dp[j] : 0.f, sum);
+        }
+      }
+      __syncthreads();  // (the stage is written again)
+    }
+    ndlt = -sum_halves(sum);
+    if (it.end - it.beg > 1) {
+      stage(it.beg, 0);
+      wait_vmem();
+      __syncthreads();
+    }
+  }
+  if (it.beg == 0 && lane < 32 && row < R) {
+    const long long at = ((long long)hk * p.total_q + it.q0) * G + row;
+    p.delta[at] = ndlt;
+    p.lse2[at] = lse2;
+  }
+  if (it.beg < it.end) {
+    f32x16 nd;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) nd[i] = ndlt;
+    auto step = [&](auto masked, int k0, int buf) {
+#pragma unroll
+      for (int kq = 0; kq < BN / 32; ++kq) {
+        f32x16 s = zero16(), dp = nd;
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          s = mfma32(fo.row8(Ks[buf], kq * 32, kk), qf[kk], s);
+          dp = mfma32(fo.row8(Vs[buf], kq * 32, kk), of[kk], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float pv = fast_exp2(fmaf(s[i], c, -lse2));
+          if constexpr (decltype(masked)::value) pv = k0 + kq * 32 + acc_row(i, lane) < hi ? pv : 0.f;
+          dp[i] *= pv;
+        }
+        bf16x8 h[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          h[t] = pack8(dp, t);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) dq[db] = mfma32(fo.tr8(Ks[buf], kq * 32, t, db), h[t], dq[db]);
+        }
+        if constexpr (TAIL) {
+          const bf16x8 x = ft.read(Ks[buf], kq * 32);
+          tail_operands(h[0], h[1]);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) tail[e] = mfma16(x, h[e], tail[e]);
+        }
+      }
+    };
+    int buf = 0, i = it.beg;
+    auto run = [&](auto masked, int stop) {
+      for (; i < stop; ++i) {
+        if (i + 1 < it.end) stage(i + 1, buf ^ 1);
+        step(masked, i * BN, buf);
+        wait_vmem();
+        __syncthreads();
+        buf ^= 1;
+      }
+    };
+    run(std::false_type{}, min(hi_all / BN, it.end));
+    run(std::true_type{}, it.end);
+  }
+  if (it.slot >= 0) {  // fp32 dQ of this range of the keys
+    float* part = p.part_q + (((long long)it.slot * p.Hkv + hk) * BM + wave * 32) * D;
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 16 * e + (lane & 15);
+        if (lane < 32 && r0 + wave * 32 + r < R) *reinterpret_cast<f32x4*>(part + r * D + 64 + 4 * (lane >> 4)) = tail[e];
+      }
+    }
+    if (row >= R) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = dq[db][4 * g + j];
+        *reinterpret_cast<f32x4*>(part + (lane & 31) * D + db * 32 + 8 * g + 4 * (lane >> 5)) = w;
+      }
+    return;
+  }
+  // (every wave has passed the last barrier: a half stage holds the rows of BN / 32 waves)
+  static_assert(NW <= 2 * (BN / 32), "one stage holds the rows of every wave");
+  const int half = wave / (BN / 32);
+  store_rows<D>(dq, tail, (half ? Vs : Ks)[0] + (wave - half * (BN / 32)) * 32 * D, min(32, R - r0 - wave * 32), lane, p.scale,
+                [&](int r) { return p.dq + packed_offset(p.sdq, hk, G, it.q0, r0 + wave * 32 + r); });
+}
+
+// Sums of the parts of cut tiles, in order: the first n_kv workgroups dK and dV, the others dQ.  One thread for four
+// columns of a row.
+template <int D, int BM, int BN>
+__global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p, int n_kv) {
+  constexpr int TPR = D / 4, PER_K = BN * TPR / 256, PER_Q = BM * TPR / 256;
+  if ((int)blockIdx.x < n_kv) {
+    const int job = blockIdx.x / PER_K, j = job / p.Hkv, hk = job - j * p.Hkv;
+    if (j >= p.list_k[1]) return;
+    const PackedJoin it = p.joins_k[j];
+    const int x = (blockIdx.x - job * PER_K) * 256 + threadIdx.x, kr = x / TPR, col = (x - kr * TPR) * 4;
+    const int key = it.tile * BN + kr;
+    if (key >= it.nk) return;
+    f32x4 k = zero4(), v = zero4();
+#pragma unroll 4
+    for (int s = 0; s < it.parts; ++s) {
+      const float* y = p.part_k + ((long long)(it.first + s) * p.Hkv + hk) * 2 * BN * D + kr * D + col;
+      k += *reinterpret_cast<const f32x4*>(y);
+      v += *reinterpret_cast<const f32x4*>(y + BN * D);
+    }
+    bf16x4 wk, wv;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      wk[c] = to_bf16(k[c] * p.scale);
+      wv[c] = to_bf16(v[c]);
+    }
+    *reinterpret_cast<bf16x4*>(p.dk + hk * p.sdk.h + (long long)(it.k0 + key) * p.sdk.t + col) = wk;
+    *reinterpret_cast<bf16x4*>(p.dv + hk * p.sdv.h + (long long)(it.k0 + key) * p.sdv.t + col) = wv;
+    return;
+  }
+  const int b = blockIdx.x - n_kv, job = b / PER_Q, j = job / p.Hkv, hk = job - j * p.Hkv;
+  if (j >= p.list_q[1]) return;
+  const PackedJoin it = p.joins_q[j];
+  const int x = (b - job * PER_Q) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
+  const int row = it.tile * BM + rt;
+  if (row >= it.nq * p.G) return;
+  f32x4 q = zero4();
+#pragma unroll 4
+  for (int s = 0; s < it.parts; ++s)
+    q += *reinterpret_cast<const f32x4*>(p.part_q + (((long long)(it.first + s) * p.Hkv + hk) * BM + rt) * D + col);
+  bf16x4 w;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) w[c] = to_bf16(q[c] * p.scale);
+  *reinterpret_cast<bf16x4*>(p.dq + packed_offset(p.sdq, hk, p.G, it.q0, row) + col) = w;
+}
+
+}  // namespace
+
+#define MW_CAT_(a, b) a##b
+#define MW_CAT(a, b) MW_CAT_(a, b)
+hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
+  constexpr int NW = 4, BN = 128;
+  if (s.dq.tile != 32 * NW || s.dq.step != 64 || s.dkv.tile != BN || s.dkv.step != 64) return hipErrorInvalidValue;
+  const long long grid_q = (long long)s.dq.max_items * s.Hkv, grid_k = (long long)s.dkv.max_items * s.Hkv;
+  const long long n_kv = (long long)s.dkv.max_joins * s.Hkv * (BN * (kD / 4) / 256);
+  const long long n_q = (long long)s.dq.max_joins * s.Hkv * (32 * NW * (kD / 4) / 256);
+  if (grid_q > 0x7fffffffLL || grid_k > 0x7fffffffLL || n_kv + n_q > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((packed_dq_kernel<kD, NW, 64, kD == 128 ? 2 : 3>), dim3((unsigned)grid_q), dim3(64 * NW), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((packed_dkdv_kernel<kD, 4, 2, 32, kD == 128 ? 6 : 0>), dim3((unsigned)grid_k), dim3(512), 0, stream, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || n_kv + n_q == 0) return e;
+  hipLaunchKernelGGL((packed_bwd_join_kernel<kD, 32 * NW, BN>), dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);
+  return hipGetLastError();
+}
+
+}  // namespace mw

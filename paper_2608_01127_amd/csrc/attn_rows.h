@@ -426,6 +426,43 @@ struct CodeTile {
   }
 };
 
+// LDS of a dK/dV kernel (NWK key waves in QG row groups of BM rows a step): Q and dO tiles of BS rows, LSE and -Delta of those rows (two stages each), then VL V
+// fragments of each key wave.
+template <int D, int NWK, int QG, int BM, int VL>
+struct KeyTileLds {
+  static constexpr int NT = 64 * NWK * QG, BS = BM * QG;
+  static constexpr int TE = stage_elems<D, BS, NT>();
+  static constexpr int RT = BS < 64 ? 64 : BS;
+  static constexpr int STAGES = 2 * 2 * TE * 2 + 2 * 2 * RT * 4;
+  static constexpr int MERGE = QG == 1 ? 0 : (QG / 2) * NWK * (D / 32 + (D % 32 != 0)) * 16 * 64 * 4;
+  static constexpr int BYTES = STAGES + NWK * VL * 1024 > MERGE ? STAGES + NWK * VL * 1024 : MERGE;
+};
+
+// Sum of the row groups' tiles in group 0, through LDS: in each round the upper half of the groups hands its tiles
+// to the lower half (a fixed order).  Every wave calls it after the last read of `x`.
+template <int G, int NWK, int N>
+__device__ __forceinline__ void add_groups(f32x16 (&acc)[N], int group, int slot, int lane, float* x) {
+#pragma unroll
+  for (int half = G / 2; half >= 1; half >>= 1) {
+    __syncthreads();
+    if (group >= half && group < 2 * half) {
+      float* y = x + ((group - half) * NWK + slot) * N * 1024 + lane;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[(n * 16 + i) * 64] = acc[n][i];
+    }
+    __syncthreads();
+    if (group < half) {
+      const float* y = x + (group * NWK + slot) * N * 1024 + lane;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[n][i] += y[(n * 16 + i) * 64];
+    }
+  }
+}
+
 // NW waves in KG key groups of NW / KG waves of 32 rows each; a step stages KG * BN keys,
 // of which a group takes its BN.  WPS: waves per SIMD the registers are allocated for.
 // Bound by a SIMD's two or three waves: over long keys the matrix units are busy 40 to 53% of the time, and waves at work

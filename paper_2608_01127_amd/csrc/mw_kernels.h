@@ -399,6 +399,108 @@ hipError_t launch_cross_bwd_64(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_72(const CrossBwdParams& p, hipStream_t stream);
 hipError_t launch_cross_bwd_128(const CrossBwdParams& p, hipStream_t stream);
 
+// ---------------------------------------------------------------------------
+// Attention of packed sequences (packed_plan.hip, attn_packed.hip): sequence s is tokens cu_q[s] .. cu_q[s + 1] of the
+// queries and cu_k[s] .. cu_k[s + 1] of the keys, both in device memory.  The rows of a key head are the tokens of its G
+// query heads: row r of a sequence is token r / G of query head hk G + r % G.
+// ---------------------------------------------------------------------------
+// One workgroup's work for a key head: tile `tile` of a sequence over steps [beg, end): row tiles step over keys, key tiles
+// over rows.  slot >= 0: the tile is cut into several items, which leave partial results in that place.
+struct PackedItem {
+  int q0, nq, k0, nk, tile, beg, end, slot;
+};
+// A cut tile: its partial results are slots [first, first + parts), in order.
+struct PackedJoin {
+  int q0, nq, k0, nk, tile, first, parts, unused;
+};
+// The plan of a pass: a head of 8 words (items, cut tiles, slots), then its items, heaviest first, then its cut tiles.
+struct PackedList {
+  bool keys;              // key tiles (dK, dV), or row tiles
+  int tile, step;         // rows and keys of a tile and a step, or keys and rows
+  int min_steps;          // no item of a cut tile is much shorter
+  int share;              // workgroups that one head's steps are divided among before a tile is cut
+  int max_tiles, max_items, max_slots, max_joins;
+  long long at;           // word of the plan where it begins
+  long long words() const { return 8 + 8LL * (max_items + max_joins); }
+};
+struct PackedShape {
+  int N, G, Hkv, D, L, total_q, total_k, n_lists;
+  PackedList fwd, dq, dkv;
+  long long words;        // of the plan: the lists, then N + 1 words of scratch for each
+};
+PackedShape packed_shape(int N, int H, int Hkv, int D, int L, int total_q, int total_k, bool backward);
+hipError_t launch_packed_plan(const PackedShape& s, const int* cu_q, const int* cu_k, int* plan, hipStream_t stream);
+
+struct PackedParams {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* o;
+  float* lse;  // [H, total_q]
+  Strides sq, sk, sv, so;  // [total, heads, D] views (b unused)
+  int Hkv, G, L, total_q;
+  const int* list;
+  const PackedJoin* joins;
+  float* part;  // [slots][Hkv][tile][D] unnormalised O, then [slots][Hkv][tile][2] (m, l)
+  int max_slots;
+  float scale_log2;
+};
+size_t packed_part_bytes(const PackedShape& s);
+hipError_t launch_packed_fwd_64(const PackedParams& p, const PackedList& list, hipStream_t stream);
+hipError_t launch_packed_fwd_72(const PackedParams& p, const PackedList& list, hipStream_t stream);
+hipError_t launch_packed_fwd_128(const PackedParams& p, const PackedList& list, hipStream_t stream);
+
+struct PackedBwdParams {
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const uint16_t* o;
+  const uint16_t* d_o;
+  const float* lse;  // [H, total_q]
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  float* delta;  // [Hkv][total_q G]: -rowsum(dO O)
+  float* lse2;   // [Hkv][total_q G]: LSE log2 e
+  Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  int Hkv, G, L, total_q;
+  bool grouped;  // a step's rows lie at fixed offsets from its first one (G divides a step and they fit 32 bits)
+  const int* list_q;
+  const int* list_k;
+  const PackedJoin* joins_q;
+  const PackedJoin* joins_k;
+  float* part_q;  // [slots][Hkv][tile][D] fp32 dQ
+  float* part_k;  // [slots][Hkv][2][tile][D] fp32 dK, dV
+  float scale, scale_log2;
+};
+hipError_t launch_packed_bwd_64(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream);
+hipError_t launch_packed_bwd_72(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream);
+hipError_t launch_packed_bwd_128(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream);
+
+// Rotary positions (rope.hip): rows of q, then of k, of B * T tokens.
+constexpr int kRopePairs = 64, kRopeTableMax = 1024;
+constexpr int kRopeAlone = 255;  // no pair
+struct RopeArgs {
+  const uint16_t* q;
+  const uint16_t* k;
+  uint16_t* q_out;
+  uint16_t* k_out;
+  Strides sq, sk, sqo, sko;
+  int B, H, Hkv, T;  // Hkv = 0: no k
+  int tokens;        // of a workgroup (set by the launcher)
+  const void* pos;   // device integers of 4 or 8 bytes, or null: first + t
+  bool pos64;
+  long long pos_axis, pos_b, pos_t, first;
+  float gain, gain_sin;  // factors of the cosine and of the sine (negative: the inverse rotation)
+  int n_pairs, units;    // pieces of a row that a thread takes at a time
+  double freq[kRopePairs];  // turns per position
+  uint8_t axis[kRopePairs];
+  // halves: first dimension of a piece, that of its partners (kRopeAlone: none) and its first pair; interleaved: pair[i],
+  // the pair that dimensions 2 i and 2 i + 1 are (kRopeAlone: none)
+  uint8_t at_a[128], at_b[128], pair[128];
+};
+hipError_t launch_rope(RopeArgs a, bool halves, int width, hipStream_t stream);
+
 // Page operations (kvpages.hip).  What the host has decided travels in the kernels' arguments.
 struct PagePool {
   uint8_t* k_pages;
@@ -440,6 +542,45 @@ struct SeqArgs {
 hipError_t launch_pages_clear(const PagePool& c, const SeqArgs& a, hipStream_t stream);
 // Entries from first + n on of a row move to `first`; its length becomes `len`.
 hipError_t launch_pages_evict(const PagePool& c, int seq, int first, int n, int used, int len, hipStream_t stream);
+
+// Eviction by weight (weigh.hip, keep.hip).  Sum of the rows' attention weights of each cached token.
+struct WeighParams {
+  const uint16_t* q;   // [B, Hkv G, T, D]
+  const float* lse;    // [B, Hkv G, T]
+  const uint8_t* k_pages;
+  const float* k_scales;
+  const int* table;
+  const int* lens;
+  float* weights;      // [N, W L]
+  float* part;         // n_parts > 1: [n_parts][blocks][64]
+  Strides sq;
+  int B, Hkv, G, T, R, L, W, per_page, n_parts;
+  bool add;
+  float scale_log2;
+};
+struct WeighSeqs {
+  int seq[kMaxSeqs];
+  int first[kMaxSeqs + 1];  // number of the first block of 64 tokens of each member, then of all
+};
+int weigh_parts(int Hkv, int R, long long blocks);
+hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipStream_t stream);
+// Sequences of which `keep` tokens stay: the `first` ones, the `recent` last ones and the heaviest others.
+struct KeepArgs {
+  int n_jobs, keep, first, recent;
+  int seq[kMaxSeqs], len[kMaxSeqs];
+};
+// Which tokens, as (page, token of the page), and their weights: [n_jobs][keep - first / L * L].
+hipError_t launch_keep_select(const PagePool& c, const KeepArgs& a, const float* weights, int2* list, float* kept,
+                              hipStream_t stream);
+// Runs of whole pages of the new sequences: places [first, first + n_tok) into pages[page0..].
+constexpr int kKeepRuns = 32, kKeepPages = 512;
+struct KeepRun {
+  int n_runs, keep, from, stride;  // the lists begin at place `from` and are `stride` apart
+  int seq[kKeepRuns], job[kKeepRuns], len[kKeepRuns], first[kKeepRuns], n_tok[kKeepRuns], page0[kKeepRuns], last[kKeepRuns];
+  int pages[kKeepPages];
+};
+hipError_t launch_keep_gather(const PagePool& c, const KeepRun& a, float* weights, const int2* list, const float* kept,
+                              hipStream_t stream);
 
 // Record the calling thread's status message (what mw_last_error returns)
 // and return `code`; MW_OK clears it.

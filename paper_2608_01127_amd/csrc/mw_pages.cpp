@@ -406,6 +406,188 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream) {
 }
 
 // ---------------------------------------------------------------------------
+// Eviction by accumulated attention weight.
+// ---------------------------------------------------------------------------
+
+static int check_weigh(const char* fn, const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T) {
+  int st = check_pages(fn, c);
+  if (!st) st = check_seqs(fn, c, seqs, n_seqs, true);
+  if (st) return st;
+  if (H < 1 || H % c->H) return fail(MW_EINVAL, "%s: %d query heads are no multiple of the cache's %d", fn, H, c->H);
+  if (H > (1 << 14)) return fail(MW_EUNSUPPORTED, "%s: H too large", fn);
+  if (T < 1) return fail(MW_EINVAL, "%s: T must be >= 1", fn);
+  if ((long long)T * (H / c->H) > kMaxT) return fail(MW_EUNSUPPORTED, "%s: too many tokens", fn);
+  if ((long long)T * H > (1LL << 30)) return fail(MW_EUNSUPPORTED, "%s: T * H is too large", fn);
+  return MW_OK;
+}
+
+static int weigh_blocks(const mw_kvpages* c, const int32_t* seqs, int n_seqs, WeighSeqs* out) {
+  const Book b = book(c);
+  long long n = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (out != nullptr) {
+      out->seq[i] = seqs[i];
+      out->first[i] = (int)n;
+    }
+    n += (b.lens[seqs[i]] + MW_PAGE_BLOCK - 1) / MW_PAGE_BLOCK;
+  }
+  if (out != nullptr) out->first[n_seqs] = (int)n;
+  return (int)n;  // at most 256 * 2^24 / 64
+}
+
+size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T) {
+  if (check_weigh("mw_kvpages_weigh_workspace_size", c, seqs, n_seqs, H, T)) return 0;
+  const int n = weigh_blocks(c, seqs, n_seqs, nullptr), parts = weigh_parts(c->H, T * (H / c->H), n);
+  return parts > 1 ? (size_t)parts * n * MW_PAGE_BLOCK * sizeof(float) : 0;
+}
+
+int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const void* q, const float* lse, int H, int T,
+                     float* weights, int add, float scale, void* workspace, size_t workspace_bytes, const mw_strides* strides,
+                     mw_stream_t stream) {
+  const char* fn = "mw_kvpages_weigh";
+  int st = check_weigh(fn, c, seqs, n_seqs, H, T);
+  if (!st) st = check_ptrs(fn, {{"q", q}, {"lse", lse}, {"weights", weights}});
+  if (!st) st = check_not_captured(fn, stream);
+  if (st) return st;
+  if (!aligned16(workspace)) return fail(MW_EALIGN, "%s: workspace is not 16-byte aligned", fn);
+  if (add != 0 && add != 1) return fail(MW_EINVAL, "%s: add must be 0 or 1", fn);
+  if (!good_scale(scale)) return fail(MW_EINVAL, "%s: scale must be finite and > 0", fn);
+  Strides sq = contiguous(H, T, c->D);
+  if (strides != nullptr) {
+    st = check_view(fn, "q", strides[0], n_seqs, H, T, c->D, false);
+    if (st) return st;
+    sq = to_internal(strides[0]);
+  }
+  WeighSeqs s{};
+  const int blocks = weigh_blocks(c, seqs, n_seqs, &s);
+  WeighParams p{};
+  p.n_parts = weigh_parts(c->H, T * (H / c->H), blocks);
+  const size_t need = p.n_parts > 1 ? (size_t)p.n_parts * blocks * MW_PAGE_BLOCK * sizeof(float) : 0;
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p.n_parts = 1;
+  p.q = static_cast<const uint16_t*>(q);
+  p.lse = lse;
+  const PagePool pool = pool_of(c);
+  p.k_pages = pool.k_pages;
+  p.k_scales = pool.k_scales;
+  p.table = pool.table;
+  p.lens = pool.lens;
+  p.weights = weights;
+  p.part = static_cast<float*>(workspace);
+  p.sq = sq;
+  p.B = n_seqs;
+  p.Hkv = c->H;
+  p.G = H / c->H;
+  p.T = T;
+  p.R = T * p.G;
+  p.L = c->L;
+  p.W = c->W;
+  p.per_page = c->L / MW_PAGE_BLOCK;
+  p.add = add != 0;
+  p.scale_log2 = scale * kLog2e;
+  return hip_status(fn, launch_weigh(p, s, c->D, static_cast<hipStream_t>(stream)));
+}
+
+// Bytes of the list of places that stay.
+static size_t places_bytes(int n_seqs, int n) { return ((size_t)n_seqs * n * sizeof(int2) + 15) / 16 * 16; }
+
+static int check_keep(const char* fn, const mw_kvpages* c, const int32_t* seqs, int n_seqs, int n_keep, int first) {
+  int st = check_pages(fn, c);
+  if (!st) st = check_seqs(fn, c, seqs, n_seqs, true);
+  if (st) return st;
+  if (n_keep < 1 || first < 0 || first > n_keep)
+    return fail(MW_EINVAL, "%s: n_keep must be >= 1 and first in [0, n_keep] (got %d, %d)", fn, n_keep, first);
+  if ((long long)n_keep > (long long)c->W * c->L)
+    return fail(MW_EINVAL, "%s: n_keep of %d exceeds a row of %d pages", fn, n_keep, c->W);
+  return MW_OK;
+}
+
+size_t mw_kvpages_evict_weighted_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int n_keep, int first) {
+  if (check_keep("mw_kvpages_evict_weighted_workspace_size", c, seqs, n_seqs, n_keep, first)) return 0;
+  const size_t places = (size_t)n_seqs * (n_keep - first / c->L * c->L);
+  return std::max<size_t>(16, places_bytes(n_seqs, n_keep - first / c->L * c->L) + places * sizeof(float));
+}
+
+int mw_kvpages_evict_weighted(mw_kvpages* c, const int32_t* seqs, int n_seqs, float* weights, int n_keep, int first,
+                              int recent, void* workspace, size_t workspace_bytes, mw_stream_t stream) {
+  const char* fn = "mw_kvpages_evict_weighted";
+  int st = check_keep(fn, c, seqs, n_seqs, n_keep, first);
+  if (!st) st = check_ptrs(fn, {{"weights", weights}, {"workspace", workspace}});
+  if (!st) st = check_not_captured(fn, stream);
+  if (st) return st;
+  if (recent < 0 || recent > n_keep - first)
+    return fail(MW_EINVAL, "%s: recent = %d is not in [0, n_keep - first]", fn, recent);
+  const size_t bytes = mw_kvpages_evict_weighted_workspace_size(c, seqs, n_seqs, n_keep, first);
+  if (workspace_bytes < bytes)
+    return fail(MW_EINVAL, "%s: workspace of %zu bytes is smaller than the %zu needed", fn, workspace_bytes, bytes);
+  const Book b = book(c);
+  const int L = c->L, w0 = first / L, w1 = pages_of(c, n_keep), from = w0 * L;
+  KeepArgs a{};
+  a.keep = n_keep;
+  a.first = first;
+  a.recent = recent;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (b.lens[seqs[i]] <= n_keep) continue;  // nothing to drop
+    a.seq[a.n_jobs] = seqs[i];
+    a.len[a.n_jobs++] = b.lens[seqs[i]];
+  }
+  if (a.n_jobs == 0) return ok();
+  const long long need = (long long)a.n_jobs * (w1 - w0);
+  if (need > b.head[2]) return fail(MW_EFULL, "%s: %lld pages are needed and %d are free", fn, need, b.head[2]);
+  int2* list = static_cast<int2*>(workspace);
+  float* kept = reinterpret_cast<float*>(static_cast<char*>(workspace) + places_bytes(n_seqs, n_keep - from));
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  const PagePool pool = pool_of(c);
+  hipError_t e = launch_keep_select(pool, a, weights, list, kept, hs);
+  if (e != hipSuccess) return hip_status(fn, e);
+  // New pages are taken before old ones are given back: no sequence's copy may land on what another one still reads.
+  // They are noted in `moved`, which only a compaction uses, until every launch has succeeded.
+  KeepRun r;
+  r.keep = n_keep;
+  r.from = from;
+  r.stride = n_keep - from;
+  r.n_runs = 0;
+  int n_pages = 0;
+  auto flush = [&]() {
+    if (e == hipSuccess && r.n_runs > 0) e = launch_keep_gather(pool, r, weights, list, kept, hs);
+    r.n_runs = 0;
+    n_pages = 0;
+  };
+  int taken = 0;
+  for (int j = 0; j < a.n_jobs; ++j) {
+    int w = w0;
+    do {
+      if (r.n_runs == kKeepRuns || n_pages == kKeepPages) flush();
+      const int i = r.n_runs++, n = std::min(w1 - w, kKeepPages - n_pages);
+      r.seq[i] = a.seq[j];
+      r.job[i] = j;
+      r.len[i] = a.len[j];
+      r.first[i] = w * L;
+      r.n_tok[i] = std::min(n_keep, (w + n) * L) - w * L;
+      r.page0[i] = n_pages;
+      r.last[i] = w + n == w1;
+      for (int x = 0; x < n; ++x) {
+        const int page = take(c, b);
+        b.moved[taken++] = page;
+        r.pages[n_pages++] = page;
+      }
+      w += n;
+    } while (w < w1);
+  }
+  flush();
+  if (e != hipSuccess) {
+    for (int i = 0; i < taken; ++i) release(b, b.moved[i]);
+    return hip_status(fn, e);
+  }
+  for (int j = 0, at = 0; j < a.n_jobs; ++j) {
+    int32_t* row = row_of(c, b, a.seq[j]);
+    for (int w = w0; w < pages_of(c, a.len[j]); ++w) release(b, row[w]);
+    for (int w = w0; w < w1; ++w) row[w] = b.moved[at++];
+    b.lens[a.seq[j]] = n_keep;
+  }
+  return ok();
+}
+
+// ---------------------------------------------------------------------------
 // Attention over the pages.
 // ---------------------------------------------------------------------------
 

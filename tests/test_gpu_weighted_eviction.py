@@ -1,0 +1,351 @@
+"""Eviction from the paged cache by accumulated attention weight: the weights against 64-bit values, what stays and its
+pages against a model of the cache, and a rollout that uses both."""
+import math
+
+import pytest
+
+from attention_bounds import attention64, check
+from test_gpu_pages import BLOCK, Model, make, randn, tokens
+
+pytestmark = pytest.mark.gpu
+
+
+def weights_of(mw, cache, model, seqs, q, lse, H, **kw):
+    """mw_kvpages_weigh into rows of markers against 64-bit values, within a bound that counts roundings: scores in 32
+    bits (2^-22 of the products' magnitudes), the exponent's sum with the LSE (2^-23 of both), the hardware's 2^x (2^-22), and a
+    sum of at most 64 partial sums, each of n / 64 terms (2^-24 a step)."""
+    import torch
+    d = cache.desc
+    w = torch.full((d.N, d.W * d.L), 3.0, device="cuda")
+    old = kw.pop("old", 0.0)
+    w[seqs] = old
+    mw.mw_kvpages_weigh(cache, seqs, q, lse, w, **kw)
+    torch.cuda.synchronize()
+    sc = kw.get("scale") or 1 / math.sqrt(d.D)
+    G = H // d.H
+    for s in range(d.N):
+        n = model.lens[s]
+        if s not in seqs:
+            assert bool((w[s] == 3).all())
+            continue
+        assert bool((w[s, n:] == old).all())
+        b = seqs.index(s)
+        k = model.values(s)[0]
+        want = torch.zeros(n, dtype=torch.float64, device="cuda")
+        off = torch.zeros_like(want)
+        rows = 0
+        for h in range(H):
+            x = q[b, h].double()
+            l = lse[b, h].double()[:, None]
+            p = torch.exp(torch.where(l == -math.inf, -math.inf, (x @ k[h // G].t()) * sc - torch.where(l == -math.inf, 0.0, l)))
+            size = sc * (x.abs() @ k[h // G].abs().t()) + torch.where(l.isfinite(), l, 0.0).abs()
+            want += p.sum(0)
+            off += (p * (2.0 ** -22 * (1 + 2 * size))).sum(0)
+            rows += x.shape[0]
+        off += 2.0 ** -24 * (rows / 32 + 64) * want + 1e-37
+        if kw.get("add", True):
+            want = want + old
+            off = off + 2.0 ** -24 * want.abs()
+        check(f"weights s={s}", w[s, :n], want, off)
+    return w
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("L", [64, 192])
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (6, 2), (16, 2)])
+def test_weights(mw, D, L, H, Hkv):
+    """One row to several tiles of them, lengths of one, a block's edge and beyond; the call's own LSE, and add."""
+    import torch
+    lens = [1, 63, 64, 200, 450]
+    N, W = 6, 8
+    cache, model = make(mw, 40, Hkv, L, D, N, W)
+    for s, n in enumerate(lens):
+        k, v = tokens((1, Hkv, n, D), 10 + s), tokens((1, Hkv, n, D), 20 + s)
+        k = (k.float() / 16).bfloat16()
+        mw.mw_kvpages_append(cache, [s], k, v)
+        model.append([s], k, v)
+    for T, seqs, layout in ((1, [4, 0, 2], "bhtd"), (33, [3, 1], "bthd"), (7, [0, 1, 2, 3, 4, 5], "bthd")):
+        print(f"[case] weigh D={D} L={L} H={H} Hkv={Hkv} T={T} {seqs}", flush=True)
+        q = randn((len(seqs), H, T, D), 30 + T, layout)
+        kn, vn = randn((len(seqs), Hkv, T, D), 31 + T), randn((len(seqs), Hkv, T, D), 32 + T)
+        _, lse = mw.mw_chunk_attn_paged(q, kn, vn, 1, T, cache, seqs, want_lse=True)
+        weights_of(mw, cache, model, seqs, q, lse, H, add=False)
+        weights_of(mw, cache, model, seqs, q, lse, H, old=0.25)
+        _, alone = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, seqs, want_lse=True)
+        w = weights_of(mw, cache, model, seqs, q, alone, H, add=False)
+        for s in seqs:  # the rows' weights over what they see sum to one: as many as rows
+            if model.lens[s]:
+                assert abs(float(w[s, :model.lens[s]].sum()) - H * T) <= H * T * 2.0 ** -12
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_rows_that_weigh_nothing(mw, D):
+    """An LSE of -inf (a row that saw nothing) or +inf."""
+    import torch
+    cache, model = make(mw, 8, 2, 64, D, 2, 4)
+    k, v = randn((1, 2, 100, D), 1), randn((1, 2, 100, D), 2)
+    mw.mw_kvpages_append(cache, [1], k, v)
+    model.append([1], k, v)
+    q = randn((1, 4, 40, D), 3)
+    lse = torch.randn(1, 4, 40, device="cuda") + 5
+    lse[0, 1] = -math.inf
+    lse[0, 2, ::3] = -math.inf
+    lse[0, 3, 5] = math.inf
+    weights_of(mw, cache, model, [1], q, lse, 4, add=False)
+    weights_of(mw, cache, model, [1], q, lse, 4, add=False, scale=0.5)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("n", [70, 3000])
+def test_many_rows_are_divided(mw, D, n):
+    """Rows of a call divided among workgroups, and not (no workspace of that size); two members of unlike lengths."""
+    import torch
+    H, Hkv, T = 8, 4, 700
+    cache, model = make(mw, 120, Hkv, 64, D, 2, 50)
+    for s, m in enumerate((n, max(1, n // 3))):
+        k, v = randn((1, Hkv, m, D), 40 + s), randn((1, Hkv, m, D), 50 + s)
+        mw.mw_kvpages_append(cache, [s], k, v)
+        model.append([s], k, v)
+    q = randn((2, H, T, D), 60, "bthd")
+    assert mw.mw_kvpages_weigh_workspace_size(cache, [0, 1], H, T) > 0
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, [0, 1], want_lse=True)
+    a = weights_of(mw, cache, model, [0, 1], q, lse, H, add=False)
+    b = weights_of(mw, cache, model, [1, 0], q.flip(0), lse.flip(0).contiguous(), H, add=False,
+                   workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    again = weights_of(mw, cache, model, [0, 1], q, lse, H, add=False)
+    assert torch.equal(a, again)
+
+
+def kept(w, n, keep, first, recent):
+    """Places that stay, in order (ties: lowest index; a NaN is the lightest)."""
+    w = [(-math.inf if x != x else x) for x in w[:n]]
+    nan = [x != x for x in w]
+    mid = sorted(range(first, n - recent), key=lambda j: (-w[j], j))[:keep - first - recent]
+    return sorted([*range(first), *mid, *range(n - recent, n)])
+
+
+def evict(mw, cache, model, seqs, weights, keep, first=0, recent=0):
+    """The call, and the same on the model."""
+    import torch
+    before = weights.clone()
+    L = model.L
+    w0, w1 = first // L, -(-keep // L)
+    mw.mw_kvpages_evict_weighted(cache, seqs, weights, keep, first=first, recent=recent)
+    torch.cuda.synchronize()
+    jobs = [s for s in seqs if model.lens[s] > keep]
+    new = model.take(len(jobs) * (w1 - w0))
+    assert len(new) == len(jobs) * (w1 - w0)
+    source = {s: (list(model.rows[s]), model.lens[s]) for s in jobs}
+    for i, s in enumerate(jobs):
+        row, n = source[s]
+        stay = kept(before[s].tolist(), n, keep, first, recent)
+        assert len(stay) == keep and stay[:first] == list(range(first))
+        pages = new[i * (w1 - w0):(i + 1) * (w1 - w0)]
+        moved = torch.tensor(stay[w0 * L:], device="cuda", dtype=torch.long)
+        where = torch.tensor(row, device="cuda")[moved // L]
+        for x in range(2):
+            value = model.code[x][where, :, moved % L].double() * torch.exp2(model.exp[x][where, :, moved % L // BLOCK].double())[..., None]
+            for c in range(0, len(moved), BLOCK):
+                val = value[c:c + BLOCK].transpose(0, 1)  # [H, t, D]
+                model.write(x, pages[c // L], c % L, val)
+        want = before[s].clone()
+        want[:keep] = before[s][torch.tensor(stay, device="cuda")]
+        want[keep:n] = 0
+        assert torch.equal(weights[s].nan_to_num(nan=1e9), want.nan_to_num(nan=1e9)), f"weights of sequence {s}"
+        model.rows[s] = row[:w0] + pages
+        model.lens[s] = keep
+    for s in range(len(model.lens)):
+        if s not in jobs:
+            assert torch.equal(weights[s].nan_to_num(nan=1e9), before[s].nan_to_num(nan=1e9))
+    model.verify()
+
+
+def filled(mw, lens, H, L, D, N, W, P, seed=1):
+    cache, model = make(mw, P, H, L, D, N, W)
+    for s, n in enumerate(lens):
+        if n:
+            k, v = tokens((1, H, n, D), seed + s), tokens((1, H, n, D), seed + 50 + s)
+            mw.mw_kvpages_append(cache, [s], k, v)
+            model.append([s], k, v)
+    return cache, model
+
+
+def some_weights(cache, seed):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    w = torch.exp(2 * torch.randn(cache.desc.N, cache.desc.W * cache.desc.L, device="cuda", generator=g))
+    return torch.where(torch.rand(w.shape, device="cuda", generator=g) < 0.2, 0.0, w.bfloat16().float())
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("L", [64, 192])
+@pytest.mark.parametrize("keep,first,recent", [(1, 0, 0), (64, 0, 64), (100, 30, 20), (200, 192, 0), (192, 192, 0), (257, 70, 187),
+                                               (399, 0, 1)])
+def test_what_stays(mw, D, L, keep, first, recent):
+    """Several sequences, some of them short enough to be left alone; ties; nothing chosen by weight; a cut only."""
+    cache, model = filled(mw, [400, 63, 0, 401, 577], 3, L, D, 6, 10, 60)
+    w = some_weights(cache, keep)
+    evict(mw, cache, model, [4, 0, 2, 1, 3], w, keep, first, recent)
+    # and again, on what is left, and more tokens behind
+    k, v = tokens((2, 3, 70, D), 90), tokens((2, 3, 70, D), 91)
+    mw.mw_kvpages_append(cache, [0, 4], k, v)
+    model.append([0, 4], k, v)
+    evict(mw, cache, model, [0, 4], some_weights(cache, keep + 1), max(1, keep // 2), first // 2, recent // 2)
+
+
+def test_equal_infinite_and_nan_weights(mw):
+    import torch
+    cache, model = filled(mw, [300, 300, 300, 300, 300], 2, 64, 64, 5, 6, 60)
+    w = torch.zeros(5, 6 * 64, device="cuda")
+    w[0] = 1.0                                     # all equal: the front ones
+    w[1, 50:80] = float("nan")
+    w[1, 100:103] = float("inf")
+    w[1, 7:300:9] = -1.0
+    w[2, ::2] = -0.0                               # equal to 0
+    w[2, 200:210] = 1e-45                          # the least above 0
+    w[3] = float("nan")
+    w[4] = -torch.arange(6 * 64, device="cuda")
+    w[4, 299] = -float("inf")
+    evict(mw, cache, model, [0, 1, 2, 3, 4], w, 123, 0, 0)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_branches_keep_their_common_pages(mw, D):
+    """The other branches read what they did; the anchor's whole pages stay shared; freed pages are those nobody reads."""
+    cache, model = filled(mw, [500], 2, 64, D, 4, 9, 40)
+    for s in (1, 2):
+        mw.mw_kvpages_fork(cache, 0, s)
+        model.rows[s], model.lens[s] = list(model.rows[0]), model.lens[0]
+    evict(mw, cache, model, [1, 2], some_weights(cache, 5), 250, 150, 60)
+    assert model.rows[1][:2] == model.rows[0][:2] == model.rows[2][:2] and model.rows[1][2] != model.rows[0][2]
+    evict(mw, cache, model, [0], some_weights(cache, 6), 130, 0, 130)
+    mw.mw_kvpages_free(cache, [0, 1])
+    model.drop([0, 1])
+    model.verify()
+
+
+def test_too_few_pages(mw):
+    import torch
+    cache, model = filled(mw, [200, 200], 2, 64, 64, 2, 4, 10)  # two pages are free
+    w = some_weights(cache, 7)
+    before = w.clone()
+    with pytest.raises(mw.MWError) as e:
+        mw.mw_kvpages_evict_weighted(cache, [0, 1], w, 100)
+    assert e.value.code == mw.MW_EFULL
+    torch.cuda.synchronize()
+    assert torch.equal(w, before)
+    model.verify()
+    evict(mw, cache, model, [0], w, 100)
+    evict(mw, cache, model, [1], w, 100)
+
+
+def test_long_sequences(mw):
+    """More tokens than are held in LDS, and more pages than travel in one launch."""
+    cache, model = filled(mw, [40001, 33100], 1, 64, 64, 2, 640, 2300)
+    w = some_weights(cache, 8)
+    evict(mw, cache, model, [0, 1], w, 33001, 1000, 501)
+    evict(mw, cache, model, [0, 1], w, 20000, 0, 0)
+
+
+def test_codes_that_were_finer(mw):
+    """A token of a small block beside one of a large block: its codes are rounded again, and become subnormal or 0."""
+    import torch
+    H, D = 1, 64
+    cache, model = make(mw, 8, H, 64, D, 1, 6)
+    k, v = randn((1, H, 192, D), 1), randn((1, H, 192, D), 2)
+    gain = torch.tensor([1.0, 2.0 ** 12, 2.0 ** -11], device="cuda").repeat_interleave(64).view(1, 1, 192, 1)
+    k, v = (k.float() * gain).bfloat16(), (v.float() * gain).bfloat16()
+    mw.mw_kvpages_append(cache, [0], k, v)
+    model.append([0], k, v)
+    w = torch.zeros(1, 6 * 64, device="cuda")
+    w[0, ::3] = 1.0
+    evict(mw, cache, model, [0], w, 64)
+
+
+def test_a_rollout_that_drops_its_lightest_tokens(mw):
+    """Positions, attention of the packed prompts, commit, single tokens over the pages with their weights, eviction, and
+    the attention over what is left: every step against 64-bit values."""
+    import torch
+    H, Hkv, D, L, lens = 4, 2, 128, 64, [300, 211]
+    T = sum(lens)
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = {n: torch.randn(T, h, D, device="cuda", generator=g).bfloat16() for n, h in (("q", H), ("k", Hkv), ("v", Hkv))}
+    rb = mw.rope_bands([dict(dim_offset=0, dim_count=D)], halves=True)
+    pos = torch.cat([torch.arange(n, device="cuda") for n in lens])
+    view = lambda t: t.transpose(0, 1)[None]
+    mw.mw_rope_apply(view(x["q"]), view(x["k"]), rb, pos, q_out=view(x["q"]), k_out=view(x["k"]))
+    cu = torch.tensor([0, *lens], device="cuda").cumsum(0).to(torch.int32)
+    pack = mw.Packed(cu, T, H, Hkv, D)
+    o, lse = mw.mw_packed_attn_fwd(x["q"], x["k"], x["v"], pack)
+    cache, model = make(mw, 24, Hkv, L, D, 2, 8)
+    at = 0
+    for s, n in enumerate(lens):
+        i = slice(at, at + n)
+        at += n
+        causal = torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1)
+        for h in range(H):
+            want = attention64(x["q"][i, h], x["k"][i, h // 2], x["v"][i, h // 2], causal, D ** -0.5)
+            check(f"o {s} {h}", o[i, h], *want["o"])
+        k, v = view(x["k"][i]), view(x["v"][i])
+        mw.mw_kvpages_append(cache, [s], k, v)
+        model.append([s], k, v)
+    w = torch.zeros(2, 8 * L, device="cuda")
+    total = torch.zeros(2, 8 * L, dtype=torch.float64, device="cuda")
+    for step in range(3):
+        q, k, v = (torch.randn(2, h, 1, D, device="cuda", generator=g).bfloat16() for h in (H, Hkv, Hkv))
+        at = torch.tensor([[model.lens[0]], [model.lens[1]]], device="cuda")
+        q, k = mw.mw_rope_apply(q, k, rb, at)
+        o, lse = mw.mw_chunk_attn_paged(q, k, v, 1, 1, cache, [0, 1], want_lse=True)
+        mw.mw_kvpages_weigh(cache, [0, 1], q, lse, w)
+        torch.cuda.synchronize()
+        for s in (0, 1):
+            kk, vv = model.values(s)
+            for h in range(H):
+                a = torch.cat([kk[h // 2], k[s, h // 2].double()])
+                c = torch.cat([vv[h // 2], v[s, h // 2].double()])
+                none = torch.zeros((1, 1), dtype=torch.bool, device="cuda")
+                want = attention64(q[s, h], a, c, none, D ** -0.5)
+                check(f"o {step} {s} {h}", o[s, h], *want["o"])
+                p = torch.exp((q[s, h].double() @ a.t())[0] * D ** -0.5 - want["lse"][0])
+                total[s, :model.lens[s]] += p[:-1]
+        # (32-bit sums of probabilities of at most 1, a few 2^-22 off each)
+        assert bool(((w.double() - total).abs() <= 3 * H * 2.0 ** -19).all())
+        mw.mw_kvpages_append(cache, [0, 1], k, v)
+        model.append([0, 1], k, v)
+    model.verify()
+    evict(mw, cache, model, [0, 1], w, 150, 10, 20)
+    q = torch.randn(2, H, 1, D, device="cuda", generator=g).bfloat16()
+    o, _ = mw.mw_chunk_attn_paged(q, None, None, 1, 1, cache, [0, 1])
+    for s in (0, 1):
+        kk, vv = model.values(s)
+        for h in range(H):
+            none = torch.zeros((1, 1), dtype=torch.bool, device="cuda")
+            check("o", o[s, h], *attention64(q[s, h], kk[h // 2], vv[h // 2], none, D ** -0.5)["o"])
+
+
+def test_refusals_of_the_binding(mw):
+    import torch
+    cache, _ = filled(mw, [100, 100], 2, 64, 64, 2, 4, 12)
+    w = torch.zeros(2, 256, device="cuda")
+    q, lse = randn((2, 4, 3, 64), 1), torch.zeros(2, 4, 3, device="cuda")
+    for bad in (w[:1], w.double(), w.cpu(), w.t().contiguous().t()):
+        with pytest.raises(ValueError):
+            mw.mw_kvpages_weigh(cache, [0, 1], q, lse, bad)
+        with pytest.raises(ValueError):
+            mw.mw_kvpages_evict_weighted(cache, [0, 1], bad, 50)
+    with pytest.raises(ValueError):
+        mw.mw_kvpages_weigh(cache, [0, 1], q, lse[:1], w)
+    with pytest.raises(ValueError):
+        mw.mw_kvpages_weigh(cache, [0], q, lse, w)
+    with pytest.raises(mw.MWError):
+        mw.mw_kvpages_weigh(cache, [1, 1], q, lse, w)
+    with pytest.raises(mw.MWError):
+        mw.mw_kvpages_evict_weighted(cache, [0, 0], w, 50)
+    graph = torch.cuda.CUDAGraph()
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    with torch.cuda.graph(graph):
+        w.add_(1.0)
+        with pytest.raises(mw.MWError):
+            mw.mw_kvpages_weigh(cache, [0, 1], q, lse, w, workspace=ws)
+        with pytest.raises(mw.MWError):
+            mw.mw_kvpages_evict_weighted(cache, [0, 1], w, 50, workspace=ws)
