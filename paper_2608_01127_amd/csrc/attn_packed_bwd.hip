@@ -17,35 +17,31 @@ namespace {
 
 constexpr int kD = MW_PACKED_HEAD_DIM;
 
-// Byte offsets, from the step's first row, of the pieces this thread stages of ROWS rows of a key head's G query heads
-// (StagePlan's pieces; G divides ROWS and a step begins with a token's first row).
+// Stages ROWS rows of a key head's G > 1 query heads from row r0 on (StagePlan's pieces): from r0's token on, a piece's
+// token and head are a few steps away, found without a division, and its bytes at a 32-bit offset (`near`).
 template <int D, int ROWS, int NT>
-struct GroupOffsets {
-  unsigned off[StagePlan<D, ROWS, NT>::ROUNDS];
-  __device__ __forceinline__ GroupOffsets(const Strides& s, int G, int tid) {
-    using SP = StagePlan<D, ROWS, NT>;
+__device__ __forceinline__ void stage_group(bf16_t* lds_tile, const bf16_t* base, const Strides& s, int r0, int G,
+                                            unsigned magic, int tid) {
+  using SP = StagePlan<D, ROWS, NT>;
+  const int t0 = (unsigned)r0 / (unsigned)G, skip = r0 - t0 * G;
+  base += (long long)t0 * s.t;
+  const unsigned st = (unsigned)s.t * 2, sh = (unsigned)s.h * 2;
 #pragma unroll
-    for (int it = 0; it < SP::ROUNDS; ++it) {
-      const int ci0 = it * NT + tid;
-      const int ci = (SP::PIECES % NT == 0 || ci0 < SP::PIECES) ? ci0 : 0;
-      const int row = ci / SP::SLOTS, ls = (ci % SP::SLOTS) ^ Tile<D>::swz(row);
-      const int t = (unsigned)row / (unsigned)G;
-      off[it] = (unsigned)((t * s.t + (row - t * G) * s.h) * 2 + ls * 16);
-    }
+  for (int it = 0; it < SP::ROUNDS; ++it) {
+    const int ci0 = it * NT + tid;
+    const int ci = (SP::PIECES % NT == 0 || ci0 < SP::PIECES) ? ci0 : 0;  // past the tile: row 0 again, into the slack
+    const int row = ci / SP::SLOTS, ls = (ci % SP::SLOTS) ^ Tile<D>::swz(row);
+    const unsigned x = skip + row, t = __umulhi(x, magic);
+    dma_lds_16_s(base, t * st + (x - t * G) * sh + ls * 16, lds_addr(lds_tile) + it * NT * 16 + wave_stage_off(tid));
   }
-  __device__ __forceinline__ void stage(bf16_t* lds_tile, const bf16_t* first_row, int tid) const {
-#pragma unroll
-    for (int it = 0; it < StagePlan<D, ROWS, NT>::ROUNDS; ++it)
-      dma_lds_16_s(first_row, off[it], lds_addr(lds_tile) + it * NT * 16 + wave_stage_off(tid));
-  }
-};
+}
 
 // dK/dV: NWK key waves of 32 keys each (K fragments, dK^T and dV^T in registers) in QG row groups; a step stages
 // BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
 // first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
 // the registers).  Lanes behind the last key repeat it and store nothing.
-template <int D, int NWK, int QG, int BM, int VL>
-__global__ __launch_bounds__(64 * NWK * QG, 2) void packed_dkdv_kernel(PackedBwdParams p) {
+template <int D, int NWK, int QG, int BM, int VL, int WPS>
+__global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedBwdParams p) {
   constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
   static_assert(16 * VL <= D, "the V fragments in LDS have no columns past D");
@@ -93,16 +89,20 @@ __global__ __launch_bounds__(64 * NWK * QG, 2) void packed_dkdv_kernel(PackedBwd
     };
     const FragOffsets<D> fo(lane, gq * D);
     const Tail72 ft(lane, gq * D);
-    const GroupOffsets<D, BS, NT> go_q(p.sq, G, tid), go_o(p.sdo, G, tid);
+    const RowOffsets<D, BS, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
+    const bf16_t* q0p = p.q + (long long)hk * G * p.sq.h + (long long)it.q0 * p.sq.t;
+    const bf16_t* o0p = p.d_o + (long long)hk * G * p.sdo.h + (long long)it.q0 * p.sdo.t;
     const long long row_base = ((long long)hk * p.total_q + it.q0) * G;
     const float* lse2 = p.lse2 + row_base;
     const float* dlt = p.delta + row_base;
     const int beg = it.beg * BS, end = min(R, it.end * BS);
     auto stage = [&](int r0, int buf) {  // rows behind the sequence's last one repeat it
-      if (p.grouped && r0 + BS <= R) {
-        const long long t = it.q0 + (G == 1 ? r0 : r0 / G);
-        go_q.stage(Qs[buf], p.q + (long long)hk * G * p.sq.h + t * p.sq.t, tid);
-        go_o.stage(Os[buf], p.d_o + (long long)hk * G * p.sdo.h + t * p.sdo.t, tid);
+      if (r0 + BS <= R && G == 1) {
+        stage_rows_s<D, BS, NT>(Qs[buf], q0p + r0 * p.sq.t, ro_q, tid);
+        stage_rows_s<D, BS, NT>(Os[buf], o0p + r0 * p.sdo.t, ro_o, tid);
+      } else if (r0 + BS <= R && p.near) {
+        stage_group<D, BS, NT>(Qs[buf], q0p, p.sq, r0, G, p.magic, tid);
+        stage_group<D, BS, NT>(Os[buf], o0p, p.sdo, r0, G, p.magic, tid);
       } else {
         stage_rows_direct<D, BS, NT>(Qs[buf], [&](int r) { return p.q + packed_offset(p.sq, hk, G, it.q0, min(r0 + r, R - 1)); },
                                      tid);
@@ -508,11 +508,19 @@ __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p,
 
 }  // namespace
 
+// The dK/dV kernel's tile: 128 keys in four waves; with two row groups of eight waves, whose barriers hold them all in step,
+// the 1B clips take 1993 for 1920 us, forward and backward, the text batch (D = 64) 399 for 381.
+template <int NWK_, int QG_, int BM_, int VL_, int WPS_>
+struct DkvTile {
+  static constexpr int NWK = NWK_, QG = QG_, BM = BM_, VL = VL_, WPS = WPS_;
+};
+using Dkv = DkvTile<4, 1, packed_dkv_step(kD), kD == 128 ? 6 : 0, kD == 64 ? 3 : 2>;
+
 #define MW_CAT_(a, b) a##b
 #define MW_CAT(a, b) MW_CAT_(a, b)
 hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
-  constexpr int NW = 4, BN = 128;
-  if (s.dq.tile != 32 * NW || s.dq.step != 64 || s.dkv.tile != BN || s.dkv.step != 64) return hipErrorInvalidValue;
+  constexpr int NW = 4, BN = 32 * Dkv::NWK;
+  if (s.dq.tile != 32 * NW || s.dq.step != 64 || s.dkv.tile != BN || s.dkv.step != Dkv::BM * Dkv::QG) return hipErrorInvalidValue;
   const long long grid_q = (long long)s.dq.max_items * s.Hkv, grid_k = (long long)s.dkv.max_items * s.Hkv;
   const long long n_kv = (long long)s.dkv.max_joins * s.Hkv * (BN * (kD / 4) / 256);
   const long long n_q = (long long)s.dq.max_joins * s.Hkv * (32 * NW * (kD / 4) / 256);
@@ -520,7 +528,8 @@ hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams&
   hipLaunchKernelGGL((packed_dq_kernel<kD, NW, 64, kD == 128 ? 2 : 3>), dim3((unsigned)grid_q), dim3(64 * NW), 0, stream, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_dkdv_kernel<kD, 4, 2, 32, kD == 128 ? 6 : 0>), dim3((unsigned)grid_k), dim3(512), 0, stream, p);
+  hipLaunchKernelGGL((packed_dkdv_kernel<kD, Dkv::NWK, Dkv::QG, Dkv::BM, Dkv::VL, Dkv::WPS>), dim3((unsigned)grid_k),
+                     dim3(64 * Dkv::NWK * Dkv::QG), 0, stream, p);
   e = hipGetLastError();
   if (e != hipSuccess || n_kv + n_q == 0) return e;
   hipLaunchKernelGGL((packed_bwd_join_kernel<kD, 32 * NW, BN>), dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);

@@ -445,6 +445,8 @@ struct PackedParams {
   int max_slots;
   float scale_log2;
 };
+// Rows of a step of the dK/dV kernel.
+constexpr int packed_dkv_step(int D) { return D == 128 ? 32 : 64; }
 size_t packed_part_bytes(const PackedShape& s);
 hipError_t launch_packed_fwd_64(const PackedParams& p, const PackedList& list, hipStream_t stream);
 hipError_t launch_packed_fwd_72(const PackedParams& p, const PackedList& list, hipStream_t stream);
@@ -464,7 +466,8 @@ struct PackedBwdParams {
   float* lse2;   // [Hkv][total_q G]: LSE log2 e
   Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   int Hkv, G, L, total_q;
-  bool grouped;  // a step's rows lie at fixed offsets from its first one (G divides a step and they fit 32 bits)
+  bool near;       // rows of a step lie within 2^32 bytes of its first token
+  unsigned magic;  // ceil(2^32 / G): x / G is the high word of their product for x < 2^15
   const int* list_q;
   const int* list_k;
   const PackedJoin* joins_q;

@@ -199,10 +199,10 @@ int mw_packed_attn_bwd(const void* q, const void* k, const void* v, const void* 
   a.L = s.L;
   a.total_q = p->total_q;
   const auto near = [&](const Strides& x) {
-    return s.dkv.step % s.G == 0 &&
-           2.0 * ((double)(s.dkv.step / s.G) * x.t + (double)(s.G - 1) * x.h + p->D) < 4294967296.0;
+    return 2.0 * ((double)(s.dkv.step / s.G + 2) * x.t + (double)s.G * x.h + p->D) < 4294967296.0;
   };
-  a.grouped = near(a.sq) && near(a.sdo);
+  a.near = near(a.sq) && near(a.sdo);
+  a.magic = (unsigned)(((1ULL << 32) + s.G - 1) / s.G);  // (2^32 wraps to 0 at 1, which is not used)
   a.list_q = p->plan + s.dq.at;
   a.list_k = p->plan + s.dkv.at;
   a.joins_q = reinterpret_cast<const PackedJoin*>(a.list_q + 8 + 8LL * s.dq.max_items);
