@@ -558,14 +558,19 @@ struct WeighParams {
   float* part;         // n_parts > 1: [n_parts][blocks][64]
   Strides sq;
   int B, Hkv, G, T, R, L, W, per_page, n_parts;
-  bool add;
+  bool many, add, near;  // (near, magic: as PackedBwdParams')
+  unsigned magic;
   float scale_log2;
 };
 struct WeighSeqs {
   int seq[kMaxSeqs];
   int first[kMaxSeqs + 1];  // number of the first block of 64 tokens of each member, then of all
 };
-int weigh_parts(int Hkv, int R, long long blocks);
+struct WeighPlan {
+  bool many;
+  int parts;
+};
+WeighPlan weigh_plan(int Hkv, int R, long long blocks);
 hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipStream_t stream);
 // Sequences of which `keep` tokens stay: the `first` ones, the `recent` last ones and the heaviest others.
 struct KeepArgs {

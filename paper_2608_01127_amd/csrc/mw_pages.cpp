@@ -437,7 +437,7 @@ static int weigh_blocks(const mw_kvpages* c, const int32_t* seqs, int n_seqs, We
 
 size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T) {
   if (check_weigh("mw_kvpages_weigh_workspace_size", c, seqs, n_seqs, H, T)) return 0;
-  const int n = weigh_blocks(c, seqs, n_seqs, nullptr), parts = weigh_parts(c->H, T * (H / c->H), n);
+  const int n = weigh_blocks(c, seqs, n_seqs, nullptr), parts = weigh_plan(c->H, T * (H / c->H), n).parts;
   return parts > 1 ? (size_t)parts * n * MW_PAGE_BLOCK * sizeof(float) : 0;
 }
 
@@ -461,7 +461,9 @@ int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const
   WeighSeqs s{};
   const int blocks = weigh_blocks(c, seqs, n_seqs, &s);
   WeighParams p{};
-  p.n_parts = weigh_parts(c->H, T * (H / c->H), blocks);
+  const WeighPlan plan = weigh_plan(c->H, T * (H / c->H), blocks);
+  p.many = plan.many;
+  p.n_parts = plan.parts;
   const size_t need = p.n_parts > 1 ? (size_t)p.n_parts * blocks * MW_PAGE_BLOCK * sizeof(float) : 0;
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p.n_parts = 1;
   p.q = static_cast<const uint16_t*>(q);
@@ -483,6 +485,8 @@ int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const
   p.W = c->W;
   p.per_page = c->L / MW_PAGE_BLOCK;
   p.add = add != 0;
+  p.near = 2.0 * (66.0 * sq.t + (double)p.G * sq.h + c->D) < 4294967296.0;
+  p.magic = (unsigned)(((1ULL << 32) + p.G - 1) / p.G);  // (2^32 wraps to 0 at 1, which is not used)
   p.scale_log2 = scale * kLog2e;
   return hip_status(fn, launch_weigh(p, s, c->D, static_cast<hipStream_t>(stream)));
 }
