@@ -7,7 +7,7 @@ namespace mw {
 
 namespace {
 
-constexpr int kThreads = 1024, kCached = 32768, kBins = 2048;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kEach = 16, kBins = 256, kCopies = 32;
 
 // Order of the weights as unsigned numbers; -0 is 0, NaN is the lightest.
 __device__ __forceinline__ unsigned order_of(float w) {
@@ -19,14 +19,18 @@ __device__ __forceinline__ unsigned order_of(float w) {
 }  // namespace
 
 // One workgroup for each sequence.  Of its tokens [first, len - recent) the k heaviest stay, of equal ones those in
-// front: the weight of the k-th is found by three counts of 11, 11 and 10 bits, from the top; then each wave walks its
-// stretch of the tokens in order and lists what stays, with its page, at the place that the stretches in front leave.
-__global__ __launch_bounds__(kThreads) void keep_select_kernel(PagePool c, KeepArgs a, const float* weights, int2* list,
-                                                               float* kept) {
-  __shared__ unsigned cache[kCached];
-  __shared__ int bins[kBins];
-  __shared__ int wave_sums[16], wave_gt[16], wave_eq[16];
+// front: the weight of the k-th is found by four counts of 8 bits, from the top; with the numbers of heavier and equal ones in
+// front of it, every token knows whether it stays and where.  A thread holds 16 tokens' weights in registers, every 1024th;
+// more tokens than that are read again for each count.  Weights that lie close fall into few bins: each bin has a counter
+// for every lane of a half wave, on a bank of its own.  Bound by its own latencies, one after another: 13 us for 2700 tokens,
+// 20 for 12900 (walking them a wave a stretch, looking up pages on the way: 25).
+__global__ __launch_bounds__(kThreads) void keep_select_kernel(PagePool c, KeepArgs a, const float* __restrict__ weights,
+                                                               int2* __restrict__ list, float* __restrict__ kept) {
+  __shared__ int bins[kBins * kCopies];
+  __shared__ int counts[kBins];
+  __shared__ int heavier[kEach * kWaves + 1], equal[kEach * kWaves + 1];
   __shared__ int chosen, above;
+  static_assert(kEach * kWaves == 256, "one wave adds up the counts, four a lane");
   const int job = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int seq = a.seq[job], len = a.len[job], n = len - a.recent - a.first, k = a.keep - a.recent - a.first;
   const float* w = weights + (long long)seq * c.W * c.L;
@@ -34,96 +38,145 @@ __global__ __launch_bounds__(kThreads) void keep_select_kernel(PagePool c, KeepA
   const int from = a.first / c.L * c.L;  // the anchor's whole pages stay where they are
   list += (long long)job * (a.keep - from);
   kept += (long long)job * (a.keep - from);
-  const bool cached = n <= kCached;
-  for (int i = tid; cached && i < n; i += kThreads) cache[i] = order_of(w[a.first + i]);
-  auto key = [&](int i) { return cached ? cache[i] : order_of(w[a.first + i]); };
+  const int per = c.L / 64;
+  auto put = [&](int place, int token, float weight) {  // entry of the token at `place` of the new sequence
+    const int blk = token >> 6, at = per == 1 ? blk : (int)__umulhi((unsigned)blk, a.per_page_magic);
+    list[place - from] = make_int2(row[at], token - at * c.L);
+    kept[place - from] = weight;
+  };
+  for (int i = from + tid; i < a.first; i += kThreads) put(i, i, w[i]);
+#pragma unroll 4
+  for (int i = tid; i < a.recent; i += kThreads) put(a.keep - a.recent + i, len - a.recent + i, w[len - a.recent + i]);
+  if (k == 0) return;
+
+  constexpr int CHUNK = kEach * kThreads;
+  const bool once = n <= CHUNK;
+  float v[kEach];
+  auto load = [&](int c0) {
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) v[j] = w[a.first + min(c0 + j * kThreads + tid, n - 1)];
+  };
+  load(0);
   unsigned limit = 0;  // the k-th heaviest, bit group by bit group
   int left = k;        // how many of those that agree with the groups so far stay
-  for (int pass = 0; pass < 3 && k > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < kBins; i += kThreads) bins[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const unsigned x = key(i);
-      if (pass == 0 || (x >> (shift + bits)) == (limit >> (shift + bits)))
-        atomicAdd(&bins[(x >> shift) & ((1u << bits) - 1)], 1);
-    }
-    __syncthreads();
-    // the bin, from the top, that holds the left-th: a thread's two bins, then the sums over threads above
-    const int hi = kBins - 1 - 2 * tid, two = bins[hi] + bins[hi - 1];
-    int in = two;
+  for (int shift = 24; shift >= 0; shift -= 8) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(in, d);
-      if (lane >= d) in += y;
-    }
-    if (lane == 63) wave_sums[wave] = in;
+    for (int i = 0; i < kBins * kCopies / kThreads; ++i) bins[i * kThreads + tid] = 0;
     __syncthreads();
-    int front = in - two;
-    for (int i = 0; i < wave; ++i) front += wave_sums[i];
-    if (front < left && front + two >= left) {
-      const bool second = front + bins[hi] < left;
-      chosen = second ? hi - 1 : hi;
-      above = second ? front + bins[hi] : front;
+    for (int c0 = 0; c0 < n; c0 += CHUNK) {
+      if (!once) load(c0);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        if (c0 + j * kThreads >= n) break;
+        const unsigned x = order_of(v[j]);
+        const bool agrees = shift == 24 || (x >> (shift + 8)) == (limit >> (shift + 8));
+        if (agrees && c0 + j * kThreads + tid < n) atomicAdd(&bins[((x >> shift) & 255u) * kCopies + (lane & 31)], 1);
+      }
+    }
+    __syncthreads();
+    {  // four threads add up a bin's counters
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < kCopies / 4; ++i) sum += bins[(tid >> 2) * kCopies + ((i * 4 + tid + (tid >> 2)) & 31)];
+      sum += __shfl_xor(sum, 1);
+      sum += __shfl_xor(sum, 2);
+      if ((tid & 3) == 0) counts[tid >> 2] = sum;
+    }
+    __syncthreads();
+    if (wave == 0) {  // the bin, from the top, that holds the left-th: four bins a lane
+      int own[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        own[i] = counts[kBins - 1 - 4 * lane - i];
+        sum += own[i];
+      }
+      int front = sum;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(front, d);
+        if (lane >= d) front += y;
+      }
+      front -= sum;
+      if (front < left && front + sum >= left) {
+        int bin = kBins - 1 - 4 * lane;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (front + own[i] < left && bin == kBins - 1 - 4 * lane - i) {
+            front += own[i];
+            --bin;
+          }
+        chosen = bin;
+        above = front;
+      }
     }
     __syncthreads();
     limit |= (unsigned)chosen << shift;
     left -= above;
+  }
+
+  int gt0 = 0, eq0 = 0;  // heavier and equal tokens of the chunks in front
+  const unsigned long long below = (1ULL << lane) - 1;
+  for (int c0 = 0; c0 < n; c0 += CHUNK) {
+    if (!once) load(c0);
+    unsigned long long gt[kEach], eq[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const bool in = c0 + j * kThreads + tid < n;
+      const unsigned x = order_of(v[j]);
+      gt[j] = __builtin_amdgcn_ballot_w64(in && x > limit);
+      eq[j] = __builtin_amdgcn_ballot_w64(in && x == limit);
+      if (lane == 0) {
+        heavier[j * kWaves + wave] = __builtin_popcountll(gt[j]);
+        equal[j * kWaves + wave] = __builtin_popcountll(eq[j]);
+      }
+    }
+    __syncthreads();
+    if (wave < 2) {  // numbers in front of each wave's 64 tokens
+      int* x = wave == 0 ? heavier : equal;
+      int own[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        own[i] = x[4 * lane + i];
+        sum += own[i];
+      }
+      int front = sum;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(front, d);
+        if (lane >= d) front += y;
+      }
+      if (lane == 63) x[kEach * kWaves] = front;
+      front -= sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[4 * lane + i] = front;
+        front += own[i];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int before = eq0 + equal[j * kWaves + wave] + __builtin_popcountll(eq[j] & below);
+      const bool stays = (gt[j] >> lane & 1) || ((eq[j] >> lane & 1) && before < left);
+      if (stays)
+        put(a.first + gt0 + heavier[j * kWaves + wave] + __builtin_popcountll(gt[j] & below) + min(before, left),
+            a.first + c0 + j * kThreads + tid, v[j]);
+    }
+    gt0 += heavier[kEach * kWaves];
+    eq0 += equal[kEach * kWaves];
     __syncthreads();
   }
-  __syncthreads();
-  // this wave's stretch: how many are heavier than the limit, and equal to it
-  const int per = (n + 15) / 16, i0 = min(n, wave * per), i1 = min(n, i0 + per);
-  int gt = 0, eq = 0;
-  for (int i = i0 + lane; i < i1; i += 64) {
-    const unsigned x = key(i);
-    gt += x > limit;
-    eq += x == limit;
-  }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    gt += __shfl_xor(gt, m);
-    eq += __shfl_xor(eq, m);
-  }
-  if (lane == 0) {
-    wave_gt[wave] = gt;
-    wave_eq[wave] = eq;
-  }
-  __syncthreads();
-  gt = eq = 0;
-  for (int i = 0; i < wave; ++i) {
-    gt += wave_gt[i];
-    eq += wave_eq[i];
-  }
-  auto put = [&](int place, int token) {  // entry of the token at `place` of the new sequence
-    list[place - from] = make_int2(row[token / c.L], token % c.L);
-    kept[place - from] = w[token];
-  };
-  const unsigned long long below = (1ULL << lane) - 1;
-  for (int i = i0; i < i1 && k > 0; i += 64) {
-    const bool in = i + lane < i1;
-    const unsigned x = in ? key(i + lane) : 0;
-    const unsigned long long e = __builtin_amdgcn_ballot_w64(in && x == limit);
-    const int mine = eq + __builtin_popcountll(e & below);
-    const bool stays = in && (x > limit || (x == limit && mine < left));
-    const unsigned long long s = __builtin_amdgcn_ballot_w64(stays);
-    if (stays) put(a.first + gt + min(eq, left) + __builtin_popcountll(s & below), a.first + i + lane);
-    // (gt + min(eq, left) tokens stay in front of this step)
-    const unsigned long long g = __builtin_amdgcn_ballot_w64(in && x > limit);
-    gt += __builtin_popcountll(g);
-    eq += __builtin_popcountll(e);
-  }
-  for (int i = from + tid; i < a.first; i += kThreads) put(i, i);
-  for (int i = tid; i < a.recent; i += kThreads) put(a.keep - a.recent + i, len - a.recent + i);
 }
 
 // The listed tokens into their pages: one workgroup for 64 of them of one head, K (blockIdx.y < H) or V.  Their block's
 // scale is the least that holds them, so a code changes only where its own block's scale was finer.  The workgroups of
-// K's first head also write the weights' row, the table and the length.
+// K's first head also write the weights' row, the table and the length.  Bound by HBM: 4 x 7664 tokens of 16 heads, D = 128,
+// 251 MB read and written: 52 us, 4.8 TB/s (in 8-byte pieces 66).
 template <int D>
 __global__ __launch_bounds__(256) void keep_gather_kernel(PagePool c, KeepRun a, float* weights, const int2* list,
                                                           const float* kept) {
-  constexpr int PPR = D / 8, PIECES = 64 * PPR, ROUNDS = (PIECES + 255) / 256;
+  constexpr int CODES = D % 16 == 0 ? 16 : 8;  // of a thread's piece
+  constexpr int PPR = D / CODES, PIECES = 64 * PPR, ROUNDS = (PIECES + 255) / 256;
   const int run = blockIdx.z, tid = threadIdx.x, L = c.L;
   const int first = a.first[run], n_tok = a.n_tok[run];  // places [first, first + n_tok), first on a page's start
   const int at = first + (int)blockIdx.x * 64;
@@ -145,7 +198,7 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(PagePool c, KeepRun a,
   const int h = is_v ? blockIdx.y - c.H : blockIdx.y, per = L / 64;
   uint8_t* pages = is_v ? c.v_pages : c.k_pages;
   float* scales = is_v ? c.v_scales : c.k_scales;
-  float x[ROUNDS][8];
+  float x[ROUNDS][CODES];
   float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
@@ -153,11 +206,17 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(PagePool c, KeepRun a,
     if (r >= n) continue;
     const int2 from = list[r];
     const long long head = (long long)from.x * c.H + h;
-    const u32x2 u = *reinterpret_cast<const u32x2*>(pages + (head * L + from.y) * D + (p - r * PPR) * 8);
-    decode8(u, x[i]);
+    const uint8_t* src = pages + (head * L + from.y) * D + (p - r * PPR) * CODES;
     const float scale = scales[head * per + from.y / 64];
+    if constexpr (CODES == 16) {
+      const u32x4 u = *reinterpret_cast<const u32x4*>(src);
+      decode8(u32x2{u[0], u[1]}, x[i]);
+      decode8(u32x2{u[2], u[3]}, x[i] + 8);
+    } else {
+      decode8(*reinterpret_cast<const u32x2*>(src), x[i]);
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < CODES; ++j) {
       x[i][j] *= scale;
       amax = fmaxf(amax, fabsf(x[i][j]));  // (a NaN leaves it)
     }
@@ -176,7 +235,14 @@ __global__ __launch_bounds__(256) void keep_gather_kernel(PagePool c, KeepRun a,
 #pragma unroll
   for (int i = 0; i < ROUNDS; ++i) {
     const int p = i * 256 + tid, r = p / PPR;
-    if (r < n) *reinterpret_cast<u32x2*>(dst + r * D + (p - r * PPR) * 8) = encode8(x[i], inv);
+    if (r >= n) continue;
+    uint8_t* to = dst + r * D + (p - r * PPR) * CODES;
+    if constexpr (CODES == 16) {
+      const u32x2 a = encode8(x[i], inv), b = encode8(x[i] + 8, inv);
+      *reinterpret_cast<u32x4*>(to) = u32x4{a[0], a[1], b[0], b[1]};
+    } else {
+      *reinterpret_cast<u32x2*>(to) = encode8(x[i], inv);
+    }
   }
 }
 

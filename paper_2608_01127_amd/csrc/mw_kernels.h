@@ -575,6 +575,7 @@ hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipS
 // Sequences of which `keep` tokens stay: the `first` ones, the `recent` last ones and the heaviest others.
 struct KeepArgs {
   int n_jobs, keep, first, recent;
+  unsigned per_page_magic;  // as RowsParams'
   int seq[kMaxSeqs], len[kMaxSeqs];
 };
 // Which tokens, as (page, token of the page), and their weights: [n_jobs][keep - first / L * L].

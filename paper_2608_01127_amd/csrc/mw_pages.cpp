@@ -529,6 +529,8 @@ int mw_kvpages_evict_weighted(mw_kvpages* c, const int32_t* seqs, int n_seqs, fl
   a.keep = n_keep;
   a.first = first;
   a.recent = recent;
+  const int per_page = L / MW_PAGE_BLOCK;
+  a.per_page_magic = (unsigned)(((1ULL << 32) + per_page - 1) / per_page);  // (2^32 wraps to 0 at 1, which is not used)
   for (int i = 0; i < n_seqs; ++i) {
     if (b.lens[seqs[i]] <= n_keep) continue;  // nothing to drop
     a.seq[a.n_jobs] = seqs[i];

@@ -18,7 +18,8 @@ __device__ __forceinline__ float pow2(int e) { return e < -126 ? 0.f : __uint_as
 // +-448 at most; NaN stays NaN.
 __device__ __forceinline__ float clamp448(float x) { return x == x ? fminf(fmaxf(x, -448.f), 448.f) : x; }
 
-__device__ __forceinline__ u32x2 encode8(const float (&x)[8], float mul) {
+// Eight values -> codes, and back.
+__device__ __forceinline__ u32x2 encode8(const float* x, float mul) {
   float y[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) y[j] = clamp448(x[j] * mul);
@@ -31,7 +32,7 @@ __device__ __forceinline__ u32x2 encode8(const float (&x)[8], float mul) {
   return r;
 }
 
-__device__ __forceinline__ void decode8(const u32x2& u, float (&x)[8]) {
+__device__ __forceinline__ void decode8(const u32x2& u, float* x) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)u[j], false);
