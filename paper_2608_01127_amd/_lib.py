@@ -750,22 +750,28 @@ class Packed:
         need = int(load().mw_packed_plan_bytes(*self._sizes))
         self.plan = torch.empty(need // 4, dtype=torch.int32, device=self.device)
         self.desc = mw_packed()
+        self._ref = ctypes.byref(self.desc)
+        self.scale = 1.0 / math.sqrt(max(1, self._sizes[5]))
         if need == 0:  # sizes out of range: the library says which
-            _check(load().mw_packed_init(ctypes.byref(self.desc), _ptr(self.cu_q), _ptr(self.cu_k), 16, 0, *self._sizes, None))
+            _check(load().mw_packed_init(self._ref, _ptr(self.cu_q), _ptr(self.cu_k), 16, 0, *self._sizes, None))
         self.update()
 
     def update(self) -> None:
         with _on_device(self.device):
-            _check(load().mw_packed_init(ctypes.byref(self.desc), _ptr(self.cu_q), _ptr(self.cu_k), _ptr(self.plan),
+            _check(load().mw_packed_init(self._ref, _ptr(self.cu_q), _ptr(self.cu_k), _ptr(self.plan),
                                          self.plan.nbytes, *self._sizes, _stream_handle(self.device)))
 
 
-def _check_packed(pack: Packed, queries, keys):
-    """Tensors by name: bf16 views [total_q,H,D] and [total_k,Hkv,D] on the batch's device."""
+def _packed_views(pack: Packed, queries, keys):
+    """Strides of bf16 views [total_q,H,D] (`queries`: tensors by name, or None) and [total_k,Hkv,D] on the batch's
+    device, as the library wants them, in the order given."""
     bf16, index = _torch().bfloat16, pack.device.index
+    strides = []
     for shape, named in ((pack.q_shape, queries), (pack.k_shape, keys)):
-        for n, t in named:
-            if t is None:
+        for n, t in named.items():
+            s = t.stride()
+            if t.dtype is bf16 and t.shape == shape and s[2] == 1 and t.get_device() == index:
+                strides.append(s)
                 continue
             if t.dtype is not bf16:
                 raise TypeError(f"{n} must be bfloat16, got {t.dtype}")
@@ -773,16 +779,18 @@ def _check_packed(pack: Packed, queries, keys):
                 raise ValueError(f"{n} must have shape {shape}, got {tuple(t.shape)}")
             if t.get_device() != index:
                 raise ValueError("all tensors must be on the GPU of the batch")
-            if t.stride(2) != 1:
-                raise ValueError(f"{n} must have a contiguous last (head) dimension")
+            raise ValueError(f"{n} must have a contiguous last (head) dimension")
+    return strides
 
 
-def _packed_strides(*ts):
-    return _strides_array(*[(0, s[1], s[0]) for s in (t.stride() for t in ts)])
+@functools.lru_cache(maxsize=512)
+def _packed_strides(*strides):
+    """mw_strides array of [T,H,D] views (kept by its values, as _strides_array's)."""
+    return _strides_array(*[(0, s[1], s[0]) for s in strides])
 
 
 def mw_packed_attn_workspace_size(pack: Packed) -> int:
-    return int(load().mw_packed_attn_workspace_size(ctypes.byref(pack.desc)))
+    return int(load().mw_packed_attn_workspace_size(pack._ref))
 
 
 def mw_packed_attn_fwd(q, k, v, pack: Packed, scale=None, out=None, lse=None, workspace=None):
@@ -792,10 +800,10 @@ def mw_packed_attn_fwd(q, k, v, pack: Packed, scale=None, out=None, lse=None, wo
 
     With no workspace given, one of the size the library asks for is allocated here (torch)."""
     torch = _torch()
-    _check_packed(pack, (("q", q), ("out", out)), (("k", k), ("v", v)))
-    dev = pack.device
-    scale = 1.0 / math.sqrt(pack.desc.D) if scale is None else float(scale)
     o = torch.empty_like(q) if out is None else out
+    sq, so, sk, sv = _packed_views(pack, {"q": q, "out": o}, {"k": k, "v": v})
+    dev = pack.device
+    scale = pack.scale if scale is None else float(scale)
     lse = torch.empty(pack.lse_shape, dtype=torch.float32, device=dev) if lse is None else lse
     _check_lse(lse, pack.lse_shape, dev)
     if workspace is None:
@@ -803,13 +811,13 @@ def mw_packed_attn_fwd(q, k, v, pack: Packed, scale=None, out=None, lse=None, wo
         workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
     nbytes = _check_workspace(workspace, dev)
     with _on_device(dev):
-        _check(load().mw_packed_attn_fwd(_ptr(q), _ptr(k), _ptr(v), ctypes.byref(pack.desc), _ptr(o), _ptr(lse), scale,
-                                         _ptr(workspace), nbytes, _packed_strides(q, k, v, o), _stream_handle(dev)))
+        _check(load().mw_packed_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), pack._ref, o.data_ptr(), lse.data_ptr(), scale,
+                                         _ptr(workspace), nbytes, _packed_strides(sq, sk, sv, so), _stream_handle(dev)))
     return o, lse
 
 
 def mw_packed_attn_bwd_workspace_size(pack: Packed) -> int:
-    need = int(load().mw_packed_attn_bwd_workspace_size(ctypes.byref(pack.desc)))
+    need = int(load().mw_packed_attn_bwd_workspace_size(pack._ref))
     if need == 0:
         _check(MW_EINVAL)  # (planned without the backward)
     return need
@@ -819,23 +827,24 @@ def mw_packed_attn_bwd(q, k, v, o, d_o, lse, pack: Packed, scale=None, workspace
     """Backward of mw_packed_attn_fwd, for a batch planned with backward=True.  Returns (dq, dk, dv): bf16 [total_q,H,D]
     and twice [total_k,Hkv,D], the latter summed over the query heads that share a key head."""
     torch = _torch()
-    _check_packed(pack, (("q", q), ("o", o), ("d_o", d_o), ("dq", dq)), (("k", k), ("v", v), ("dk", dk), ("dv", dv)))
     dev = pack.device
-    if lse is None:
-        raise ValueError("lse is required")
-    _check_lse(lse, pack.lse_shape, dev)
-    scale = 1.0 / math.sqrt(pack.desc.D) if scale is None else float(scale)
-    if workspace is None:
-        workspace = torch.empty(mw_packed_attn_bwd_workspace_size(pack), dtype=torch.uint8, device=dev)
-    nbytes = _check_workspace(workspace, dev)
     # (a gradient of keys shared between heads does not share their strides)
     dq = torch.empty(pack.q_shape, dtype=q.dtype, device=dev) if dq is None else dq
     dk = torch.empty(pack.k_shape, dtype=q.dtype, device=dev) if dk is None else dk
     dv = torch.empty(pack.k_shape, dtype=q.dtype, device=dev) if dv is None else dv
+    sq, so, sdo, sdq, sk, sv, sdk, sdv = _packed_views(pack, {"q": q, "o": o, "d_o": d_o, "dq": dq},
+                                                       {"k": k, "v": v, "dk": dk, "dv": dv})
+    if lse is None:
+        raise ValueError("lse is required")
+    _check_lse(lse, pack.lse_shape, dev)
+    scale = pack.scale if scale is None else float(scale)
+    if workspace is None:
+        workspace = torch.empty(mw_packed_attn_bwd_workspace_size(pack), dtype=torch.uint8, device=dev)
+    nbytes = _check_workspace(workspace, dev)
     with _on_device(dev):
-        _check(load().mw_packed_attn_bwd(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(d_o), _ptr(lse), ctypes.byref(pack.desc),
-                                         _ptr(dq), _ptr(dk), _ptr(dv), scale, _ptr(workspace), nbytes,
-                                         _packed_strides(q, k, v, o, d_o, dq, dk, dv), _stream_handle(dev)))
+        _check(load().mw_packed_attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), d_o.data_ptr(), lse.data_ptr(),
+                                         pack._ref, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), scale, _ptr(workspace), nbytes,
+                                         _packed_strides(sq, sk, sv, so, sdo, sdq, sdk, sdv), _stream_handle(dev)))
     return dq, dk, dv
 
 
@@ -862,47 +871,52 @@ def mw_rope_apply(q, k, bands: mw_rope_bands, positions=None, first: int = 0, in
     back, which gives the gradients of q and k from those of the outputs.  positions: int32 or int64 on the GPU, [T] or
     [B,T], for bands of several axes [axes,T] or [axes,B,T]; None: first, first + 1, ...  Views with a contiguous
     head dimension are read and written in place; an output may be its input.  Returns (q_out, k_out)."""
-    torch = _torch()
-    B, H, T, D = q.shape if len(q.shape) == 4 else (0, 0, 0, 0)
-    dev = q.device
-    Hkv = 0
-    ts = [q] if q_out is None else [q, q_out]
-    if not _plain_views(ts, q.shape, q):
+    shape = q.shape
+    if not _plain_views((q,) if q_out is None else (q, q_out), shape, q):
         _bf16_4d("q", q, view=True)
-        _check_like("q_out", ts[-1], q.shape, dev)
+        if q_out is not None:
+            _check_like("q_out", q_out, shape, q.device)
+    B, H, T, D = shape
+    dev, Hkv = q.device, 0
     if k is not None:
-        shape = (B, k.shape[1] if len(k.shape) == 4 else 0, T, D)
-        Hkv = shape[1]
-        ts = [k] if k_out is None else [k, k_out]
-        if not _plain_views(ts, shape, q):
-            _check_like("k", k, shape, dev)
-            _check_like("k_out", ts[-1], shape, dev)
+        k_shape = (B, k.shape[1] if k.dim() == 4 else 0, T, D)
+        Hkv = k_shape[1]
+        if not _plain_views((k,) if k_out is None else (k, k_out), k_shape, q):
+            _check_like("k", k, k_shape, dev)
+            if k_out is not None:
+                _check_like("k_out", k_out, k_shape, dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    pos_strides, pos_bytes = None, 0
+    pos_strides, pos_bytes, pos = None, 0, 0
     if positions is not None:
-        p, axes = positions, bands.n_axes
-        if p.dtype not in (torch.int32, torch.int64) or p.device != dev:
-            raise ValueError("positions must be int32 or int64 on the device of q")
-        s, shape = p.stride(), tuple(p.shape)
-        if axes > 1:
-            if shape not in ((axes, T), (axes, B, T)):
-                raise ValueError(f"positions must be [axes,T] or [axes,B,T] = {(axes, B, T)}, got {shape}")
-            pos_strides = _strides_array((s[1] if len(s) == 3 else 0, s[0], s[-1]))
-        else:
-            if shape not in ((T,), (B, T)):
-                raise ValueError(f"positions must be [T] or [B,T] = {(B, T)}, got {shape}")
-            pos_strides = _strides_array((s[0] if len(s) == 2 else 0, 0, s[-1]))
-        pos_bytes = p.element_size()
-    q_out = torch.empty_like(q) if q_out is None else q_out
-    if k is not None and k_out is None:
-        k_out = torch.empty_like(k)
-    ks = (q, q_out) if k is None else (k, k_out)
+        pos, pos_bytes, pos_strides = _positions(positions, bands.n_axes, B, T, dev)
+    q_out = _torch().empty_like(q) if q_out is None else q_out
+    if k is None:
+        strides = _strides(q, q, q_out, q_out)
+    else:
+        k_out = _torch().empty_like(k) if k_out is None else k_out
+        strides = _strides(q, k, q_out, k_out)
     with _on_device(dev):
-        _check(load().mw_rope_apply(_ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), ctypes.byref(bands), _ptr(positions), pos_bytes,
-                                    pos_strides, operator.index(first), int(bool(inverse)), _strides(q, ks[0], q_out, ks[1]),
-                                    B, H, Hkv, T, D, _stream_handle(dev)))
+        _check(load().mw_rope_apply(q.data_ptr(), _ptr(k), q_out.data_ptr(), _ptr(k_out), ctypes.byref(bands), pos, pos_bytes,
+                                    pos_strides, first, 1 if inverse else 0, strides, B, H, Hkv, T, D, _stream_handle(dev)))
     return q_out, k_out
+
+
+def _positions(p, axes, B, T, dev):
+    """Address, bytes and strides (member, axis, token) of a tensor of positions."""
+    torch = _torch()
+    if p.dtype not in (torch.int32, torch.int64) or p.device != dev:
+        raise ValueError("positions must be int32 or int64 on the device of q")
+    s, shape = p.stride(), p.shape
+    if axes > 1:
+        if shape != (axes, T) and shape != (axes, B, T):
+            raise ValueError(f"positions must be [axes,T] or [axes,B,T] = {(axes, B, T)}, got {tuple(shape)}")
+        strides = (s[1] if len(s) == 3 else 0, s[0], s[-1])
+    else:
+        if shape != (T,) and shape != (B, T):
+            raise ValueError(f"positions must be [T] or [B,T] = {(B, T)}, got {tuple(shape)}")
+        strides = (s[0] if len(s) == 2 else 0, 0, s[-1])
+    return p.data_ptr(), p.element_size(), _strides_array(strides)
 
 
 # ----------------------------------------------------------------------------- paged 8-bit cache

@@ -48,7 +48,7 @@ UNITS = [  # (object name, source, extra flags)
     *((f"paged{d}", "attn_rows.hip", [f"-DMW_ROWS_HEAD_DIM={d}", "-DMW_ROWS_PAGED"]) for d in (64, 72, 128)),
     *((f"cross_bwd{d}", "attn_cross_bwd.hip", [f"-DMW_CROSS_HEAD_DIM={d}"]) for d in (64, 72, 128)),
     *((f"packed{d}", "attn_packed.hip", [f"-DMW_PACKED_HEAD_DIM={d}"]) for d in (64, 72, 128)),
-    *((f"packed_bwd{d}", "attn_packed_bwd.hip", [f"-DMW_PACKED_HEAD_DIM={d}"]) for d in (64, 72, 128)),
+    *((f"packed_bwd{d}", "attn_packed_bwd.hip", [f"-DMW_PACKED_HEAD_DIM={d}", "-DMW_SCALAR_LDS"]) for d in (64, 72, 128)),
     ("packed_plan", "packed_plan.hip", []),
     ("rope", "rope.hip", []),
     ("weigh", "weigh.hip", []),

@@ -33,4 +33,7 @@ __device__ __forceinline__ long long packed_offset(const Strides& s, int hk, int
   return (long long)(hk * G + (r - t * G)) * s.h + (long long)(q0 + t) * s.t;
 }
 
+// Workgroups of 256 threads, four columns each, that join a tile of n rows.
+constexpr int join_blocks(int n, int D) { return (n * (D / 4) + 255) / 256; }
+
 }  // namespace mw

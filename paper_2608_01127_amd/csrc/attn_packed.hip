@@ -147,13 +147,13 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_fwd_kernel(PackedParams p
 // sum 2^(m_s - M) l_s and LSE = (M + log2 of that sum) ln 2.  One thread for four columns of a row.
 template <int D, int BM>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p) {
-  constexpr int TPR = D / 4, BLOCKS = BM * TPR / 256;
+  constexpr int TPR = D / 4, BLOCKS = join_blocks(BM, D);
   const int job = blockIdx.x / BLOCKS, j = job / p.Hkv, hk = job - j * p.Hkv;
   if (j >= p.list[1]) return;
   const PackedJoin it = p.joins[j];
   const int x = (blockIdx.x - job * BLOCKS) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
   const int row = it.tile * BM + rt, G = p.G;
-  if (row >= it.nq * G) return;
+  if (rt >= BM || row >= it.nq * G) return;
   const float* ml = p.part + (long long)p.max_slots * p.Hkv * BM * D;
   float M = -INFINITY, l = 0.f;
   f32x4 acc = zero4();
@@ -204,8 +204,7 @@ hipError_t launch_fwd_tile(const PackedParams& p, const PackedList& list, hipStr
   constexpr int BM = 32 * NW / KG;
   if (list.tile != BM || list.step != BN * KG) return hipErrorInvalidValue;
   const long long grid = (long long)list.max_items * p.Hkv;
-  constexpr int per_join = BM * (kD / 4) / 256;
-  const long long joins = (long long)list.max_joins * p.Hkv * per_join;
+  const long long joins = (long long)list.max_joins * p.Hkv * join_blocks(BM, kD);
   if (grid > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidValue;
   hipLaunchKernelGGL((packed_fwd_kernel<kD, NW, BN, KG, WPS>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p);
   const hipError_t e = hipGetLastError();
@@ -219,7 +218,7 @@ hipError_t launch_fwd_tile(const PackedParams& p, const PackedList& list, hipStr
 #define MW_CAT_(a, b) a##b
 #define MW_CAT(a, b) MW_CAT_(a, b)
 hipError_t MW_CAT(launch_packed_fwd_, MW_PACKED_HEAD_DIM)(const PackedParams& p, const PackedList& list, hipStream_t stream) {
-  if (list.tile == 64) return launch_fwd_tile<4, 32, 2, 2>(p, list, stream);
+  if (list.kind == PackedTile::pairs) return launch_fwd_tile<4, 32, 2, 2>(p, list, stream);
   return launch_fwd_tile<4, 64, 1, kD == 128 ? 2 : 3>(p, list, stream);
 }
 

@@ -52,7 +52,12 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
     const int all = max(0, (int)((unsigned)(min(k0 + BN, n) - 1) / (unsigned)L) * L - (n - it.nq)) * G;
     bf16x8 kf[KK], vf[KK];
     const bf16_t* vfrag = Vs + (kw * VL * 64 + lane) * 8;
-    auto load_keys = [&] {
+    for (int f = wave; f < NWK * VL; f += NW) {  // V fragments in LDS, one a wave and round, as they lie in registers
+      const int w = f / (VL > 0 ? VL : 1), kk = f - w * VL;
+      const long long kr = it.k0 + min(k0 + w * 32 + (lane & 31), n - 1);
+      dma_lds_16(p.v + hk * p.sv.h + kr * p.sv.t + 16 * kk + 8 * (lane >> 5), lds_addr(Vs) + f * 1024);
+    }
+    {
       const long long kr = it.k0 + min(key, n - 1);
       const bf16_t* ka = p.k + hk * p.sk.h + kr * p.sk.t + 8 * (lane >> 5);
       const bf16_t* va = p.v + hk * p.sv.h + kr * p.sv.t + 8 * (lane >> 5);
@@ -60,17 +65,18 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
       for (int kk = 0; kk < KK; ++kk) {
         if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
           kf[kk] = *reinterpret_cast<const bf16x8*>(ka + 16 * kk);
-          vf[kk] = *reinterpret_cast<const bf16x8*>(va + 16 * kk);
+          if (kk >= VL) vf[kk] = *reinterpret_cast<const bf16x8*>(va + 16 * kk);
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) kf[kk][j] = vf[kk][j] = (__bf16)0.f;
         }
-        if (kk < VL && qg == 0) *reinterpret_cast<bf16x8*>(Vs + ((kw * VL + kk) * 64 + lane) * 8) = vf[kk];
       }
-    };
+    }
     const FragOffsets<D> fo(lane, gq * D);
     const Tail72 ft(lane, gq * D);
-    const RowOffsets<D, BS, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
+    // offsets of one query head's rows, held in registers where there are any to spare
+    constexpr bool HELD = D != 128 || QG == 1;
+    const RowOffsets<D, HELD ? BS : 32, NT> ro_q(p.sq.t, tid), ro_o(p.sdo.t, tid);
     const bf16_t* q0p = p.q + (long long)hk * G * p.sq.h + (long long)it.q0 * p.sq.t;
     const bf16_t* o0p = p.d_o + (long long)hk * G * p.sdo.h + (long long)it.q0 * p.sdo.t;
     const long long row_base = ((long long)hk * p.total_q + it.q0) * G;
@@ -78,9 +84,15 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
     const float* dlt = p.delta + row_base;
     const int beg = it.beg * BS, end = min(R, it.end * BS);
     auto stage = [&](int r0, int buf) {  // rows behind the sequence's last one repeat it
-      if (r0 + BS <= R && G == 1) {
-        stage_rows_s<D, BS, NT>(Qs[buf], q0p + r0 * p.sq.t, ro_q, tid);
-        stage_rows_s<D, BS, NT>(Os[buf], o0p + r0 * p.sdo.t, ro_o, tid);
+      bool done = false;
+      if constexpr (HELD) {
+        if (r0 + BS <= R && G == 1) {
+          stage_rows_s<D, BS, NT>(Qs[buf], uniform(q0p + r0 * p.sq.t), ro_q, tid);
+          stage_rows_s<D, BS, NT>(Os[buf], uniform(o0p + r0 * p.sdo.t), ro_o, tid);
+          done = true;
+        }
+      }
+      if (done) {
       } else if (r0 + BS <= R && p.near) {
         stage_group<D, BS, NT>(Qs[buf], q0p, p.sq, r0, G, p.magic, tid);
         stage_group<D, BS, NT>(Os[buf], o0p, p.sdo, r0, G, p.magic, tid);
@@ -161,8 +173,7 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
         }
       }
     };
-    stage(beg, 0);  // ahead of the keys, whose V fragments are waited for on their way into LDS
-    load_keys();
+    stage(beg, 0);
     wait_vmem();
     __syncthreads();
     int buf = 0, r0 = beg;
@@ -261,21 +272,24 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
     }
 }
 
-// dQ: NW waves of 32 rows each (Q and dO fragments, dQ^T in registers), walking the keys, BN a step.
-template <int D, int NW, int BN, int WPS>
+// dQ: NW waves in KG key groups of NW / KG waves of 32 rows each (Q and dO fragments, dQ^T in registers); a step stages
+// BN * KG keys, of which a group takes its BN, and the groups' dQ are added through LDS at the end.
+template <int D, int NW, int KG, int BN, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams p) {
-  constexpr int BM = 32 * NW, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
+  constexpr int NWR = NW / KG, BM = 32 * NWR, BS = BN * KG, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
-  constexpr int TE = stage_elems<D, BN, NT>();
+  constexpr int TE = stage_elems<D, BS, NT>();
   __shared__ __attribute__((aligned(16))) bf16_t lds[2][2][TE];
   bf16_t(*Ks)[TE] = lds[0];
   bf16_t(*Vs)[TE] = lds[1];
+  static_assert(KG == 1 || (KG / 2) * NWR * DB * 4096 <= (int)sizeof(lds), "the groups' sums fit the stages");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % NWR, kg = wave / NWR;
   int hk;
   PackedItem it;
   if (!work_item(p.list_q, p.Hkv, hk, it)) return;
   const int G = p.G, R = it.nq * G, n = it.nk, r0 = it.tile * BM;
-  const int row = r0 + wave * 32 + (lane & 31), rc = min(row, R - 1);
+  const int row = r0 + rw * 32 + (lane & 31), rc = min(row, R - 1);
   // This row's Q, dO and O, asked for before anything that waits: their latencies then pass together.
   bf16x8 qf[KK], of[KK], y[KK];
   {
@@ -305,14 +319,14 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
   const bf16_t* v0p = p.v + (long long)it.k0 * p.sv.t + hk * p.sv.h;
   const FragOffsets<D> fo(lane, 0);
   const Tail72 ft(lane, 0);
-  const RowOffsets<D, BN, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
+  const RowOffsets<D, BS, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
   auto stage = [&](int i, int buf) {  // keys behind the sequence's last one repeat it
-    const long long k0 = (long long)i * BN;
-    if (k0 + BN <= n) {
-      stage_rows_s<D, BN, NT>(Ks[buf], k0p + k0 * p.sk.t, ro_k, tid);
-      stage_rows_s<D, BN, NT>(Vs[buf], v0p + k0 * p.sv.t, ro_v, tid);
+    const long long k0 = (long long)i * BS;
+    if (k0 + BS <= n) {
+      stage_rows_s<D, BS, NT>(Ks[buf], k0p + k0 * p.sk.t, ro_k, tid);
+      stage_rows_s<D, BS, NT>(Vs[buf], v0p + k0 * p.sv.t, ro_v, tid);
     } else {
-      stage_kv_rows_direct<D, BN, NT>(Ks[buf], Vs[buf], [&](int r) -> RowPair {
+      stage_kv_rows_direct<D, BS, NT>(Ks[buf], Vs[buf], [&](int r) -> RowPair {
         const long long j = min(k0 + r, (long long)n - 1);
         return {k0p + j * p.sk.t, v0p + j * p.sv.t};
       }, tid);
@@ -331,7 +345,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
   // Rows of few keys: Delta = sum_j P_j dP_j of the probabilities at hand.  rowsum(dO O) has O's rounding to bf16, which
   // next to few keys' dP - Delta is not small (cross_dq_kernel); a tile whose first row sees at most a step of
   // keys is walked twice.
-  if (hi_all <= BN && it.slot < 0 && it.beg < it.end) {
+  if (hi_all <= 64 && it.slot < 0 && it.beg < it.end) {
     float sum = 0.f;
     for (int i = it.beg; i < it.end; ++i) {
       if (i > it.beg) {
@@ -340,7 +354,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
         __syncthreads();
       }
 #pragma unroll 1
-      for (int kq = 0; kq < BN / 32; ++kq) {
+      for (int kq = 0; kq < BS / 32; ++kq) {  // (each group forms the whole sum)
         f32x16 s = zero16(), dp = zero16();
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
@@ -349,7 +363,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const bool in = i * BN + kq * 32 + acc_row(j, lane) < hi;
+          const bool in = i * BS + kq * 32 + acc_row(j, lane) < hi;
           sum = fmaf(in ? fast_exp2(fmaf(s[j], c, -lse2)) : 0.f, in ? dp[j] : 0.f, sum);
         }
       }
@@ -362,7 +376,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
       __syncthreads();
     }
   }
-  if (it.beg == 0 && lane < 32 && row < R) {
+  if (it.beg == 0 && kg == 0 && lane < 32 && row < R) {
     const long long at = ((long long)hk * p.total_q + it.q0) * G + row;
     p.delta[at] = ndlt;
     p.lse2[at] = lse2;
@@ -377,13 +391,13 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
         f32x16 s = zero16(), dp = nd;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-          s = mfma32(fo.row8(Ks[buf], kq * 32, kk), qf[kk], s);
-          dp = mfma32(fo.row8(Vs[buf], kq * 32, kk), of[kk], dp);
+          s = mfma32(fo.row8(Ks[buf], kg * BN + kq * 32, kk), qf[kk], s);
+          dp = mfma32(fo.row8(Vs[buf], kg * BN + kq * 32, kk), of[kk], dp);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           float pv = fast_exp2(fmaf(s[i], c, -lse2));
-          if constexpr (decltype(masked)::value) pv = k0 + kq * 32 + acc_row(i, lane) < hi ? pv : 0.f;
+          if constexpr (decltype(masked)::value) pv = k0 + kg * BN + kq * 32 + acc_row(i, lane) < hi ? pv : 0.f;
           dp[i] *= pv;
         }
         bf16x8 h[2];
@@ -391,10 +405,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
         for (int t = 0; t < 2; ++t) {
           h[t] = pack8(dp, t);
 #pragma unroll
-          for (int db = 0; db < DB; ++db) dq[db] = mfma32(fo.tr8(Ks[buf], kq * 32, t, db), h[t], dq[db]);
+          for (int db = 0; db < DB; ++db) dq[db] = mfma32(fo.tr8(Ks[buf], kg * BN + kq * 32, t, db), h[t], dq[db]);
         }
         if constexpr (TAIL) {
-          const bf16x8 x = ft.read(Ks[buf], kq * 32);
+          const bf16x8 x = ft.read(Ks[buf], kg * BN + kq * 32);
           tail_operands(h[0], h[1]);
 #pragma unroll
           for (int e = 0; e < 2; ++e) tail[e] = mfma16(x, h[e], tail[e]);
@@ -405,22 +419,36 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
     auto run = [&](auto masked, int stop) {
       for (; i < stop; ++i) {
         if (i + 1 < it.end) stage(i + 1, buf ^ 1);
-        step(masked, i * BN, buf);
+        step(masked, i * BS, buf);
         wait_vmem();
         __syncthreads();
         buf ^= 1;
       }
     };
-    run(std::false_type{}, min(hi_all / BN, it.end));
+    run(std::false_type{}, min(hi_all / BS, it.end));
     run(std::true_type{}, it.end);
   }
+  if constexpr (KG > 1) {
+    float* m = reinterpret_cast<float*>(&lds[0][0][0]);
+    add_groups<KG, NWR>(dq, kg, rw, lane, m);
+    if constexpr (TAIL) {
+      f32x16 rest[1] = {zero16()};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rest[0][i] = tail[i / 4][i % 4];
+      add_groups<KG, NWR>(rest, kg, rw, lane, m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) tail[i / 4][i % 4] = rest[0][i];
+    }
+    __syncthreads();     // (the stages are written again below)
+    if (kg > 0) return;  // no barrier follows
+  }
   if (it.slot >= 0) {  // fp32 dQ of this range of the keys
-    float* part = p.part_q + (((long long)it.slot * p.Hkv + hk) * BM + wave * 32) * D;
+    float* part = p.part_q + (((long long)it.slot * p.Hkv + hk) * BM + rw * 32) * D;
     if constexpr (TAIL) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int r = 16 * e + (lane & 15);
-        if (lane < 32 && r0 + wave * 32 + r < R) *reinterpret_cast<f32x4*>(part + r * D + 64 + 4 * (lane >> 4)) = tail[e];
+        if (lane < 32 && r0 + rw * 32 + r < R) *reinterpret_cast<f32x4*>(part + r * D + 64 + 4 * (lane >> 4)) = tail[e];
       }
     }
     if (row >= R) return;
@@ -435,25 +463,25 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
       }
     return;
   }
-  // (every wave has passed the last barrier: a half stage holds the rows of BN / 32 waves)
-  static_assert(NW <= 2 * (BN / 32), "one stage holds the rows of every wave");
-  const int half = wave / (BN / 32);
-  store_rows<D>(dq, tail, (half ? Vs : Ks)[0] + (wave - half * (BN / 32)) * 32 * D, min(32, R - r0 - wave * 32), lane, p.scale,
-                [&](int r) { return p.dq + packed_offset(p.sdq, hk, G, it.q0, r0 + wave * 32 + r); });
+  // (every wave has passed the last barrier: a half stage holds the rows of BS / 32 waves)
+  static_assert(NWR <= 2 * (BS / 32), "one stage holds the rows of every wave");
+  const int half = rw / (BS / 32);
+  store_rows<D>(dq, tail, (half ? Vs : Ks)[0] + (rw - half * (BS / 32)) * 32 * D, min(32, R - r0 - rw * 32), lane, p.scale,
+                [&](int r) { return p.dq + packed_offset(p.sdq, hk, G, it.q0, r0 + rw * 32 + r); });
 }
 
 // Sums of the parts of cut tiles, in order: the first n_kv workgroups dK and dV, the others dQ.  One thread for four
 // columns of a row.
 template <int D, int BM, int BN>
 __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p, int n_kv) {
-  constexpr int TPR = D / 4, PER_K = BN * TPR / 256, PER_Q = BM * TPR / 256;
+  constexpr int TPR = D / 4, PER_K = join_blocks(BN, D), PER_Q = join_blocks(BM, D);
   if ((int)blockIdx.x < n_kv) {
     const int job = blockIdx.x / PER_K, j = job / p.Hkv, hk = job - j * p.Hkv;
     if (j >= p.list_k[1]) return;
     const PackedJoin it = p.joins_k[j];
     const int x = (blockIdx.x - job * PER_K) * 256 + threadIdx.x, kr = x / TPR, col = (x - kr * TPR) * 4;
     const int key = it.tile * BN + kr;
-    if (key >= it.nk) return;
+    if (kr >= BN || key >= it.nk) return;
     f32x4 k = zero4(), v = zero4();
 #pragma unroll 4
     for (int s = 0; s < it.parts; ++s) {
@@ -476,7 +504,7 @@ __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p,
   const PackedJoin it = p.joins_q[j];
   const int x = (b - job * PER_Q) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
   const int row = it.tile * BM + rt;
-  if (row >= it.nq * p.G) return;
+  if (rt >= BM || row >= it.nq * p.G) return;
   f32x4 q = zero4();
 #pragma unroll 4
   for (int s = 0; s < it.parts; ++s)
@@ -489,32 +517,55 @@ __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p,
 
 }  // namespace
 
-// The dK/dV kernel's tile: 128 keys in four waves; with two row groups of eight waves, whose barriers hold them all in step,
-// the 1B clips take 1993 for 1920 us, forward and backward, the text batch (D = 64) 399 for 381.
-template <int NWK_, int QG_, int BM_, int VL_, int WPS_>
-struct DkvTile {
-  static constexpr int NWK = NWK_, QG = QG_, BM = BM_, VL = VL_, WPS = WPS_;
-};
-using Dkv = DkvTile<4, 1, packed_dkv_step(kD), kD == 128 ? 6 : 0, kD == 64 ? 3 : 2>;
+namespace {
+
+template <int NW, int KG, int WPS>
+hipError_t launch_dq(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
+  constexpr int BN = 64 / KG;
+  if (s.dq.tile != 32 * NW / KG || s.dq.step != 64) return hipErrorInvalidValue;
+  const long long grid = (long long)s.dq.max_items * s.Hkv;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((packed_dq_kernel<kD, NW, KG, BN, WPS>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int NWK, int QG, int BM, int VL, int WPS>
+hipError_t launch_dkdv(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
+  if (s.dkv.tile != 32 * NWK || s.dkv.step != BM * QG) return hipErrorInvalidValue;
+  const long long grid = (long long)s.dkv.max_items * s.Hkv;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((packed_dkdv_kernel<kD, NWK, QG, BM, VL, WPS>), dim3((unsigned)grid), dim3(64 * NWK * QG), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int BM, int BN>
+hipError_t launch_join(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
+  const long long n_kv = (long long)s.dkv.max_joins * s.Hkv * join_blocks(BN, kD);
+  const long long n_q = (long long)s.dq.max_joins * s.Hkv * join_blocks(BM, kD);
+  if (n_kv + n_q > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (n_kv + n_q == 0) return hipSuccess;
+  hipLaunchKernelGGL((packed_bwd_join_kernel<kD, BM, BN>), dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);
+  return hipGetLastError();
+}
+
+}  // namespace
 
 #define MW_CAT_(a, b) a##b
 #define MW_CAT(a, b) MW_CAT_(a, b)
+// 128 keys in four waves: with two row groups of eight waves, whose barriers hold them all in step, the 1B clips take 1993 for
+// 1920 us, forward and backward, the text batch (D = 64) 399 for 381.
 hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
-  constexpr int NW = 4, BN = 32 * Dkv::NWK;
-  if (s.dq.tile != 32 * NW || s.dq.step != 64 || s.dkv.tile != BN || s.dkv.step != Dkv::BM * Dkv::QG) return hipErrorInvalidValue;
-  const long long grid_q = (long long)s.dq.max_items * s.Hkv, grid_k = (long long)s.dkv.max_items * s.Hkv;
-  const long long n_kv = (long long)s.dkv.max_joins * s.Hkv * (BN * (kD / 4) / 256);
-  const long long n_q = (long long)s.dq.max_joins * s.Hkv * (32 * NW * (kD / 4) / 256);
-  if (grid_q > 0x7fffffffLL || grid_k > 0x7fffffffLL || n_kv + n_q > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_dq_kernel<kD, NW, 64, kD == 128 ? 2 : 3>), dim3((unsigned)grid_q), dim3(64 * NW), 0, stream, p);
-  hipError_t e = hipGetLastError();
+  const bool wide_q = s.dq.kind == PackedTile::wide, wide_k = s.dkv.kind == PackedTile::wide;
+  hipError_t e = wide_q ? launch_dq<4, 1, kD == 64 ? 3 : 2>(p, s, stream) : launch_dq<4, 2, 2>(p, s, stream);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((packed_dkdv_kernel<kD, Dkv::NWK, Dkv::QG, Dkv::BM, Dkv::VL, Dkv::WPS>), dim3((unsigned)grid_k),
-                     dim3(64 * Dkv::NWK * Dkv::QG), 0, stream, p);
-  e = hipGetLastError();
-  if (e != hipSuccess || n_kv + n_q == 0) return e;
-  hipLaunchKernelGGL((packed_bwd_join_kernel<kD, 32 * NW, BN>), dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);
-  return hipGetLastError();
+  if (wide_k) {
+    e = launch_dkdv<4, 1, packed_dkv_step(kD, PackedTile::wide), kD == 128 ? 6 : 0, kD == 64 ? 3 : 2>(p, s, stream);
+  } else {
+    e = launch_dkdv<2, 2, 32, kD == 128 ? 7 : 0, 2>(p, s, stream);
+  }
+  if (e != hipSuccess) return e;
+  if (wide_q) return wide_k ? launch_join<128, 128>(p, s, stream) : launch_join<128, 64>(p, s, stream);
+  return wide_k ? launch_join<64, 128>(p, s, stream) : launch_join<64, 64>(p, s, stream);
 }
 
 }  // namespace mw

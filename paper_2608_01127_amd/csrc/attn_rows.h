@@ -426,21 +426,21 @@ struct CodeTile {
   }
 };
 
-// Stages ROWS rows of a key head's G > 1 query heads from row r0 on (StagePlan's pieces): from r0's token on, a piece's
+// Stages ROWS rows of a key head's G query heads from row r0 on (StagePlan's pieces): from r0's token on, a piece's
 // token and head are a few steps away, found without a division, and its bytes at a 32-bit offset (`near`).
 template <int D, int ROWS, int NT>
 __device__ __forceinline__ void stage_group(bf16_t* lds_tile, const bf16_t* base, const Strides& s, int r0, int G,
                                             unsigned magic, int tid) {
   using SP = StagePlan<D, ROWS, NT>;
-  const int t0 = (unsigned)r0 / (unsigned)G, skip = r0 - t0 * G;
-  base += (long long)t0 * s.t;
+  const int t0 = G == 1 ? r0 : (unsigned)r0 / (unsigned)G, skip = r0 - t0 * G;
+  base = uniform(base + (long long)t0 * s.t);
   const unsigned st = (unsigned)s.t * 2, sh = (unsigned)s.h * 2;
 #pragma unroll
   for (int it = 0; it < SP::ROUNDS; ++it) {
     const int ci0 = it * NT + tid;
     const int ci = (SP::PIECES % NT == 0 || ci0 < SP::PIECES) ? ci0 : 0;  // past the tile: row 0 again, into the slack
     const int row = ci / SP::SLOTS, ls = (ci % SP::SLOTS) ^ Tile<D>::swz(row);
-    const unsigned x = skip + row, t = __umulhi(x, magic);
+    const unsigned x = skip + row, t = G == 1 ? x : __umulhi(x, magic);
     dma_lds_16_s(base, t * st + (x - t * G) * sh + ls * 16, lds_addr(lds_tile) + it * NT * 16 + wave_stage_off(tid));
   }
 }

@@ -225,12 +225,22 @@ __device__ __forceinline__ unsigned wave_stage_off(int tid) {
   return __builtin_amdgcn_readfirstlane((unsigned)(tid & ~63) * 16u);
 }
 
+// The same in a scalar register.  An asm operand does not bring it back where the compiler has worked it out in a vector
+// one, as it does in the packed backward (units built with MW_SCALAR_LDS); the others' code is better without.
+__device__ __forceinline__ unsigned scalar(unsigned lds_dst) {
+#ifdef MW_SCALAR_LDS
+  return __builtin_amdgcn_readfirstlane(lds_dst);
+#else
+  return lds_dst;
+#endif
+}
+
 // `lds_dst` is the wave-uniform LDS byte address of the wave's 64 x 16 bytes.
 __device__ __forceinline__ void dma_lds_16(const void* src, unsigned lds_dst) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds_dst) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(scalar(lds_dst)) : "m0", "memory");
 }
 __device__ __forceinline__ void dma_lds_4(const void* src, unsigned lds_dst) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds_dst) : "m0", "memory");
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(scalar(lds_dst)) : "m0", "memory");
 }
 
 // Pieces of a ROWS x D tile staged by NT threads: whole rounds of NT, the last
@@ -272,8 +282,16 @@ __device__ __forceinline__ void stage_rows_direct(bf16_t* lds_tile, RowPtr row_p
 // 32-bit byte offset (the saddr form): a tile whose rows are equally spaced is
 // staged from one scalar base per tile and offsets computed once per kernel.
 __device__ __forceinline__ void dma_lds_16_s(const void* sbase, unsigned voff, unsigned lds_dst) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds_dst)
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(scalar(lds_dst))
                : "m0", "memory");
+}
+
+// A pointer that is the same in every lane, in scalar registers: what the saddr form needs, also where the compiler has
+// worked it out in vector ones.
+__device__ __forceinline__ const bf16_t* uniform(const bf16_t* p) {
+  const unsigned long long x = (unsigned long long)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)x), hi = __builtin_amdgcn_readfirstlane((unsigned)(x >> 32));
+  return (const bf16_t*)(((unsigned long long)hi << 32) | lo);
 }
 
 // Byte offsets, from the tile's first row, of the 16-byte pieces this thread

@@ -413,9 +413,13 @@ struct PackedItem {
 struct PackedJoin {
   int q0, nq, k0, nk, tile, first, parts, unused;
 };
+// Tiles of 128 rows (or keys), or of 64 in two groups of waves that share each step's keys (or rows), for grids that
+// would leave CUs idle.
+enum class PackedTile { wide, pairs };
 // The plan of a pass: a head of 8 words (items, cut tiles, slots), then its items, heaviest first, then its cut tiles.
 struct PackedList {
   bool keys;              // key tiles (dK, dV), or row tiles
+  PackedTile kind;        // the kernel's configuration
   int tile, step;         // rows and keys of a tile and a step, or keys and rows
   int min_steps;          // no item of a cut tile is much shorter
   int share;              // workgroups that one head's steps are divided among before a tile is cut
@@ -446,7 +450,7 @@ struct PackedParams {
   float scale_log2;
 };
 // Rows of a step of the dK/dV kernel.
-constexpr int packed_dkv_step(int D) { return D == 128 ? 32 : 64; }
+constexpr int packed_dkv_step(int D, PackedTile t) { return t == PackedTile::wide && D != 72 ? 32 : 64; }
 size_t packed_part_bytes(const PackedShape& s);
 hipError_t launch_packed_fwd_64(const PackedParams& p, const PackedList& list, hipStream_t stream);
 hipError_t launch_packed_fwd_72(const PackedParams& p, const PackedList& list, hipStream_t stream);

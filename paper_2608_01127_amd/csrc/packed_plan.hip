@@ -203,14 +203,23 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
 
 namespace {
 
+// Workgroups that run at once, two a CU: tiles are cut where that many would not have an even share.  (256, 768, 1024: one
+// token of 8 sequences 34.7, 42.5, 43.5 for 33.9 us; the text batch of 8192 tokens, forward and backward, 467, 401, 383 for
+// 368 us.)
+constexpr int kSlots = 512;
+// Keys (or rows) that an item of a cut tile walks at least.
+constexpr int kLeast = 512;
+
 // units: rows (or keys) of all sequences; walked: keys (or rows) that a tile's steps run over at most.
-void finish_list(PackedList& l, PackedShape& s, long long units, long long walked, int slots) {
-  l.share = std::max(1, slots / s.Hkv);
+void finish_list(PackedList& l, PackedShape& s, long long units, long long walked) {
+  l.share = std::max(1, kSlots / s.Hkv);
   l.max_tiles = (int)std::min<long long>(units / l.tile + s.N, 0x3fffffff);
   // parts = ceil(steps / target), target >= all steps / share: fewer than one for each tile and `share` more; of cut
   // tiles, which have more steps than target, at most twice steps / target
   l.max_items = l.max_tiles + l.share;
-  const long long steps = (walked + l.step - 1) / l.step, parts = (steps + l.min_steps - 1) / l.min_steps;
+  const long long steps = (walked + l.step - 1) / l.step;
+  if (walked <= 2 * kLeast) l.min_steps = (int)steps;  // what a cut would save, the join's launch costs
+  const long long parts = (steps + l.min_steps - 1) / l.min_steps;
   l.max_slots = parts > 1 ? (int)std::min<long long>(2 * l.share, parts * l.max_tiles) : 0;
   l.max_joins = parts > 1 ? std::min(l.share, l.max_tiles) : 0;
   l.at = s.words;
@@ -218,12 +227,13 @@ void finish_list(PackedList& l, PackedShape& s, long long units, long long walke
   s.n_lists += 1;
 }
 
-}  // namespace
+// Tiles of 64 up to this many of them over all heads, us as (128 | 64): forward, D = 128, 8 heads x 2900 27.3 | 25.1, 16 heads
+// on 4 x 1800 21.1 | 18.6, x 19200 402 | 480; D = 64, 16 on 4 x 4000 58.1 | 50.0; forward and backward, dQ and the forward in
+// 64, dK/dV as (128 | 64): D = 128, 8 x 2900 97.7 | 90.1, 12 x 3960 197 | 192; D = 64, 12 x 4000 173 | 163, 24 on 8 x 8192 368
+// | 384; D = 72, 16 x 4717, all three, 198 | 186.
+int packed_small(int D, bool keys) { return D == 128 ? 768 : (D == 72 ? 1400 : (keys ? 768 : 1536)); }
 
-// Workgroups that run at once, two a CU: tiles are cut where that many would not have an even share.  (256, 768, 1024: one
-// token of 8 sequences 34.7, 42.5, 43.5 for 33.9 us; the text batch of 8192 tokens, forward and backward, 467, 401, 383 for
-// 368 us.)
-constexpr int kSlots = 512;
+}  // namespace
 
 PackedShape packed_shape(int N, int H, int Hkv, int D, int L, int total_q, int total_k, bool backward) {
   PackedShape s{};
@@ -235,21 +245,18 @@ PackedShape packed_shape(int N, int H, int Hkv, int D, int L, int total_q, int t
   s.total_q = total_q;
   s.total_k = total_k;
   const long long rows = (long long)total_q * s.G;
-  // row tiles of 64 rows for batches of few rows a sequence (single tokens), else of 128
-  s.fwd.tile = rows <= 64LL * N ? 64 : 128;
-  s.fwd.step = 64;
-  s.fwd.min_steps = 8;
-  finish_list(s.fwd, s, rows, total_k, kSlots);
+  const auto add = [&](PackedList& l, bool keys, long long units, long long walked) {
+    l.keys = keys;
+    l.kind = (units / 64 + N) * Hkv <= packed_small(D, keys) ? PackedTile::pairs : PackedTile::wide;
+    l.tile = l.kind == PackedTile::pairs ? 64 : 128;
+    l.step = keys ? packed_dkv_step(D, l.kind) : 64;
+    l.min_steps = kLeast / l.step;
+    finish_list(l, s, units, walked);
+  };
+  add(s.fwd, false, rows, total_k);
   if (backward) {
-    s.dq.tile = 128;
-    s.dq.step = 64;
-    s.dq.min_steps = 8;
-    finish_list(s.dq, s, rows, total_k, kSlots);
-    s.dkv.keys = true;
-    s.dkv.tile = 128;
-    s.dkv.step = packed_dkv_step(D);
-    s.dkv.min_steps = 512 / s.dkv.step;
-    finish_list(s.dkv, s, total_k, rows, kSlots);
+    add(s.dq, false, rows, total_k);
+    add(s.dkv, true, total_k, rows);
   }
   s.words += (long long)s.n_lists * (N + 1);
   return s;

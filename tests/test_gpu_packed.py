@@ -135,6 +135,17 @@ def test_long_keys_of_few_rows_are_cut(mw, D):
 
 
 @pytest.mark.parametrize("D", [64, 72, 128])
+def test_cut_tiles_of_every_size_are_joined_whole(mw, D):
+    """Tiles of 64 and of 128 rows and keys, every row and key of them, cut along long keys or rows."""
+    for H, nk, nq in ((2, [6000], [64]), (1, [5000, 4000], [64, 63]), (2, [4100], [2050]), (1, [3000], [3000])):
+        pack = mw.Packed(edges(nq), sum(nq), H, 1, D, cu_k=edges(nk), total_k=sum(nk), backward=True)
+        assert mw.mw_packed_attn_workspace_size(pack) > 0
+        verify(mw, nk, H, 1, D, nq=nq, seed=sum(nk) + H)
+    verify(mw, [700, 64], 8, 1, D, seed=12)      # rows of many heads: key tiles are cut
+    verify(mw, [2000, 1100], 16, 8, D, seed=13)  # tiles of 128 at some widths
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
 @pytest.mark.parametrize("chunk", [1, 600])
 def test_long_sequences(mw, D, chunk):
     """Whole steps, steps on the diagonal and cut tiles of both directions."""
