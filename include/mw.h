@@ -524,8 +524,8 @@ int mw_packed_init(mw_packed* p, const int32_t* cu_q, const int32_t* cu_k, int32
  * strides  : 4 entries, for q, k, v, o (NULL = all contiguous): h and t as in mw_strides,
  *            t the stride of the tokens; b is not used
  * Rows of o and lse behind the last sequence are left as they were, and tokens behind it
- * are not read.  A key or value that a row does not see weighs 0 there, and has to be finite;
- * those of other sequences may hold anything.
+ * are not read.  A key or value that a row does not see weighs 0 there, and has to be finite
+ * (in the backward a row's q and d_o too); tokens of other sequences may hold anything.
  * Arithmetic as in mw_block_causal_attn_fwd.  The calling thread's current device must be
  * the device of the stream and of the tensors.
  * Errors: MW_EINVAL (null, p not initialised, workspace too small, scale not finite and

@@ -890,6 +890,8 @@ def mw_rope_apply(q, k, bands: mw_rope_bands, positions=None, first: int = 0, in
     pos_strides, pos_bytes, pos = None, 0, 0
     if positions is not None:
         pos, pos_bytes, pos_strides = _positions(positions, bands.n_axes, B, T, dev)
+    elif not -2**62 <= operator.index(first) < 2**62:
+        raise ValueError(f"{first} is out of range")
     q_out = _torch().empty_like(q) if q_out is None else q_out
     if k is None:
         strides = _strides(q, q, q_out, q_out)

@@ -385,6 +385,84 @@ def test_side_stream_and_graph_replays(mw):
                 assert torch.equal(a, b)
 
 
+def test_places_out_of_range_stay_within_the_tensors(mw):
+    """Lengths that overrun the tensors are cut, descending ones empty; what lies around the outputs is left alone."""
+    import torch
+    H, D, T = 2, 64, 100
+    wide = [torch.full((T + 200, H, D), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(4)]
+    o, dq, dk, dv = (w[100:100 + T] for w in wide)
+    q, k, v, do = (randn((T, H, D), 90 + i) for i in range(4))
+    cu = torch.tensor([-5, 50, 300, 20, 90, 2**31 - 1], device="cuda").to(torch.int32)
+    pack = mw.Packed(cu, T, H, H, D, backward=True)
+    lse = torch.full((H, T), 7.0, device="cuda")
+    mw.mw_packed_attn_fwd(q, k, v, pack, out=o, lse=lse)
+    mw.mw_packed_attn_bwd(q, k, v, o, do, lse, pack, dq=dq, dk=dk, dv=dv)
+    torch.cuda.synchronize()
+    for w in wide:
+        assert bool((w[:100] == 7).all()) and bool((w[100 + T:] == 7).all())
+    hidden = hidden_of(50, 50, 1)  # the first sequence is not touched by the others
+    check("o", o[:20, 0], *(x[:20] for x in attention64(q[:50, 0], k[:50, 0], v[:50, 0], hidden, D ** -0.5)["o"]))
+
+
+def test_two_plans_of_a_batch_give_the_same_bits(mw):
+    """Where the plan puts an item is decided by atomics, what the item computes is not."""
+    import torch
+    lens, H, Hkv, D = [3000, 2, 700, 0, 1111, 40], 4, 2, 128
+    T = sum(lens)
+    q, do = randn((T, H, D), 95), randn((T, H, D), 96)
+    k, v = randn((T, Hkv, D), 97), randn((T, Hkv, D), 98)
+    runs = []
+    for _ in range(3):
+        pack = mw.Packed(edges(lens), T, H, Hkv, D, backward=True)
+        o, lse = mw.mw_packed_attn_fwd(q, k, v, pack)
+        runs.append((o, lse, *mw.mw_packed_attn_bwd(q, k, v, o, do, lse, pack)))
+    torch.cuda.synchronize()
+    for other in runs[1:]:
+        for a, b in zip(runs[0], other):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_heads_far_apart(mw, D):
+    """Query heads of a key head more than 2^32 bytes apart read as their copies."""
+    import torch
+    T, H, far = 200, 3, 2**30 + 64
+    big = [torch.empty(2 * far + T * D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    q, do = (b.as_strided((T, H, D), (D, far, 1)) for b in big)
+    q.copy_(randn((T, H, D), 101))
+    do.copy_(randn((T, H, D), 102))
+    k, v = randn((T, 1, D), 103), randn((T, 1, D), 104)
+    pack = mw.Packed(edges([150, 50]), T, H, 1, D, backward=True)
+    runs = []
+    for x, y in ((q, do), (q.contiguous(), do.contiguous())):
+        o, lse = mw.mw_packed_attn_fwd(x, k, v, pack, out=torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda"))
+        runs.append((o, lse, *mw.mw_packed_attn_bwd(x, k, v, o, y, lse, pack)))
+    torch.cuda.synchronize()
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits(mw):
+    """Keys of more than 2^32 bytes: single tokens at the end of a long and of a short sequence."""
+    import torch
+    Hkv, D, nk = 16, 128, [1_100_000, 777]
+    Tk = sum(nk)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    k, v = (torch.empty((Tk, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (k, v):
+        for i in range(0, Tk, 1 << 17):
+            t[i:i + (1 << 17)] = torch.randn((min(Tk, i + (1 << 17)) - i, Hkv, D), device="cuda", generator=g).bfloat16()
+    q = randn((4, 32, D), 8)
+    pack = mw.Packed(edges([1, 3]), 4, 32, Hkv, D, cu_k=edges(nk), total_k=Tk)
+    o, lse = mw.mw_packed_attn_fwd(q, k, v, pack)
+    torch.cuda.synchronize()
+    for i, j, h in ((slice(0, 1), slice(0, nk[0]), 31), (slice(1, 4), slice(nk[0], Tk), 0), (slice(1, 4), slice(nk[0], Tk), 31)):
+        n = j.stop - j.start
+        want = attention64(q[i, h], k[j, h // 2], v[j, h // 2], hidden_of(i.stop - i.start, n, 1), D ** -0.5)
+        check(f"o {h}", o[i, h], *want["o"])
+        check(f"lse {h}", lse[h, i], *want["lse"])
+
+
 def test_refusals_of_the_binding(mw):
     import torch
     T, H, D = 10, 2, 64

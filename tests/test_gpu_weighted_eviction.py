@@ -96,6 +96,63 @@ def test_rows_that_weigh_nothing(mw, D):
 
 
 @pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("H,Hkv,T", [(8, 8, 600), (6, 2, 400), (5, 1, 77)])
+def test_rows_staged_for_several_blocks(mw, D, H, Hkv, T):
+    """One query head to a key head, an odd number of them; strided rows, a last step partly filled, lengths that end
+    within a group of blocks."""
+    cache, model = make(mw, 260, Hkv, 128, D, 3, 80)
+    for s, m in enumerate((9001, 130, 4000)):
+        k, v = randn((1, Hkv, m, D), 70 + s), randn((1, Hkv, m, D), 80 + s)
+        mw.mw_kvpages_append(cache, [s], k, v)
+        model.append([s], k, v)
+    q = randn((3, H, T, D), 61, "bthd")
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, [2, 0, 1], want_lse=True)
+    lse[0, 0, ::7] = -math.inf
+    weights_of(mw, cache, model, [2, 0, 1], q, lse, H, old=0.5)
+
+
+def test_pages_beyond_32_bits(mw):
+    """A pool of more than 2^32 bytes: weights and eviction of a sequence in its last pages."""
+    import torch
+    H, D, L, n = 16, 128, 640, 60_000
+    cache = mw.KVPages(3900, H, L, D, 2, 3800)
+    k, v = randn((1, H, n, D), 1), randn((1, H, n, D), 2)
+    for _ in range(40):  # 2.4 million tokens in front
+        mw.mw_kvpages_append(cache, [0], k, v)
+    model = Model(cache, 3900, H, L, D, 2, 3800)
+    model.rows[0], model.lens[0] = list(range(3750)), 2_400_000
+    x, y = tokens((1, H, 1500, D), 3), tokens((1, H, 1500, D), 4)
+    mw.mw_kvpages_append(cache, [1], x, y)
+    model.append([1], x, y)
+    assert cache.page_of(1, 0) == 3750 and 3750 * H * L * D > 2**32
+    q = (randn((1, H, 90, D), 5).float() / 64).bfloat16()
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, 90, cache, [1], want_lse=True)
+    w = torch.zeros((2, 3800 * L), device="cuda")
+    mw.mw_kvpages_weigh(cache, [1], q, lse, w)
+    torch.cuda.synchronize()
+    kk = model.values(1)[0]
+    want = torch.zeros(1500, dtype=torch.float64, device="cuda")
+    for h in range(H):
+        want += torch.softmax(q[0, h].double() @ kk[h].t() * D ** -0.5, -1).sum(0)
+    # (scores of up to 2^7 in 32 bits: 2^-16 of a weight)
+    assert bool(((w[1, :1500].double() - want).abs() <= 2.0 ** -14 * want + 1e-30).all())
+    before = w.clone()
+    mw.mw_kvpages_evict_weighted(cache, [1], w, 700, first=100, recent=50)
+    torch.cuda.synchronize()
+    stay = torch.tensor(kept(before[1, :1500].tolist(), 1500, 700, 100, 50), device="cuda")
+    assert torch.equal(w[1, :700], before[1][stay]) and not bool(w[1, 700:].any())
+    assert [cache.page_of(1, i) for i in range(2)] == [3753, 3754] and cache.len(1) == 700 and cache.n_free == 3900 - 3752
+    old = kk[:, stay]
+    for p, at in ((3753, 0), (3754, 640)):
+        m = min(640, 700 - at)
+        scale = cache.k_scales[p].double().repeat_interleave(BLOCK, -1)[:, :m, None]
+        got = cache.k_pages[p, :, :m].view(torch.float8_e4m3fn).double() * scale
+        exact = old[:, at:at + m]
+        # codes change only where a finer block's become subnormal in the new one: half a step of 2^-9 of its scale
+        assert bool(((got - exact).abs() <= 2.0 ** -10 * scale).all())
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
 @pytest.mark.parametrize("n", [70, 3000])
 def test_many_rows_are_divided(mw, D, n):
     """Rows of a call divided among workgroups, and not (no workspace of that size); two members of unlike lengths."""
