@@ -7,7 +7,7 @@ namespace mw {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kEach = 16, kBins = 256, kCopies = 32;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kEach = 16, kBins = 256, kCopies = 32, kFew = 64;
 
 // Order of the weights as unsigned numbers; -0 is 0, NaN is the lightest.
 __device__ __forceinline__ unsigned order_of(float w) {
@@ -22,14 +22,15 @@ __device__ __forceinline__ unsigned order_of(float w) {
 // front: the weight of the k-th is found by four counts of 8 bits, from the top; with the numbers of heavier and equal ones in
 // front of it, every token knows whether it stays and where.  A thread holds 16 tokens' weights in registers, every 1024th;
 // more tokens than that are read again for each count.  Weights that lie close fall into few bins: each bin has a counter
-// for every lane of a half wave, on a bank of its own.  Bound by its own latencies, one after another: 13 us for 2700 tokens,
-// 20 for 12900 (walking them a wave a stretch, looking up pages on the way: 25).
+// for every lane of a half wave, on a bank of its own.  Bound by its own latencies, one after another: 12 us for 2700 tokens,
+// 18 for 12900 (walking them a wave a stretch, looking up pages on the way: 25; without the ranking of the last few 20).
 __global__ __launch_bounds__(kThreads) void keep_select_kernel(PagePool c, KeepArgs a, const float* __restrict__ weights,
                                                                int2* __restrict__ list, float* __restrict__ kept) {
   __shared__ int bins[kBins * kCopies];
   __shared__ int counts[kBins];
   __shared__ int heavier[kEach * kWaves + 1], equal[kEach * kWaves + 1];
-  __shared__ int chosen, above;
+  __shared__ unsigned few[kFew];
+  __shared__ int chosen, above, n_few;
   static_assert(kEach * kWaves == 256, "one wave adds up the counts, four a lane");
   const int job = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int seq = a.seq[job], len = a.len[job], n = len - a.recent - a.first, k = a.keep - a.recent - a.first;
@@ -112,6 +113,38 @@ __global__ __launch_bounds__(kThreads) void keep_select_kernel(PagePool c, KeepA
     __syncthreads();
     limit |= (unsigned)chosen << shift;
     left -= above;
+    if (counts[chosen] > kFew || shift == 0) continue;
+    // few are left to choose from: each of them is ranked among them
+    if (tid == 0) n_few = 0;
+    __syncthreads();
+    for (int c0 = 0; c0 < n; c0 += CHUNK) {
+      if (!once) load(c0);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        const unsigned x = order_of(v[j]);
+        if (c0 + j * kThreads + tid < n && (x >> shift) == (limit >> shift)) few[atomicAdd(&n_few, 1)] = x;
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const int m = n_few;
+      const unsigned x = few[lane < m ? lane : 0];
+      int heavier_few = 0, equal_few = 0;
+      for (int i = 0; i < m; ++i) {
+        const unsigned y = __shfl(x, i);
+        heavier_few += y > x;
+        equal_few += y == x;
+      }
+      // the left-th (lanes of equal values agree)
+      if (lane < m && heavier_few < left && heavier_few + equal_few >= left) {
+        few[0] = x;
+        above = heavier_few;
+      }
+    }
+    __syncthreads();
+    limit = few[0];
+    left -= above;
+    break;
   }
 
   int gt0 = 0, eq0 = 0;  // heavier and equal tokens of the chunks in front
