@@ -35,5 +35,8 @@ __device__ __forceinline__ long long packed_offset(const Strides& s, int hk, int
 
 // Workgroups of 256 threads, four columns each, that join a tile of n rows.
 constexpr int join_blocks(int n, int D) { return (n * (D / 4) + 255) / 256; }
+// How many tiles are cut only the device knows: at most that many workgroups take what there is in turns.  (One workgroup
+// for each that there could be, 8192 of 19200 prompt tokens, most of them empty: the call 406 for 404 us.)
+constexpr int kJoinGrid = 1024;
 
 }  // namespace mw

@@ -148,52 +148,54 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_fwd_kernel(PackedParams p
 template <int D, int BM>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedParams p) {
   constexpr int TPR = D / 4, BLOCKS = join_blocks(BM, D);
-  const int job = blockIdx.x / BLOCKS, j = job / p.Hkv, hk = job - j * p.Hkv;
-  if (j >= p.list[1]) return;
-  const PackedJoin it = p.joins[j];
-  const int x = (blockIdx.x - job * BLOCKS) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
-  const int row = it.tile * BM + rt, G = p.G;
-  if (rt >= BM || row >= it.nq * G) return;
-  const float* ml = p.part + (long long)p.max_slots * p.Hkv * BM * D;
-  float M = -INFINITY, l = 0.f;
-  f32x4 acc = zero4();
-  constexpr int U = 4;  // partial results in flight
-  for (int s0 = 0; s0 < it.parts; s0 += U) {
-    float mv[U], lv[U];
-    f32x4 v[U];
+  const int n = p.list[1] * p.Hkv * BLOCKS;
+  for (int id = blockIdx.x; id < n; id += gridDim.x) {
+    const int job = id / BLOCKS, j = job / p.Hkv, hk = job - j * p.Hkv;
+    const PackedJoin it = p.joins[j];
+    const int x = (id - job * BLOCKS) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
+    const int row = it.tile * BM + rt, G = p.G;
+    if (rt >= BM || row >= it.nq * G) continue;
+    const float* ml = p.part + (long long)p.max_slots * p.Hkv * BM * D;
+    float M = -INFINITY, l = 0.f;
+    f32x4 acc = zero4();
+    constexpr int U = 4;  // partial results in flight
+    for (int s0 = 0; s0 < it.parts; s0 += U) {
+      float mv[U], lv[U];
+      f32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = s0 + u < it.parts;
-      const long long at = ((long long)(it.first + (in ? s0 + u : s0)) * p.Hkv + hk) * BM + rt;
-      mv[u] = in ? ml[2 * at] : -INFINITY;
-      lv[u] = ml[2 * at + 1];
-      v[u] = *reinterpret_cast<const f32x4*>(p.part + at * D + col);
+      for (int u = 0; u < U; ++u) {
+        const bool in = s0 + u < it.parts;
+        const long long at = ((long long)(it.first + (in ? s0 + u : s0)) * p.Hkv + hk) * BM + rt;
+        mv[u] = in ? ml[2 * at] : -INFINITY;
+        lv[u] = ml[2 * at + 1];
+        v[u] = *reinterpret_cast<const f32x4*>(p.part + at * D + col);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, mv[u]);
+      const float a = M == -INFINITY ? 0.f : fast_exp2(M - Mn);
+      l *= a;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] *= a;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = mv[u] == -INFINITY ? 0.f : fast_exp2(mv[u] - Mn);
+        l = fmaf(w, lv[u], l);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, v[u][c], acc[c]);
+      }
+      M = Mn;
     }
-    float Mn = M;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16x4 w;
 #pragma unroll
-    for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, mv[u]);
-    const float a = M == -INFINITY ? 0.f : fast_exp2(M - Mn);
-    l *= a;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] *= a;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float w = mv[u] == -INFINITY ? 0.f : fast_exp2(mv[u] - Mn);
-      l = fmaf(w, lv[u], l);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] = fmaf(w, v[u][c], acc[c]);
+    for (int c = 0; c < 4; ++c) w[c] = to_bf16(acc[c] * inv);
+    *reinterpret_cast<bf16x4*>(p.o + packed_offset(p.so, hk, G, it.q0, row) + col) = w;
+    if (col == 0) {
+      const int t = row / G;
+      p.lse[(long long)(hk * G + (row - t * G)) * p.total_q + it.q0 + t] =
+          l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994530942f;
     }
-    M = Mn;
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  bf16x4 w;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) w[c] = to_bf16(acc[c] * inv);
-  *reinterpret_cast<bf16x4*>(p.o + packed_offset(p.so, hk, G, it.q0, row) + col) = w;
-  if (col == 0) {
-    const int t = row / G;
-    p.lse[(long long)(hk * G + (row - t * G)) * p.total_q + it.q0 + t] =
-        l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994530942f;
   }
 }
 
@@ -204,8 +206,8 @@ hipError_t launch_fwd_tile(const PackedParams& p, const PackedList& list, hipStr
   constexpr int BM = 32 * NW / KG;
   if (list.tile != BM || list.step != BN * KG) return hipErrorInvalidValue;
   const long long grid = (long long)list.max_items * p.Hkv;
-  const long long joins = (long long)list.max_joins * p.Hkv * join_blocks(BM, kD);
-  if (grid > 0x7fffffffLL || joins > 0x7fffffffLL) return hipErrorInvalidValue;
+  const long long joins = std::min((long long)list.max_joins * p.Hkv * join_blocks(BM, kD), (long long)kJoinGrid);
+  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
   hipLaunchKernelGGL((packed_fwd_kernel<kD, NW, BN, KG, WPS>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.part == nullptr) return e;

@@ -470,49 +470,49 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
                 [&](int r) { return p.dq + packed_offset(p.sdq, hk, G, it.q0, r0 + rw * 32 + r); });
 }
 
-// Sums of the parts of cut tiles, in order: the first n_kv workgroups dK and dV, the others dQ.  One thread for four
-// columns of a row.
+// Sums of the parts of cut tiles, in order: dK and dV, then dQ.  One thread for four columns of a row.
 template <int D, int BM, int BN>
-__global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p, int n_kv) {
+__global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p) {
   constexpr int TPR = D / 4, PER_K = join_blocks(BN, D), PER_Q = join_blocks(BM, D);
-  if ((int)blockIdx.x < n_kv) {
-    const int job = blockIdx.x / PER_K, j = job / p.Hkv, hk = job - j * p.Hkv;
-    if (j >= p.list_k[1]) return;
-    const PackedJoin it = p.joins_k[j];
-    const int x = (blockIdx.x - job * PER_K) * 256 + threadIdx.x, kr = x / TPR, col = (x - kr * TPR) * 4;
-    const int key = it.tile * BN + kr;
-    if (kr >= BN || key >= it.nk) return;
-    f32x4 k = zero4(), v = zero4();
+  const int n_kv = p.list_k[1] * p.Hkv * PER_K, n = n_kv + p.list_q[1] * p.Hkv * PER_Q;
+  for (int id = blockIdx.x; id < n; id += gridDim.x) {
+    if (id < n_kv) {
+      const int job = id / PER_K, j = job / p.Hkv, hk = job - j * p.Hkv;
+      const PackedJoin it = p.joins_k[j];
+      const int x = (id - job * PER_K) * 256 + threadIdx.x, kr = x / TPR, col = (x - kr * TPR) * 4;
+      const int key = it.tile * BN + kr;
+      if (kr >= BN || key >= it.nk) continue;
+      f32x4 k = zero4(), v = zero4();
 #pragma unroll 4
-    for (int s = 0; s < it.parts; ++s) {
-      const float* y = p.part_k + ((long long)(it.first + s) * p.Hkv + hk) * 2 * BN * D + kr * D + col;
-      k += *reinterpret_cast<const f32x4*>(y);
-      v += *reinterpret_cast<const f32x4*>(y + BN * D);
-    }
-    bf16x4 wk, wv;
+      for (int s = 0; s < it.parts; ++s) {
+        const float* y = p.part_k + ((long long)(it.first + s) * p.Hkv + hk) * 2 * BN * D + kr * D + col;
+        k += *reinterpret_cast<const f32x4*>(y);
+        v += *reinterpret_cast<const f32x4*>(y + BN * D);
+      }
+      bf16x4 wk, wv;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      wk[c] = to_bf16(k[c] * p.scale);
-      wv[c] = to_bf16(v[c]);
+      for (int c = 0; c < 4; ++c) {
+        wk[c] = to_bf16(k[c] * p.scale);
+        wv[c] = to_bf16(v[c]);
+      }
+      *reinterpret_cast<bf16x4*>(p.dk + hk * p.sdk.h + (long long)(it.k0 + key) * p.sdk.t + col) = wk;
+      *reinterpret_cast<bf16x4*>(p.dv + hk * p.sdv.h + (long long)(it.k0 + key) * p.sdv.t + col) = wv;
+      continue;
     }
-    *reinterpret_cast<bf16x4*>(p.dk + hk * p.sdk.h + (long long)(it.k0 + key) * p.sdk.t + col) = wk;
-    *reinterpret_cast<bf16x4*>(p.dv + hk * p.sdv.h + (long long)(it.k0 + key) * p.sdv.t + col) = wv;
-    return;
+    const int b = id - n_kv, job = b / PER_Q, j = job / p.Hkv, hk = job - j * p.Hkv;
+    const PackedJoin it = p.joins_q[j];
+    const int x = (b - job * PER_Q) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
+    const int row = it.tile * BM + rt;
+    if (rt >= BM || row >= it.nq * p.G) continue;
+    f32x4 q = zero4();
+#pragma unroll 4
+    for (int s = 0; s < it.parts; ++s)
+      q += *reinterpret_cast<const f32x4*>(p.part_q + (((long long)(it.first + s) * p.Hkv + hk) * BM + rt) * D + col);
+    bf16x4 w;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = to_bf16(q[c] * p.scale);
+    *reinterpret_cast<bf16x4*>(p.dq + packed_offset(p.sdq, hk, p.G, it.q0, row) + col) = w;
   }
-  const int b = blockIdx.x - n_kv, job = b / PER_Q, j = job / p.Hkv, hk = job - j * p.Hkv;
-  if (j >= p.list_q[1]) return;
-  const PackedJoin it = p.joins_q[j];
-  const int x = (b - job * PER_Q) * 256 + threadIdx.x, rt = x / TPR, col = (x - rt * TPR) * 4;
-  const int row = it.tile * BM + rt;
-  if (rt >= BM || row >= it.nq * p.G) return;
-  f32x4 q = zero4();
-#pragma unroll 4
-  for (int s = 0; s < it.parts; ++s)
-    q += *reinterpret_cast<const f32x4*>(p.part_q + (((long long)(it.first + s) * p.Hkv + hk) * BM + rt) * D + col);
-  bf16x4 w;
-#pragma unroll
-  for (int c = 0; c < 4; ++c) w[c] = to_bf16(q[c] * p.scale);
-  *reinterpret_cast<bf16x4*>(p.dq + packed_offset(p.sdq, hk, p.G, it.q0, row) + col) = w;
 }
 
 }  // namespace
@@ -540,11 +540,11 @@ hipError_t launch_dkdv(const PackedBwdParams& p, const PackedShape& s, hipStream
 
 template <int BM, int BN>
 hipError_t launch_join(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
-  const long long n_kv = (long long)s.dkv.max_joins * s.Hkv * join_blocks(BN, kD);
-  const long long n_q = (long long)s.dq.max_joins * s.Hkv * join_blocks(BM, kD);
-  if (n_kv + n_q > 0x7fffffffLL) return hipErrorInvalidValue;
-  if (n_kv + n_q == 0) return hipSuccess;
-  hipLaunchKernelGGL((packed_bwd_join_kernel<kD, BM, BN>), dim3((unsigned)(n_kv + n_q)), dim3(256), 0, stream, p, (int)n_kv);
+  const long long n =
+      (long long)s.Hkv * (s.dkv.max_joins * join_blocks(BN, kD) + s.dq.max_joins * join_blocks(BM, kD));
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL((packed_bwd_join_kernel<kD, BM, BN>), dim3((unsigned)std::min(n, (long long)kJoinGrid)), dim3(256), 0,
+                     stream, p);
   return hipGetLastError();
 }
 
