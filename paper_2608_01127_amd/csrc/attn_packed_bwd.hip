@@ -21,6 +21,11 @@ constexpr int kD = MW_PACKED_HEAD_DIM;
 // BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
 // first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
 // the registers).  Lanes behind the last key repeat it and store nothing.
+//
+// Bound by the matrix products, 8 D a pair of the 14 D of the backward (S and dP are formed in both kernels, so that neither
+// has to add to memory that others add to), with two waves a SIMD: clips of 600 to 9600 tokens, 19200 in all, 12 heads, D =
+// 128, 890 to 970 us, 945 TF executed, matrix units 56% busy at 1.62 GHz, which is what the power limit leaves.  D = 64 (24
+// heads on 8, 8192 tokens) 169 us, 860 TF: 1072 workgroups over 768 places.
 template <int D, int NWK, int QG, int BM, int VL, int WPS>
 __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedBwdParams p) {
   constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
@@ -274,6 +279,8 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
 
 // dQ: NW waves in KG key groups of NW / KG waves of 32 rows each (Q and dO fragments, dQ^T in registers); a step stages
 // BN * KG keys, of which a group takes its BN, and the groups' dQ are added through LDS at the end.
+// Bound by the matrix products, 6 D a pair, as above: the clips 635 to 690 us, 1011 TF executed, matrix units 60% busy at
+// 1.62 GHz; the 8192 tokens of D = 64 115 us, 944 TF; 4717 tokens of 16 heads, D = 72, 65 us, 790 TF.
 template <int D, int NW, int KG, int BN, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams p) {
   constexpr int NWR = NW / KG, BM = 32 * NWR, BS = BN * KG, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
@@ -470,7 +477,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
                 [&](int r) { return p.dq + packed_offset(p.sdq, hk, G, it.q0, r0 + rw * 32 + r); });
 }
 
-// Sums of the parts of cut tiles, in order: dK and dV, then dQ.  One thread for four columns of a row.
+// Sums of the parts of cut tiles, in order: dK and dV, then dQ.  One thread for four columns of a row.  5 us where little is
+// cut; 9 for the 8192 tokens above, whose parts (16 MB) it reads at 1.9 TB/s.
 template <int D, int BM, int BN>
 __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p) {
   constexpr int TPR = D / 4, PER_K = join_blocks(BN, D), PER_Q = join_blocks(BM, D);
@@ -556,12 +564,14 @@ hipError_t launch_join(const PackedBwdParams& p, const PackedShape& s, hipStream
 // 1920 us, forward and backward, the text batch (D = 64) 399 for 381.
 hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
   const bool wide_q = s.dq.kind == PackedTile::wide, wide_k = s.dkv.kind == PackedTile::wide;
-  hipError_t e = wide_q ? launch_dq<4, 1, kD == 64 ? 3 : 2>(p, s, stream) : launch_dq<4, 2, 2>(p, s, stream);
+  constexpr PackedTile W = PackedTile::wide, P = PackedTile::pairs;
+  constexpr PackedPass DQ = PackedPass::dq, KV = PackedPass::dkdv;
+  hipError_t e = wide_q ? launch_dq<4, 1, packed_per_cu(DQ, kD, W)>(p, s, stream) : launch_dq<4, 2, packed_per_cu(DQ, kD, P)>(p, s, stream);
   if (e != hipSuccess) return e;
   if (wide_k) {
-    e = launch_dkdv<4, 1, packed_dkv_step(kD, PackedTile::wide), kD == 128 ? 6 : 0, kD == 64 ? 3 : 2>(p, s, stream);
+    e = launch_dkdv<4, 1, packed_dkv_step(kD, W), kD == 128 ? 6 : 0, packed_per_cu(KV, kD, W)>(p, s, stream);
   } else {
-    e = launch_dkdv<2, 2, 32, kD == 128 ? 7 : 0, 2>(p, s, stream);
+    e = launch_dkdv<2, 2, 32, kD == 128 ? 7 : 0, packed_per_cu(KV, kD, P)>(p, s, stream);
   }
   if (e != hipSuccess) return e;
   if (wide_q) return wide_k ? launch_join<128, 128>(p, s, stream) : launch_join<128, 64>(p, s, stream);

@@ -445,8 +445,8 @@ __device__ __forceinline__ void stage_group(bf16_t* lds_tile, const bf16_t* base
   }
 }
 
-// LDS of a dK/dV kernel (NWK key waves in QG row groups of BM rows a step): Q and dO tiles of BS rows, LSE and -Delta of those rows (two stages each), then VL V
-// fragments of each key wave.
+// LDS of a dK/dV kernel (NWK key waves in QG row groups of BM rows a step): Q and dO tiles of BS rows, LSE and -Delta of
+// those rows (two stages each), then VL V fragments of each key wave.
 template <int D, int NWK, int QG, int BM, int VL>
 struct KeyTileLds {
   static constexpr int NT = 64 * NWK * QG, BS = BM * QG;

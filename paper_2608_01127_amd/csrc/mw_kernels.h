@@ -416,6 +416,11 @@ struct PackedJoin {
 // Tiles of 128 rows (or keys), or of 64 in two groups of waves that share each step's keys (or rows), for grids that
 // would leave CUs idle.
 enum class PackedTile { wide, pairs };
+// Workgroups that a CU runs at once (of four waves each, so waves a SIMD).
+enum class PackedPass { fwd, dq, dkdv };
+constexpr int packed_per_cu(PackedPass pass, int D, PackedTile t) {
+  return t == PackedTile::wide && (D == 64 || (D == 72 && pass == PackedPass::fwd)) ? 3 : 2;
+}
 // The plan of a pass: a head of 8 words (items, cut tiles, slots), then its items, heaviest first, then its cut tiles.
 struct PackedList {
   bool keys;              // key tiles (dK, dV), or row tiles
@@ -423,6 +428,7 @@ struct PackedList {
   int tile, step;         // rows and keys of a tile and a step, or keys and rows
   int min_steps;          // no item of a cut tile is much shorter
   int share;              // workgroups that one head's steps are divided among before a tile is cut
+  int places;             // workgroups of one head that run at once
   int max_tiles, max_items, max_slots, max_joins;
   long long at;           // word of the plan where it begins
   long long words() const { return 8 + 8LL * (max_items + max_joins); }

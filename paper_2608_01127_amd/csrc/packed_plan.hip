@@ -48,7 +48,12 @@ __device__ __forceinline__ void steps_of(const PackedList& l, const Sequence& s,
   }
 }
 
-constexpr int kThreads = 1024, kBins = 1024;
+constexpr int kThreads = 1024, kBins = 1024, kCUs = 256;
+
+// Workgroups that tiles are shared out to, two a CU: one that has more than an even share of the steps is cut.  (256, 768,
+// 1024: one token of 8 sequences 34.7, 42.5, 43.5 for 33.9 us; the text batch of 8192 tokens, forward and backward, 467, 401,
+// 383 for 368 us.)
+constexpr int kSlots = 512;
 
 // Sum over the workgroup and everything in front of this thread (exclusive).
 __device__ __forceinline__ int block_scan(int x, int* wave_sums, int& total) {
@@ -73,18 +78,93 @@ __device__ __forceinline__ int block_scan(int x, int* wave_sums, int& total) {
   return front + in - x;
 }
 
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// What an item costs beside its steps, in steps (6: two sequences of 1500 and 1400 tokens, 8 heads, D = 128, forward and
+// backward 95.8 for 91.1 us; 9 and 12 between them, 24 as 16).
+constexpr int kBegin = 16;
+
+// Length of the items that fewer tiles than kSlots are cut into, from `lo` steps (an even share) to `hi` (no cut).  With no
+// more items than places, the longest one decides; with more, two of the first places + 1 items meet in one place.  Each wave
+// prices one length from lo to the shortest that leaves no more items than places.
+// (Always lo: one token of 8 sequences of up to 15840 keys 42.7 for 34.3 us.  Always the other end, of kSlots places: 8 heads
+// of 3471, 2406 and 1997 tokens, D = 64, forward and backward 182 for 147; 4 heads on 1 of 3091, 2664 and 1849, D = 72, 113
+// for 105.)
+__device__ __forceinline__ int few_tiles_target(const int* tile_steps, int n_tiles, int places, int lo, int hi,
+                                                unsigned long long all_steps, int* trial) {
+  constexpr int NW = kThreads / 64, PER = kSlots / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, least = lo;
+  int n[PER], len[PER], parts[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) n[i] = 64 * i + lane < n_tiles ? tile_steps[64 * i + lane] : -1;
+  auto cut = [&](int target) {  // items
+    int all = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      parts[i] = n[i] < 0 ? 0 : max(1, (n[i] + target - 1) / target);
+      all += parts[i];
+    }
+    return wave_sum(all);
+  };
+  int a = lo, b = hi;
+  while (a < b) {
+    const int mid = a + (int)((long long)(b - a) * wave / NW);
+    const int items = cut(mid);
+    if (lane == 0) trial[wave] = items;
+    __syncthreads();
+    int w = 0;
+    while (w < NW && trial[w] > places) ++w;
+    const int from = a, span = b - a;
+    if (w > 0) a = from + (int)((long long)span * (w - 1) / NW) + 1;
+    if (w < NW) b = from + (int)((long long)span * w / NW);
+    __syncthreads();
+  }
+  const int target = least + (int)((long long)(b - least) * wave / (NW - 1)), items = cut(target);
+  long long cost = target + kBegin;
+  if (items > places) {
+    // x: the (places + 1)-th longest item
+    int x = 0, y = target;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) len[i] = parts[i] == 0 ? 0 : (n[i] + parts[i] - 1) / parts[i];
+    while (x < y) {
+      const int mid = x + (y - x) / 2;
+      int more = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) more += len[i] > mid ? parts[i] : 0;
+      if (wave_sum(more) > places) {
+        x = mid + 1;
+      } else {
+        y = mid;
+      }
+    }
+    cost = max(cost, 2 * ((long long)x + kBegin));
+    cost = max(cost, (long long)(all_steps + (long long)items * kBegin) / places);
+  }
+  if (lane == 0) trial[wave] = (int)min(cost, 0x7fffffffLL);
+  __syncthreads();
+  int best = 0;
+  for (int w = 1; w < NW; ++w)
+    if (trial[w] <= trial[best]) best = w;
+  return least + (int)((long long)(b - least) * best / (NW - 1));
+}
+
 }  // namespace
 
 // One workgroup for each list.  Tiles are numbered sequence after sequence; with all steps known, a tile longer than a
-// workgroup's share of them is cut into items of about equal length (of few tiles, into no more items than run at once:
-// one token of 8 sequences of up to 15840 keys 42 -> 34 us); the items are put in order of their length, longest first,
-// by counting (items of a bin in any order: the order decides when a workgroup runs, not what it computes).
-// 9 us for six sequences of up to 19200 tokens; a batch is planned once for all layers.
+// workgroup's share of them is cut into items of about equal length; the items are put in order of their length, longest
+// first, by counting (items of a bin in any order: the order decides when a workgroup runs, not what it computes).
+// A chain of short phases: 15 us for seven sequences of 19200 tokens in all, 17 with the backward's lists, in one launch;
+// a batch is planned once for all layers.
 __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   __shared__ int wave_sums[kThreads / 64];
   __shared__ int bins[kBins];
   __shared__ unsigned long long all_steps;
-  __shared__ int longest, n_items, n_slots, n_joins;
+  __shared__ int longest, n_slots, n_joins;
+  __shared__ int tile_steps[kSlots], trial[kThreads / 64];
   const PackedList l = a.list[blockIdx.x];
   const int tid = threadIdx.x;
   int* head = a.plan + l.at;
@@ -121,14 +201,14 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
     }
     return lo;
   };
-  int beg, end, steps = 0;  // (steps: of tile `tid`)
+  int beg, end;
   {
     unsigned long long sum = 0;
     int most = 0;
     for (int t = tid; t < n_tiles; t += kThreads) {
       const int s = find(t);
       steps_of(l, Sequence(a, s), t - first[s], a.G, a.L, beg, end);
-      if (t == tid) steps = end - beg;
+      if (t < kSlots) tile_steps[t] = end - beg;
       sum += end - beg;
       most = max(most, end - beg);
     }
@@ -137,28 +217,10 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
   const unsigned long long mean = (all_steps + l.share - 1) / l.share;
-  int target;
-  if (n_tiles < l.share) {
-    // as short as leaves no more items than workgroups that run at once
-    int lo = (int)min(max(mean, (unsigned long long)l.min_steps), 0x7fffffffULL), hi = max(lo, longest);
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (tid == 0) n_items = 0;
-      __syncthreads();
-      if (tid < n_tiles) atomicAdd(&n_items, max(1, (steps + mid - 1) / mid));
-      __syncthreads();
-      if (n_items <= l.share) {
-        hi = mid;
-      } else {
-        lo = mid + 1;
-      }
-      __syncthreads();
-    }
-    target = lo;
-  } else {
-    // (twice the mean: the text batch 469 for 387 us)
-    target = (int)min(max(mean, (unsigned long long)l.min_steps), 0x7fffffffULL);
-  }
+  // (twice the mean: the text batch 469 for 387 us)
+  int target = (int)min(max(mean, (unsigned long long)l.min_steps), 0x7fffffffULL);
+  if (n_tiles < l.share && target < longest)
+    target = few_tiles_target(tile_steps, n_tiles, l.places, target, longest, all_steps, trial);
   const int top = min(target, longest);
   auto bin_of = [&](int steps, int parts) { return kBins - 1 - (int)((long long)(steps / parts) * (kBins - 1) / max(top, 1)); };
   for (int t = tid; t < n_tiles; t += kThreads) {
@@ -173,6 +235,11 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   __syncthreads();
   bins[tid] = mine;
   __syncthreads();
+  // The first round meets empty CUs, the second the same ones in the same order: turned round, it gives the CU of the
+  // longest item the shortest of it (16 heads of 4717 tokens, D = 72, forward and backward 181.5 -> 176.7 us, the 1B clips 1876
+  // -> 1860).
+  const int round = max(1, kCUs / a.Hkv), n_two = min(2 * round, min(all_items, l.max_items));
+  auto place = [&](int x) { return x < round || x >= n_two ? x : round + n_two - 1 - x; };
   for (int t0 = 0; t0 < n_tiles; t0 += kThreads) {
     const int t = t0 + tid;
     if (t < n_tiles) {
@@ -189,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
       }
       for (int i = 0; i < parts; ++i)
         if (at + i < l.max_items)
-          items[at + i] = {q.q0, q.nq, q.k0, q.nk, tile, beg + (int)((long long)n * i / parts),
+          items[place(at + i)] = {q.q0, q.nq, q.k0, q.nk, tile, beg + (int)((long long)n * i / parts),
                            beg + (int)((long long)n * (i + 1) / parts), parts > 1 ? slot + i : -1};
     }
     __syncthreads();  // (earlier tiles take the earlier places of a bin: neighbours stay near each other)
@@ -203,16 +270,13 @@ __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
 
 namespace {
 
-// Workgroups that run at once, two a CU: tiles are cut where that many would not have an even share.  (256, 768, 1024: one
-// token of 8 sequences 34.7, 42.5, 43.5 for 33.9 us; the text batch of 8192 tokens, forward and backward, 467, 401, 383 for
-// 368 us.)
-constexpr int kSlots = 512;
 // Keys (or rows) that an item of a cut tile walks at least.
 constexpr int kLeast = 512;
 
 // units: rows (or keys) of all sequences; walked: keys (or rows) that a tile's steps run over at most.
-void finish_list(PackedList& l, PackedShape& s, long long units, long long walked) {
+void finish_list(PackedList& l, PackedShape& s, long long units, long long walked, int per_cu) {
   l.share = std::max(1, kSlots / s.Hkv);
+  l.places = std::max(1, kCUs * per_cu / s.Hkv);
   l.max_tiles = (int)std::min<long long>(units / l.tile + s.N, 0x3fffffff);
   // parts = ceil(steps / target), target >= all steps / share: fewer than one for each tile and `share` more; of cut
   // tiles, which have more steps than target, at most twice steps / target
@@ -245,18 +309,19 @@ PackedShape packed_shape(int N, int H, int Hkv, int D, int L, int total_q, int t
   s.total_q = total_q;
   s.total_k = total_k;
   const long long rows = (long long)total_q * s.G;
-  const auto add = [&](PackedList& l, bool keys, long long units, long long walked) {
+  const auto add = [&](PackedList& l, PackedPass pass, long long units, long long walked) {
+    const bool keys = pass == PackedPass::dkdv;
     l.keys = keys;
     l.kind = (units / 64 + N) * Hkv <= packed_small(D, keys) ? PackedTile::pairs : PackedTile::wide;
     l.tile = l.kind == PackedTile::pairs ? 64 : 128;
     l.step = keys ? packed_dkv_step(D, l.kind) : 64;
     l.min_steps = kLeast / l.step;
-    finish_list(l, s, units, walked);
+    finish_list(l, s, units, walked, packed_per_cu(pass, D, l.kind));
   };
-  add(s.fwd, false, rows, total_k);
+  add(s.fwd, PackedPass::fwd, rows, total_k);
   if (backward) {
-    add(s.dq, false, rows, total_k);
-    add(s.dkv, true, total_k, rows);
+    add(s.dq, PackedPass::dq, rows, total_k);
+    add(s.dkv, PackedPass::dkdv, total_k, rows);
   }
   s.words += (long long)s.n_lists * (N + 1);
   return s;

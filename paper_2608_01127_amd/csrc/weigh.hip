@@ -162,8 +162,9 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_kernel(WeighParams p, WeighS
 
 // Many rows: a workgroup takes NW blocks of a member, one a wave, and one part of the pairs (key head, step of 64 rows),
 // whose Q and LSE it stages in LDS for all of them, a step ahead (reading Q anew for each block: the 1B stream step below 718
-// us).  Bound by the exponentials: 16 of 24 cycles an element of vector work, next to 16 of matrix work.  12 heads x 4800
-// rows of a guidance pair over 14700 and 11025 tokens, D = 128: 367 us, 1034 TF.
+// us).  Bound by the exponentials, 16 of 24 cycles of vector work an element, next to 16 of matrix work: vector work 65%,
+// matrix units 53% busy, with what a wave waits for between them.  12 heads x 4800 rows of a guidance pair over 14700 and
+// 11025 tokens, D = 128: 367 us, 1034 TF.
 template <int D, int NW, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p, WeighSeqs seqs) {
   constexpr int KK = (D + 15) / 16, NT = 64 * NW, BS = 64;
