@@ -499,8 +499,15 @@ struct RopeArgs {
   uint16_t* q_out;
   uint16_t* k_out;
   Strides sq, sk, sqo, sko;
-  int B, H, Hkv, T;  // Hkv = 0: no k
-  int tokens;        // of a workgroup (set by the launcher)
+  int B, T;
+  struct Heads {
+    int n, per_group;
+    unsigned magic;  // ceil(2^32 / per_group)
+  } heads_q, heads_k;  // (no k: n = 0)
+  // of a workgroup (set by the launcher): its tokens, and heads in so many groups; rows by head, or by token
+  int tokens, blocks, groups;
+  bool by_head;
+  unsigned tokens_magic, pairs_magic;
   const void* pos;   // device integers of 4 or 8 bytes, or null: first + t
   bool pos64;
   long long pos_axis, pos_b, pos_t, first;

@@ -122,8 +122,8 @@ int mw_rope_apply(const void* q, const void* k, void* q_out, void* k_out, const 
   a.sqo = sv[2];
   a.sko = sv[3];
   a.B = B;
-  a.H = H;
-  a.Hkv = with_k ? Hkv : 0;
+  a.heads_q.n = H;
+  a.heads_k.n = with_k ? Hkv : 0;
   a.T = T;
   a.pos = positions;
   a.pos64 = pos_bytes == 8;

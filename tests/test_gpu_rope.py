@@ -204,6 +204,50 @@ def test_long_and_wide(mw):
     verify(ko, want64(k, bands, halves, gain, pos))
 
 
+@pytest.mark.parametrize("form", ["interleaved", "halves", "odd halves", "part"])
+@pytest.mark.parametrize("H,Hkv", [(61, 7), (60, 1), (1, 62), (64, 0)])
+def test_tokens_of_many_heads_in_a_row(mw, form, H, Hkv):
+    """Heads in groups, of which the last ones may hold none of q or of k, and the last block fewer tokens."""
+    import torch
+    B, T, D = 2, 8197, 72
+    bands, halves, gain = FORMS[form](D)
+    axes = 1 + max(b.get("axis", 0) for b in bands)
+    rb = mw.rope_bands(bands, halves=halves, gain=gain)
+    q, k = randn((B, H, T, D), 50), randn((B, Hkv, T, D), 51) if Hkv else None
+    pos = positions(axes, B, T, "members", torch.int64)
+    rows = pos if axes > 1 else pos[None]
+    qo, ko = mw.mw_rope_apply(q, k, rb, pos)
+    torch.cuda.synchronize()
+    for x, y in ((q, qo), (k, ko)):
+        if x is not None:
+            for b in range(B):
+                verify(y[b:b + 1], want64(x[b:b + 1], bands, halves, gain, rows[:, b:b + 1]))
+    mw.mw_rope_apply(q, k, rb, pos, q_out=q, k_out=k)
+    torch.cuda.synchronize()
+    assert torch.equal(q, qo) and (k is None or torch.equal(k, ko))
+
+
+@pytest.mark.parametrize("D", [64, 72])
+def test_heads_of_another_order_and_far_apart(mw, D):
+    """q by head, k by token; heads whose distance passes 32 bits of bytes."""
+    import torch
+    rb = mw.rope_bands([dict(dim_offset=0, dim_count=D)], halves=True)
+    B, H, T = 1, 3, 1000
+    q, k = randn((B, H, T, D), 52), randn((B, 2, T, D), 53, "bthd")
+    qo, ko = mw.mw_rope_apply(q, k, rb)
+    far = torch.empty(2 * (1 << 31) + T * D, dtype=torch.bfloat16, device="cuda").as_strided((B, H, T, D), (0, 1 << 31, D, 1))
+    far.copy_(q)
+    out = torch.empty_like(q)
+    mw.mw_rope_apply(far, k, rb, q_out=out)
+    mw.mw_rope_apply(q, k, rb, q_out=far)
+    torch.cuda.synchronize()
+    bands = [dict(dim_offset=0, dim_count=D)]
+    pos = torch.arange(T, device="cuda")[None]
+    verify(qo, want64(q, bands, True, 1.0, pos))
+    verify(ko, want64(k, bands, True, 1.0, pos))
+    assert torch.equal(out, qo) and torch.equal(far, qo)
+
+
 def test_side_stream_and_graph_replays(mw):
     import torch
     rb = mw.rope_bands([dict(dim_offset=0, dim_count=128)], halves=True)
