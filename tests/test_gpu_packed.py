@@ -152,6 +152,13 @@ def test_long_sequences(mw, D, chunk):
     verify(mw, [2111, 777, 90], 2, 1, D, chunk=chunk, seed=9)
 
 
+@pytest.mark.parametrize("D,H,Hkv,chunk,lens", [(64, 8, 8, 64, [3471, 2406, 1997]), (72, 4, 1, 1, [3091, 2664, 1849]),
+                                                (128, 4, 2, 1, [8, 1353, 2, 2523, 1706]), (72, 2, 2, 64, [4763, 4353])])
+def test_fewer_tiles_than_places(mw, D, H, Hkv, chunk, lens):
+    """Tiles cut into more items than run at once, and into fewer; parts of uneven number."""
+    verify(mw, lens, H, Hkv, D, chunk=chunk, seed=60)
+
+
 @pytest.mark.parametrize("D", [64, 72, 128])
 def test_many_sequences(mw, D):
     import torch
