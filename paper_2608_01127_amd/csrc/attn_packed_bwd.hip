@@ -566,7 +566,8 @@ hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams&
   const bool wide_q = s.dq.kind == PackedTile::wide, wide_k = s.dkv.kind == PackedTile::wide;
   constexpr PackedTile W = PackedTile::wide, P = PackedTile::pairs;
   constexpr PackedPass DQ = PackedPass::dq, KV = PackedPass::dkdv;
-  hipError_t e = wide_q ? launch_dq<4, 1, packed_per_cu(DQ, kD, W)>(p, s, stream) : launch_dq<4, 2, packed_per_cu(DQ, kD, P)>(p, s, stream);
+  hipError_t e = wide_q ? launch_dq<4, 1, packed_per_cu(DQ, kD, W)>(p, s, stream)
+                        : launch_dq<4, 2, packed_per_cu(DQ, kD, P)>(p, s, stream);
   if (e != hipSuccess) return e;
   if (wide_k) {
     e = launch_dkdv<4, 1, packed_dkv_step(kD, W), kD == 128 ? 6 : 0, packed_per_cu(KV, kD, W)>(p, s, stream);

@@ -7,7 +7,6 @@
 
 namespace mw {
 
-
 namespace {
 
 // Sum of 16 values over the 32 lanes of a half wave: lane l of a half holds the sum of value (l % 32) / 2.
