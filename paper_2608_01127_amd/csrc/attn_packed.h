@@ -13,9 +13,9 @@
 namespace mw {
 
 // What a workgroup does for key head hk; false: nothing (the grid is sized for the most items there can be).
-__device__ __forceinline__ bool work_item(const int* list, int Hkv, int& hk, PackedItem& it) {
+__device__ __forceinline__ bool work_item(const int* list, int bid, int Hkv, int& hk, PackedItem& it) {
   int rank;
-  tile_item(blockIdx.x, Hkv, hk, rank);
+  tile_item(bid, Hkv, hk, rank);
   if (rank >= list[0]) return false;
   it = reinterpret_cast<const PackedItem*>(list + 8)[rank];
   return true;

@@ -64,8 +64,8 @@ __device__ __forceinline__ void finish_packed(const PackedParams& p, const RowBl
 // Many rows are bound by matrix units and softmax side by side: seven prompts, 19200 tokens in all, 16 heads on 4, D = 128,
 // 404 us, 1001 TF executed, matrix units 57% and vector work 55% busy at 1.68 GHz; D = 64 (8192 tokens, 24 heads on 8) 89
 // us, vector work 82%: its exponentials are as many as at D = 128, for half the products.  D = 72 (4717 tokens, 16 heads)
-// 48 us: products of 80 columns, and LDS conflicts in 31% of the LDS-active cycles.  Few rows are bound by reading keys and values:
-// one token of 8 sequences, 147 MB, 26 us and the join, 34 the call, 4.3 TB/s.
+// 48 us: products of 80 columns, and LDS conflicts in 31% of the LDS-active cycles.  Few rows are bound by reading keys and
+// values: one token of 8 sequences, 147 MB, 26 us and the join, 34 the call, 4.3 TB/s.
 template <int D, int NW, int BN, int KG, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void packed_fwd_kernel(PackedParams p) {
   constexpr int NWR = NW / KG, BM = 32 * NWR, NT = 64 * NW, BK = BN * KG;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_fwd_kernel(PackedParams p
   const int rw = wave % NWR, kg = wave / NWR;
   int hk;
   PackedItem it;
-  if (!work_item(p.list, p.Hkv, hk, it)) return;
+  if (!work_item(p.list, blockIdx.x, p.Hkv, hk, it)) return;
   const int G = p.G, R = it.nq * G, r0 = it.tile * BM;
 
   // this lane's row and its Q fragments; rows behind the last and columns past D are zeros
@@ -229,9 +229,8 @@ hipError_t launch_fwd_tile(const PackedParams& p, const PackedList& list, hipStr
 #define MW_CAT_(a, b) a##b
 #define MW_CAT(a, b) MW_CAT_(a, b)
 hipError_t MW_CAT(launch_packed_fwd_, MW_PACKED_HEAD_DIM)(const PackedParams& p, const PackedList& list, hipStream_t stream) {
-  constexpr PackedPass F = PackedPass::fwd;
-  if (list.kind == PackedTile::pairs) return launch_fwd_tile<4, 32, 2, packed_per_cu(F, kD, PackedTile::pairs)>(p, list, stream);
-  return launch_fwd_tile<4, 64, 1, packed_per_cu(F, kD, PackedTile::wide)>(p, list, stream);
+  if (list.kind == PackedTile::pairs) return launch_fwd_tile<4, 32, 2, packed_fwd_per_cu(kD, PackedTile::pairs)>(p, list, stream);
+  return launch_fwd_tile<4, 64, 1, packed_fwd_per_cu(kD, PackedTile::wide)>(p, list, stream);
 }
 
 }  // namespace mw

@@ -3,8 +3,9 @@
 //   dQ = scale dS K,  dK = scale sum_r dS_r^T Q_r
 // over the rows r of a key head (attn_packed.hip).
 //
-//   dQ kernel    : a wave owns 32 rows and walks the keys they see; it forms Delta (and LSE log2 e) for the other one.
-//   dK/dV kernel : a wave owns 32 keys and walks the rows that see them, staged in LDS.
+//   terms kernel : Delta and LSE log2 e of each row.
+//   grad kernel  : dK and dV, of which a wave owns 32 keys and walks the rows that see them, staged in LDS; and dQ, of which
+//                  a wave owns 32 rows and walks the keys they see.
 //   join kernel  : adds the parts of tiles that the plan has cut, in their order.  No atomics.
 #include <algorithm>
 #include <type_traits>
@@ -17,23 +18,150 @@ namespace {
 
 constexpr int kD = MW_PACKED_HEAD_DIM;
 
+// LDS of a row tile's kernels: K and V tiles of BN * KG keys, two stages each; the groups' sums.
+template <int D, int NW, int KG, int BN>
+struct RowTileLds {
+  static constexpr int TE = stage_elems<D, BN * KG, 64 * NW>();
+  static constexpr int BYTES = 2 * 2 * TE * 2;
+  static_assert(KG == 1 || (KG / 2) * (NW / KG) * (D / 32) * 4096 <= BYTES, "the groups' sums fit the stages");
+};
+
+// A sequence's keys and values, staged BS at a time; keys behind the last one repeat it.
+template <int D, int BS, int NT>
+struct KeyStage {
+  const bf16_t *k, *v;
+  long long sk, sv;
+  int n;
+  RowOffsets<D, BS, NT> ro_k, ro_v;
+  __device__ __forceinline__ KeyStage(const PackedBwdParams& p, const PackedItem& it, int hk, int tid)
+      : k(p.k + (long long)it.k0 * p.sk.t + hk * p.sk.h), v(p.v + (long long)it.k0 * p.sv.t + hk * p.sv.h), sk(p.sk.t),
+        sv(p.sv.t), n(it.nk), ro_k(p.sk.t, tid), ro_v(p.sv.t, tid) {}
+  __device__ __forceinline__ void stage(int i, bf16_t* Kt, bf16_t* Vt, int tid) const {
+    const long long k0 = (long long)i * BS;
+    if (k0 + BS <= n) {
+      stage_rows_s<D, BS, NT>(Kt, k + k0 * sk, ro_k, tid);
+      stage_rows_s<D, BS, NT>(Vt, v + k0 * sv, ro_v, tid);
+    } else {
+      stage_kv_rows_direct<D, BS, NT>(Kt, Vt, [&](int r) -> RowPair {
+        const long long j = min(k0 + r, (long long)n - 1);
+        return {k + j * sk, v + j * sv};
+      }, tid);
+    }
+  }
+};
+
+// Delta and LSE log2 e of the rows of a tile, for both gradients: rowsum(dO O), which has O's rounding to bf16.  Next to few
+// keys' dP - Delta that is not small (cross_dq_kernel): rows of a tile whose first one sees at most 64 keys take sum_j P_j dP_j.
+// Bound by reading dO and O: 19200 rows of 12 heads, D = 128, 118 MB in 27 us (31 with a row read by two lanes).
+template <int D>
+__global__ __launch_bounds__(256) void packed_terms_kernel(PackedBwdParams p, int BM) {
+  constexpr int BS = 64, NT = 256, KK = (D + 15) / 16;
+  using LD = RowTileLds<D, 4, 1, BS>;
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[LD::TE], Vs[LD::TE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int hk;
+  PackedItem it;
+  if (!work_item(p.list_q, blockIdx.x, p.Hkv, hk, it) || it.beg > 0) return;
+  const int G = p.G, R = it.nq * G, n = it.nk, r0 = it.tile * BM;
+  const long long terms = ((long long)hk * p.total_q + it.q0) * G;
+  auto lse_of = [&](int r) {
+    const int t = r / G;
+    return p.lse[(long long)(hk * G + (r - t * G)) * p.total_q + it.q0 + t] * 1.4426950408889634f;
+  };
+  if (it.slot >= 0 || it.beg == it.end || sees(r0, G, it.nq, n, p.L) > 64) {
+    // a row is read by eight lanes, or sixteen, a quarter of the tile by a wave
+    constexpr int LPR = D == 128 ? 16 : 8, ROWS = 64 / LPR, ITERS = 32 / ROWS, PER = (D / 8 + LPR - 1) / LPR;
+    const int part = lane % LPR, first = r0 + wave * (BM / 4) + lane / LPR;
+    bf16x8 x[ITERS][PER], y[ITERS][PER];
+    float lse2[ITERS];
+#pragma unroll
+    for (int i = 0; i < ITERS; ++i) {
+      if (i * ROWS >= BM / 4) break;
+      const int rc = min(first + i * ROWS, R - 1);
+      const bf16_t* da = p.d_o + packed_offset(p.sdo, hk, G, it.q0, rc);
+      const bf16_t* oa = p.o + packed_offset(p.so, hk, G, it.q0, rc);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int col = min(8 * (part + j * LPR), D - 8);  // (D = 72: its last eight columns are one lane's)
+        x[i][j] = *reinterpret_cast<const bf16x8*>(da + col);
+        y[i][j] = *reinterpret_cast<const bf16x8*>(oa + col);
+      }
+      lse2[i] = lse_of(rc);
+    }
+#pragma unroll
+    for (int i = 0; i < ITERS; ++i) {
+      const int row = first + i * ROWS;
+      if (i * ROWS >= BM / 4) break;
+      float dot = 0.f;
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = part + j * LPR < D / 8 ? fmaf((float)x[i][j][e], (float)y[i][j][e], dot) : dot;
+#pragma unroll
+      for (int m = 1; m < LPR; m <<= 1) dot += __shfl_xor(dot, m);
+      if (part == 0 && row < R) {
+        p.delta[terms + row] = -dot;
+        p.lse2[terms + row] = lse2[i];
+      }
+    }
+    return;
+  }
+  const int row = r0 + wave * 32 + (lane & 31), rc = min(row, R - 1), hi = sees(rc, G, it.nq, n, p.L);
+  const float lse2 = lse_of(rc);
+  const bf16_t* qa = p.q + packed_offset(p.sq, hk, G, it.q0, rc) + 8 * (lane >> 5);
+  const bf16_t* da = p.d_o + packed_offset(p.sdo, hk, G, it.q0, rc) + 8 * (lane >> 5);
+  bf16x8 qf[KK], of[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
+      qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
+      of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = (__bf16)0.f;
+    }
+  }
+  const FragOffsets<D> fo(lane, 0);
+  const KeyStage<D, BS, NT> keys(p, it, hk, tid);
+  float sum = 0.f;
+  for (int i = it.beg; i < it.end; ++i) {
+    if (i > it.beg) __syncthreads();  // (the stage has been read)
+    keys.stage(i, Ks, Vs, tid);
+    wait_vmem();
+    __syncthreads();
+#pragma unroll 1
+    for (int kq = 0; kq < BS / 32; ++kq) {
+      f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        s = mfma32(fo.row8(Ks, kq * 32, kk), qf[kk], s);
+        dp = mfma32(fo.row8(Vs, kq * 32, kk), of[kk], dp);
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const bool in = i * BS + kq * 32 + acc_row(j, lane) < hi;
+        sum = fmaf(in ? fast_exp2(fmaf(s[j], p.scale_log2, -lse2)) : 0.f, in ? dp[j] : 0.f, sum);
+      }
+    }
+  }
+  sum = sum_halves(sum);
+  if (wave * 32 < BM && lane < 32 && row < R) {
+    p.delta[terms + row] = -sum;
+    p.lse2[terms + row] = lse2;
+  }
+}
+
 // dK/dV: NWK key waves of 32 keys each (K fragments, dK^T and dV^T in registers) in QG row groups; a step stages
 // BM * QG rows, of which a group takes its BM, and the groups' gradients are added through LDS at the end.  The
 // first VL V fragments are read from LDS, where they lie as in the registers (D = 128: two waves per SIMD need
 // the registers).  Lanes behind the last key repeat it and store nothing.
-//
-// Bound by the matrix products, 8 D a pair of the 14 D of the backward (S and dP are formed in both kernels, so that neither
-// has to add to memory that others add to), with two waves a SIMD: clips of 600 to 9600 tokens, 19200 in all, 12 heads, D =
-// 128, 890 to 970 us, 945 TF executed, matrix units 56% busy at 1.62 GHz, which is what the power limit leaves.  D = 64 (24
-// heads on 8, 8192 tokens) 169 us, 860 TF: 1072 workgroups over 768 places.
-template <int D, int NWK, int QG, int BM, int VL, int WPS>
-__global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedBwdParams p) {
+template <int D, int NWK, int QG, int BM, int VL>
+__device__ __forceinline__ void packed_dkdv(const PackedBwdParams& p, const int bid, unsigned char* lds) {
   constexpr int NW = NWK * QG, BN = 32 * NWK, NT = 64 * NW, BS = BM * QG, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
   static_assert(16 * VL <= D, "the V fragments in LDS have no columns past D");
   using LD = KeyTileLds<D, NWK, QG, BM, VL>;
   constexpr int TE = LD::TE, RT = LD::RT;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[LD::BYTES];
   bf16_t(*Qs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);
   bf16_t(*Os)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds + 4 * TE);
   float(*lse_s)[RT] = reinterpret_cast<float(*)[RT]>(lds + 8 * TE);
@@ -43,7 +171,7 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
   const int kw = wave % NWK, qg = wave / NWK, gq = qg * BM;
   int hk;
   PackedItem it;
-  if (!work_item(p.list_k, p.Hkv, hk, it)) return;
+  if (!work_item(p.list_k, bid, p.Hkv, hk, it)) return;
   const int G = p.G, R = it.nq * G, n = it.nk, L = p.L;
   const int k0 = it.tile * BN, key = k0 + kw * 32 + (lane & 31);
   f32x16 dk[DB], dv[DB];
@@ -279,115 +407,49 @@ __global__ __launch_bounds__(64 * NWK * QG, WPS) void packed_dkdv_kernel(PackedB
 
 // dQ: NW waves in KG key groups of NW / KG waves of 32 rows each (Q and dO fragments, dQ^T in registers); a step stages
 // BN * KG keys, of which a group takes its BN, and the groups' dQ are added through LDS at the end.
-// Bound by the matrix products, 6 D a pair, as above: the clips 635 to 690 us, 1011 TF executed, matrix units 60% busy at
-// 1.62 GHz; the 8192 tokens of D = 64 115 us, 944 TF; 4717 tokens of 16 heads, D = 72, 65 us, 790 TF.
-template <int D, int NW, int KG, int BN, int WPS>
-__global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams p) {
+template <int D, int NW, int KG, int BN>
+__device__ __forceinline__ void packed_dq(const PackedBwdParams& p, const int bid, unsigned char* lds) {
   constexpr int NWR = NW / KG, BM = 32 * NWR, BS = BN * KG, NT = 64 * NW, KK = (D + 15) / 16, DB = D / 32;
   constexpr bool TAIL = D % 32 != 0;
-  constexpr int TE = stage_elems<D, BS, NT>();
-  __shared__ __attribute__((aligned(16))) bf16_t lds[2][2][TE];
-  bf16_t(*Ks)[TE] = lds[0];
-  bf16_t(*Vs)[TE] = lds[1];
-  static_assert(KG == 1 || (KG / 2) * NWR * DB * 4096 <= (int)sizeof(lds), "the groups' sums fit the stages");
+  using LD = RowTileLds<D, NW, KG, BN>;
+  constexpr int TE = LD::TE;
+  bf16_t(*Ks)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds);
+  bf16_t(*Vs)[TE] = reinterpret_cast<bf16_t(*)[TE]>(lds + 4 * TE);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % NWR, kg = wave / NWR;
   int hk;
   PackedItem it;
-  if (!work_item(p.list_q, p.Hkv, hk, it)) return;
+  if (!work_item(p.list_q, bid, p.Hkv, hk, it)) return;
   const int G = p.G, R = it.nq * G, n = it.nk, r0 = it.tile * BM;
   const int row = r0 + rw * 32 + (lane & 31), rc = min(row, R - 1);
-  // This row's Q, dO and O, asked for before anything that waits: their latencies then pass together.
-  bf16x8 qf[KK], of[KK], y[KK];
+  bf16x8 qf[KK], of[KK];
   {
     const bf16_t* qa = p.q + packed_offset(p.sq, hk, G, it.q0, rc) + 8 * (lane >> 5);
     const bf16_t* da = p.d_o + packed_offset(p.sdo, hk, G, it.q0, rc) + 8 * (lane >> 5);
-    const bf16_t* oa = p.o + packed_offset(p.so, hk, G, it.q0, rc) + 8 * (lane >> 5);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       if (D % 16 == 0 || 16 * kk + 8 * (lane >> 5) < D) {
         of[kk] = *reinterpret_cast<const bf16x8*>(da + 16 * kk);
-        y[kk] = *reinterpret_cast<const bf16x8*>(oa + 16 * kk);
         qf[kk] = *reinterpret_cast<const bf16x8*>(qa + 16 * kk);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = y[kk][j] = (__bf16)0.f;
+        for (int j = 0; j < 8; ++j) qf[kk][j] = of[kk][j] = (__bf16)0.f;
       }
     }
   }
-  const int row_t = rc / G;
-  const float lse = p.lse[(long long)(hk * G + (rc - row_t * G)) * p.total_q + it.q0 + row_t];
+  const long long at = ((long long)hk * p.total_q + it.q0) * G + rc;
+  const float ndlt = p.delta[at], lse2 = p.lse2[at], c = p.scale_log2;
   const int hi = sees(rc, G, it.nq, n, p.L), hi_all = sees(r0, G, it.nq, n, p.L);
   f32x16 dq[DB];
   f32x4 tail[2] = {zero4(), zero4()};
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = zero16();
-  const bf16_t* k0p = p.k + (long long)it.k0 * p.sk.t + hk * p.sk.h;
-  const bf16_t* v0p = p.v + (long long)it.k0 * p.sv.t + hk * p.sv.h;
   const FragOffsets<D> fo(lane, 0);
   const Tail72 ft(lane, 0);
-  const RowOffsets<D, BS, NT> ro_k(p.sk.t, tid), ro_v(p.sv.t, tid);
-  auto stage = [&](int i, int buf) {  // keys behind the sequence's last one repeat it
-    const long long k0 = (long long)i * BS;
-    if (k0 + BS <= n) {
-      stage_rows_s<D, BS, NT>(Ks[buf], k0p + k0 * p.sk.t, ro_k, tid);
-      stage_rows_s<D, BS, NT>(Vs[buf], v0p + k0 * p.sv.t, ro_v, tid);
-    } else {
-      stage_kv_rows_direct<D, BS, NT>(Ks[buf], Vs[buf], [&](int r) -> RowPair {
-        const long long j = min(k0 + r, (long long)n - 1);
-        return {k0p + j * p.sk.t, v0p + j * p.sv.t};
-      }, tid);
-    }
-  };
-  if (it.beg < it.end) stage(it.beg, 0);
-  float dot = 0.f;
-#pragma unroll
-  for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) dot = fmaf((float)of[kk][j], (float)y[kk][j], dot);
-  float ndlt = -sum_halves(dot);
-  const float c = p.scale_log2, lse2 = lse * 1.4426950408889634f;
+  const KeyStage<D, BS, NT> keys(p, it, hk, tid);
+  if (it.beg < it.end) keys.stage(it.beg, Ks[0], Vs[0], tid);
   wait_vmem();
   __syncthreads();
-  // Rows of few keys: Delta = sum_j P_j dP_j of the probabilities at hand.  rowsum(dO O) has O's rounding to bf16, which
-  // next to few keys' dP - Delta is not small (cross_dq_kernel); a tile whose first row sees at most a step of
-  // keys is walked twice.
-  if (hi_all <= 64 && it.slot < 0 && it.beg < it.end) {
-    float sum = 0.f;
-    for (int i = it.beg; i < it.end; ++i) {
-      if (i > it.beg) {
-        stage(i, 0);
-        wait_vmem();
-        __syncthreads();
-      }
-#pragma unroll 1
-      for (int kq = 0; kq < BS / 32; ++kq) {  // (each group forms the whole sum)
-        f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          s = mfma32(fo.row8(Ks[0], kq * 32, kk), qf[kk], s);
-          dp = mfma32(fo.row8(Vs[0], kq * 32, kk), of[kk], dp);
-        }
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const bool in = i * BS + kq * 32 + acc_row(j, lane) < hi;
-          sum = fmaf(in ? fast_exp2(fmaf(s[j], c, -lse2)) : 0.f, in ? dp[j] : 0.f, sum);
-        }
-      }
-      __syncthreads();  // (the stage is written again)
-    }
-    ndlt = -sum_halves(sum);
-    if (it.end - it.beg > 1) {
-      stage(it.beg, 0);
-      wait_vmem();
-      __syncthreads();
-    }
-  }
-  if (it.beg == 0 && kg == 0 && lane < 32 && row < R) {
-    const long long at = ((long long)hk * p.total_q + it.q0) * G + row;
-    p.delta[at] = ndlt;
-    p.lse2[at] = lse2;
-  }
   if (it.beg < it.end) {
     f32x16 nd;
 #pragma unroll
@@ -425,7 +487,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
     int buf = 0, i = it.beg;
     auto run = [&](auto masked, int stop) {
       for (; i < stop; ++i) {
-        if (i + 1 < it.end) stage(i + 1, buf ^ 1);
+        if (i + 1 < it.end) keys.stage(i + 1, Ks[buf ^ 1], Vs[buf ^ 1], tid);
         step(masked, i * BS, buf);
         wait_vmem();
         __syncthreads();
@@ -436,7 +498,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
     run(std::true_type{}, it.end);
   }
   if constexpr (KG > 1) {
-    float* m = reinterpret_cast<float*>(&lds[0][0][0]);
+    float* m = reinterpret_cast<float*>(lds);
     add_groups<KG, NWR>(dq, kg, rw, lane, m);
     if constexpr (TAIL) {
       f32x16 rest[1] = {zero16()};
@@ -478,7 +540,7 @@ __global__ __launch_bounds__(64 * NW, WPS) void packed_dq_kernel(PackedBwdParams
 }
 
 // Sums of the parts of cut tiles, in order: dK and dV, then dQ.  One thread for four columns of a row.  5 us where little is
-// cut; 9 for the 8192 tokens above, whose parts (16 MB) it reads at 1.9 TB/s.
+// cut, 7 for the text batch below.
 template <int D, int BM, int BN>
 __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p) {
   constexpr int TPR = D / 4, PER_K = join_blocks(BN, D), PER_Q = join_blocks(BM, D);
@@ -525,24 +587,51 @@ __global__ __launch_bounds__(256) void packed_bwd_join_kernel(PackedBwdParams p)
 
 }  // namespace
 
-namespace {
+// A tile's configuration: rows (dQ) and keys (dK, dV) of 128 in four waves, or of 64 in two groups of two.
+template <int D, PackedTile T>
+struct Config {
+  static constexpr bool WIDE = T == PackedTile::wide;
+  static constexpr int TILE = WIDE ? 128 : 64, GROUPS = WIDE ? 1 : 2;
+  static constexpr int VL = D == 128 ? (WIDE ? 6 : 7) : 0;
+  static constexpr int BM = packed_dkv_step(D, T) / GROUPS;
+  using Rows = RowTileLds<D, 4, GROUPS, 64 / GROUPS>;
+  using Keys = KeyTileLds<D, TILE / 32, GROUPS, BM, VL>;
+};
 
-template <int NW, int KG, int WPS>
-hipError_t launch_dq(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
-  constexpr int BN = 64 / KG;
-  if (s.dq.tile != 32 * NW / KG || s.dq.step != 64) return hipErrorInvalidValue;
-  const long long grid = (long long)s.dq.max_items * s.Hkv;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_dq_kernel<kD, NW, KG, BN, WPS>), dim3((unsigned)grid), dim3(64 * NW), 0, stream, p);
-  return hipGetLastError();
+// Both in one grid: the longer dK/dV items first, so that dQ's fill the places that the last of them leave (the text batch
+// below 253 us, one after the other, with Delta formed by dQ's, 283; 512 tokens of 8 heads, D = 128, forward and backward 44
+// -> 36).
+//
+// Bound by the matrix products: 14 D a pair for the 10 that the gradients need, because S and dP are formed for both, so that
+// neither has to add to memory that others add to.  Clips of 600 to 9600 tokens, 19200 in all, 12 heads, D = 128: 1600 us,
+// 1008 TF executed, matrix units 58% busy with two waves a SIMD at 1.65 GHz, which is what the power limit leaves; the text
+// batch, 8192 tokens, 24 heads on 8, D = 64, 1005 TF; 4717 tokens of 16 heads, D = 72, 138 us, 884 TF.
+template <int D, PackedTile TQ, PackedTile TK>
+__global__ __launch_bounds__(256, packed_bwd_per_cu(D, TQ, TK)) void packed_grad_kernel(PackedBwdParams p, int n_keys) {
+  using Q = Config<D, TQ>;
+  using K = Config<D, TK>;
+  constexpr int BYTES = Q::Rows::BYTES > K::Keys::BYTES ? Q::Rows::BYTES : K::Keys::BYTES;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[BYTES];
+  if ((int)blockIdx.x < n_keys) {
+    packed_dkdv<D, K::TILE / 32, K::GROUPS, K::BM, K::VL>(p, blockIdx.x, lds);
+  } else {
+    packed_dq<D, 4, Q::GROUPS, 64 / Q::GROUPS>(p, blockIdx.x - n_keys, lds);
+  }
 }
 
-template <int NWK, int QG, int BM, int VL, int WPS>
-hipError_t launch_dkdv(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
-  if (s.dkv.tile != 32 * NWK || s.dkv.step != BM * QG) return hipErrorInvalidValue;
-  const long long grid = (long long)s.dkv.max_items * s.Hkv;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_dkdv_kernel<kD, NWK, QG, BM, VL, WPS>), dim3((unsigned)grid), dim3(64 * NWK * QG), 0, stream, p);
+namespace {
+
+template <PackedTile TQ, PackedTile TK>
+hipError_t launch_grad(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
+  if (s.dq.tile != Config<kD, TQ>::TILE || s.dq.step != 64 || s.dkv.tile != Config<kD, TK>::TILE ||
+      s.dkv.step != packed_dkv_step(kD, TK))
+    return hipErrorInvalidValue;
+  const long long n_rows = (long long)s.dq.max_items * s.Hkv, n_keys = (long long)s.dkv.max_items * s.Hkv;
+  if (n_rows + n_keys > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((packed_terms_kernel<kD>), dim3((unsigned)n_rows), dim3(256), 0, stream, p, s.dq.tile);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((packed_grad_kernel<kD, TQ, TK>), dim3((unsigned)(n_keys + n_rows)), dim3(256), 0, stream, p, (int)n_keys);
   return hipGetLastError();
 }
 
@@ -565,15 +654,8 @@ hipError_t launch_join(const PackedBwdParams& p, const PackedShape& s, hipStream
 hipError_t MW_CAT(launch_packed_bwd_, MW_PACKED_HEAD_DIM)(const PackedBwdParams& p, const PackedShape& s, hipStream_t stream) {
   const bool wide_q = s.dq.kind == PackedTile::wide, wide_k = s.dkv.kind == PackedTile::wide;
   constexpr PackedTile W = PackedTile::wide, P = PackedTile::pairs;
-  constexpr PackedPass DQ = PackedPass::dq, KV = PackedPass::dkdv;
-  hipError_t e = wide_q ? launch_dq<4, 1, packed_per_cu(DQ, kD, W)>(p, s, stream)
-                        : launch_dq<4, 2, packed_per_cu(DQ, kD, P)>(p, s, stream);
-  if (e != hipSuccess) return e;
-  if (wide_k) {
-    e = launch_dkdv<4, 1, packed_dkv_step(kD, W), kD == 128 ? 6 : 0, packed_per_cu(KV, kD, W)>(p, s, stream);
-  } else {
-    e = launch_dkdv<2, 2, 32, kD == 128 ? 7 : 0, packed_per_cu(KV, kD, P)>(p, s, stream);
-  }
+  const hipError_t e = wide_q ? (wide_k ? launch_grad<W, W>(p, s, stream) : launch_grad<W, P>(p, s, stream))
+                              : (wide_k ? launch_grad<P, W>(p, s, stream) : launch_grad<P, P>(p, s, stream));
   if (e != hipSuccess) return e;
   if (wide_q) return wide_k ? launch_join<128, 128>(p, s, stream) : launch_join<128, 64>(p, s, stream);
   return wide_k ? launch_join<64, 128>(p, s, stream) : launch_join<64, 64>(p, s, stream);

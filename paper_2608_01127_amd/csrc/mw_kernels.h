@@ -417,9 +417,9 @@ struct PackedJoin {
 // would leave CUs idle.
 enum class PackedTile { wide, pairs };
 // Workgroups that a CU runs at once (of four waves each, so waves a SIMD).
-enum class PackedPass { fwd, dq, dkdv };
-constexpr int packed_per_cu(PackedPass pass, int D, PackedTile t) {
-  return t == PackedTile::wide && (D == 64 || (D == 72 && pass == PackedPass::fwd)) ? 3 : 2;
+constexpr int packed_fwd_per_cu(int D, PackedTile t) { return t == PackedTile::wide && D != 128 ? 3 : 2; }
+constexpr int packed_bwd_per_cu(int D, PackedTile rows, PackedTile keys) {
+  return D == 64 && rows == PackedTile::wide && keys == PackedTile::wide ? 3 : 2;
 }
 // The plan of a pass: a head of 8 words (items, cut tiles, slots), then its items, heaviest first, then its cut tiles.
 struct PackedList {

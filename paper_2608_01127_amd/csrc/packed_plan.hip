@@ -275,8 +275,11 @@ constexpr int kLeast = 512;
 
 // units: rows (or keys) of all sequences; walked: keys (or rows) that a tile's steps run over at most.
 void finish_list(PackedList& l, PackedShape& s, long long units, long long walked, int per_cu) {
-  l.share = std::max(1, kSlots / s.Hkv);
-  l.places = std::max(1, kCUs * per_cu / s.Hkv);
+  // (the backward's two lists run in one grid: with the forward's share each, 12 heads of 3531 tokens, D = 128, forward and
+  // backward 156 for 149 us; with half of it the text batch 411 for 348)
+  const int slots = s.n_lists == 0 ? kSlots : kSlots * 3 / 4;
+  l.share = std::max(1, slots / s.Hkv);
+  l.places = std::max(1, kCUs * per_cu * slots / kSlots / s.Hkv);
   l.max_tiles = (int)std::min<long long>(units / l.tile + s.N, 0x3fffffff);
   // parts = ceil(steps / target), target >= all steps / share: fewer than one for each tile and `share` more; of cut
   // tiles, which have more steps than target, at most twice steps / target
@@ -309,19 +312,22 @@ PackedShape packed_shape(int N, int H, int Hkv, int D, int L, int total_q, int t
   s.total_q = total_q;
   s.total_k = total_k;
   const long long rows = (long long)total_q * s.G;
-  const auto add = [&](PackedList& l, PackedPass pass, long long units, long long walked) {
-    const bool keys = pass == PackedPass::dkdv;
+  const auto kind = [&](bool keys, long long units) {
+    return (units / 64 + N) * Hkv <= packed_small(D, keys) ? PackedTile::pairs : PackedTile::wide;
+  };
+  const auto add = [&](PackedList& l, bool keys, long long units, long long walked, int per_cu) {
     l.keys = keys;
-    l.kind = (units / 64 + N) * Hkv <= packed_small(D, keys) ? PackedTile::pairs : PackedTile::wide;
+    l.kind = kind(keys, units);
     l.tile = l.kind == PackedTile::pairs ? 64 : 128;
     l.step = keys ? packed_dkv_step(D, l.kind) : 64;
     l.min_steps = kLeast / l.step;
-    finish_list(l, s, units, walked, packed_per_cu(pass, D, l.kind));
+    finish_list(l, s, units, walked, per_cu);
   };
-  add(s.fwd, PackedPass::fwd, rows, total_k);
+  add(s.fwd, false, rows, total_k, packed_fwd_per_cu(D, kind(false, rows)));
   if (backward) {
-    add(s.dq, PackedPass::dq, rows, total_k);
-    add(s.dkv, PackedPass::dkdv, total_k, rows);
+    const int per_cu = packed_bwd_per_cu(D, kind(false, rows), kind(true, total_k));
+    add(s.dq, false, rows, total_k, per_cu);
+    add(s.dkv, true, total_k, rows, per_cu);
   }
   s.words += (long long)s.n_lists * (N + 1);
   return s;
