@@ -392,6 +392,55 @@ def test_side_stream_and_graph_replays(mw):
                 assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("D,H,Hkv,lens", [(128, 4, 2, [1500, 7, 2600]), (64, 12, 4, [4100, 900]), (72, 3, 3, [5, 3000])])
+def test_two_calls_at_once_share_a_plan(mw, D, H, Hkv, lens):
+    """Both directions on two streams, eagerly and as two graphs replayed together, against one after the other."""
+    import torch
+    T = sum(lens)
+    pack = mw.Packed(edges(lens), T, H, Hkv, D, backward=True)
+    sets = []
+    for seed in (70, 80):
+        q, do = randn((T, H, D), seed), randn((T, H, D), seed + 1)
+        k, v = randn((T, Hkv, D), seed + 2), randn((T, Hkv, D), seed + 3)
+        work = [torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+                for n in (mw.mw_packed_attn_workspace_size(pack), mw.mw_packed_attn_bwd_workspace_size(pack))]
+        out = [torch.empty_like(q), torch.empty((H, T), device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(k)]
+        sets.append((q, k, v, do, work, out))
+
+    def run(x):
+        q, k, v, do, work, out = x
+        mw.mw_packed_attn_fwd(q, k, v, pack, out=out[0], lse=out[1], workspace=work[0])
+        mw.mw_packed_attn_bwd(q, k, v, out[0], do, out[1], pack, workspace=work[1], dq=out[2], dk=out[3], dv=out[4])
+
+    want = []
+    for x in sets:
+        run(x)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in x[5]])
+    streams = [torch.cuda.Stream() for _ in sets]
+    graphs = []
+    for s, x in zip(streams, sets):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            run(x)
+        graphs.append(g)
+    for eager in (True, False, True, False):
+        for x in sets:
+            for t in x[5]:
+                t.fill_(9.0)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for s, x, g in zip(streams, sets, graphs):
+                with torch.cuda.stream(s):
+                    if eager:
+                        run(x)
+                    else:
+                        g.replay()
+        torch.cuda.synchronize()
+        for x, w in zip(sets, want):
+            assert all(torch.equal(a, b) for a, b in zip(x[5], w))
+
+
 def test_places_out_of_range_stay_within_the_tensors(mw):
     """Lengths that overrun the tensors are cut, descending ones empty; what lies around the outputs is left alone."""
     import torch
