@@ -703,9 +703,12 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
  * weights : fp32 [N, W * L], a row for each sequence; entries behind its length are left as
  *           they were.  add = 1: added to what is there; 0: written.  They are the caller's: fork,
  *           copy, free and evict do not move them.
- * workspace: mw_kvpages_weigh_workspace_size(...) bytes, or NULL: the rows of a call are then not
- *           divided among workgroups.
- * Products as in mw_chunk_attn_paged, sums in fp32, deterministic.
+ * workspace: optional; mw_kvpages_weigh_workspace_size(...) bytes divide the rows of a call among
+ *           workgroups as fast as can be.  With fewer they are divided into what fits, with NULL not at
+ *           all, which is slower.  The size is that for the sequences' present lengths and may shrink
+ *           as they grow; it is never above 64 MiB.
+ * Products as in mw_chunk_attn_paged, sums in fp32, deterministic (in an order that the sizes and
+ * workspace_bytes decide).
  * Refuses a stream under HIP graph capture (the host's lengths size the call).
  * Errors: MW_EINVAL (also a sequence listed twice), MW_EALIGN, MW_EUNSUPPORTED, MW_EHIP. */
 size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T);

@@ -587,7 +587,11 @@ struct WeighPlan {
   bool many;
   int parts;
 };
-WeighPlan weigh_plan(int Hkv, int R, long long blocks);
+// Bytes of one part's sums, and the most that a call's parts take.
+constexpr size_t weigh_part_bytes(long long blocks) { return (size_t)blocks * 64 * sizeof(float); }
+constexpr size_t kWeighBytes = (size_t)64 << 20;
+// bytes: of the workspace.
+WeighPlan weigh_plan(int Hkv, int R, long long blocks, size_t bytes);
 hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipStream_t stream);
 // Sequences of which `keep` tokens stay: the `first` ones, the `recent` last ones and the heaviest others.
 struct KeepArgs {

@@ -437,8 +437,8 @@ static int weigh_blocks(const mw_kvpages* c, const int32_t* seqs, int n_seqs, We
 
 size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T) {
   if (check_weigh("mw_kvpages_weigh_workspace_size", c, seqs, n_seqs, H, T)) return 0;
-  const int n = weigh_blocks(c, seqs, n_seqs, nullptr), parts = weigh_plan(c->H, T * (H / c->H), n).parts;
-  return parts > 1 ? (size_t)parts * n * MW_PAGE_BLOCK * sizeof(float) : 0;
+  const int n = weigh_blocks(c, seqs, n_seqs, nullptr), parts = weigh_plan(c->H, T * (H / c->H), n, kWeighBytes).parts;
+  return parts > 1 ? parts * weigh_part_bytes(n) : 0;
 }
 
 int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const void* q, const float* lse, int H, int T,
@@ -461,11 +461,9 @@ int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const
   WeighSeqs s{};
   const int blocks = weigh_blocks(c, seqs, n_seqs, &s);
   WeighParams p{};
-  const WeighPlan plan = weigh_plan(c->H, T * (H / c->H), blocks);
+  const WeighPlan plan = weigh_plan(c->H, T * (H / c->H), blocks, workspace == nullptr ? 0 : workspace_bytes);
   p.many = plan.many;
   p.n_parts = plan.parts;
-  const size_t need = p.n_parts > 1 ? (size_t)p.n_parts * blocks * MW_PAGE_BLOCK * sizeof(float) : 0;
-  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) p.n_parts = 1;
   p.q = static_cast<const uint16_t*>(q);
   p.lse = lse;
   const PagePool pool = pool_of(c);

@@ -80,7 +80,8 @@ __device__ __forceinline__ void put_sum(const WeighParams& p, const WeighSeqs& s
 
 // w_j = sum over rows r and key heads of exp(scale q_r k_j - LSE_r).  A wave keeps a block of 64 cached tokens' keys of a
 // head in registers (S^T = K Q^T, rows of S^T are keys) and adds up the probabilities of its rows there, so that rows are
-// summed across lanes once, at the end.  Sums are in 32 bits, in an order that the sizes alone decide; no atomics.
+// summed across lanes once, at the end.  Sums are in 32 bits, in an order that the sizes and the
+// workspace decide; no atomics.
 //
 // Few rows: bound by reading the codes.  A workgroup takes one block and one part of the pairs (key head, tile of 32 rows),
 // its waves take pairs in turn and read Q as they need it.  Short workgroups, so the more at once the better (one token of 8
@@ -316,12 +317,15 @@ hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipS
 // tokens, D = 128, us: 64 rows 18.3 few | 42.5 many, 128 29.4 | 19.4, 600 82 | 41; 4 heads x 2000 rows over 300 tokens, D =
 // 64, 13.9 | 22.7).  Its parts are those of the least time in rounds of the 512 workgroups that run at once, each of its
 // steps and a beginning as long as three (always about 768 workgroups: the 1B stream step 386 us, so 367).
-WeighPlan weigh_plan(int Hkv, int R, long long blocks) {
+// No more parts than the workspace holds, and never more than kWeighBytes of them (by this count of rounds that costs 1.3%
+// at most in 20000 drawn sizes of up to 2^18 blocks and 2^17 rows; without the limit parts of 750 MB came up).
+WeighPlan weigh_plan(int Hkv, int R, long long blocks, size_t bytes) {
   const long long groups = (blocks + kWaves - 1) / kWaves, steps = (long long)Hkv * ((R + 63) / 64);
+  const long long most = std::max(1LL, (long long)(std::min(bytes, kWeighBytes) / weigh_part_bytes(std::max(1LL, blocks))));
   if (R > 64 && groups * steps >= 1024) {
     long long best = 0;
     WeighPlan plan{true, 1};
-    for (long long n = 1; n <= std::min(64LL, steps); ++n) {
+    for (long long n = 1; n <= std::min({64LL, steps, most}); ++n) {
       const long long t = (groups * n + 511) / 512 * ((steps + n - 1) / n + 3);
       if (n > 1 && t >= best) continue;
       best = t;
@@ -330,7 +334,7 @@ WeighPlan weigh_plan(int Hkv, int R, long long blocks) {
     return plan;
   }
   const long long units = (long long)Hkv * ((R + 31) / 32);
-  return {false, (int)std::max(1LL, std::min(units / 16, (1024 + blocks - 1) / std::max(1LL, blocks)))};
+  return {false, (int)std::max(1LL, std::min({units / 16, (1024 + blocks - 1) / std::max(1LL, blocks), most}))};
 }
 
 }  // namespace mw

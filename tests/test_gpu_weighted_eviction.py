@@ -406,3 +406,28 @@ def test_refusals_of_the_binding(mw):
             mw.mw_kvpages_weigh(cache, [0, 1], q, lse, w, workspace=ws)
         with pytest.raises(mw.MWError):
             mw.mw_kvpages_evict_weighted(cache, [0, 1], w, 50, workspace=ws)
+
+
+@pytest.mark.parametrize("H,T,n", [(8, 700, 3000), (256, 40, 500)])
+def test_weights_with_a_workspace_of_another_size(mw, H, T, n):
+    """One sized for other lengths: smaller ones divide the rows into what fits, larger ones change nothing."""
+    import torch
+    Hkv, D = 4, 64
+    cache, model = make(mw, 120, Hkv, 64, D, 1, 50)
+    k, v = randn((1, Hkv, n, D), 41), randn((1, Hkv, n, D), 51)
+    mw.mw_kvpages_append(cache, [0], k, v)
+    model.append([0], k, v)
+    q = randn((1, H, T, D), 60)
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, [0], want_lse=True)
+    need, one = mw.mw_kvpages_weigh_workspace_size(cache, [0], H, T), -(-n // 64) * 256
+    assert need >= 3 * one
+    whole = weights_of(mw, cache, model, [0], q, lse, H, add=False)
+    for nbytes in (need + 1024, need, need - 16, 2 * one, 2 * one - 16, one, 16):
+        print(f"[case] weigh {n} tokens, workspace of {nbytes} of {need} bytes", flush=True)
+        space = torch.full((nbytes + 256,), 255, dtype=torch.uint8, device="cuda")  # (as fp32: NaN)
+        w = weights_of(mw, cache, model, [0], q, lse, H, add=False, workspace=space[:nbytes])
+        parts = int((~space[:nbytes // 4 * 4].view(torch.float32).isnan()).sum()) // n
+        assert parts == 0 if nbytes < 2 * one else 2 <= parts <= nbytes // one
+        assert bool((space[nbytes:] == 255).all())
+        if nbytes >= need:
+            assert torch.equal(w, whole)

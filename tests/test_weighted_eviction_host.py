@@ -91,3 +91,19 @@ def test_workspace_sizes():
     f = lambda H, T, *s: mw.load().mw_kvpages_weigh_workspace_size(ctypes.byref(c.c), seqs(*s), len(s), H, T)
     hold(c, 0, 5000)
     assert f(2, 1, 0) == 0 and f(2, 4000, 0) > 0 and f(3, 4000, 0) == 0
+
+
+def test_no_workspace_for_weights_is_above_its_limit():
+    """At any lengths, which it does not grow with: one of 64 MiB serves every call."""
+    c = Cache(L=1024, W=10000, P=40000)
+    f = lambda H, T, *s: mw.load().mw_kvpages_weigh_workspace_size(ctypes.byref(c.c), seqs(*s), len(s), H, T)
+    sizes = {}
+    for n in (1, 64, 5000, 19200, 64000, 131072, 133000, 700_000, 4_000_000):
+        c = Cache(L=1024, W=10000, P=40000)
+        hold(c, 0, n)
+        hold(c, 1, n // 3 + 1)
+        for H, T in ((2, 1), (2, 40), (16, 4800), (128, 60000), (2, 1 << 20)):
+            for s in ((0,), (1, 0)):
+                size = sizes[n, H, s] = f(H, T, *s)
+                assert 0 <= size <= 64 << 20 and size % 256 == 0
+    assert any(sizes[a, H, s] > sizes[b, H, s] for a, H, s in sizes for b in (700_000, 4_000_000) if a < b)
