@@ -699,7 +699,7 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
  *     weights[s][j] (+)= sum_{h, t} exp(scale q[b, h, t] . k_j - lse[b, h, t]),  s = seqs[b]
  * q       : bf16 [n_seqs, H, T, D] view (strides: 1 entry, NULL = contiguous) and
  * lse     : fp32 [n_seqs, H, T] as given to and left by that call, over the same cached tokens
- *           (a row of LSE -inf weighs nothing)
+ *           (a row of LSE -inf weighs nothing, whatever its query holds)
  * weights : fp32 [N, W * L], a row for each sequence; entries behind its length are left as
  *           they were.  add = 1: added to what is there; 0: written.  They are the caller's: fork,
  *           copy, free and evict do not move them.

@@ -145,6 +145,12 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_kernel(WeighParams p, WeighS
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(kf[kb][kk], qf[kk], s[kb]);
+    if (wave_any(lse == -INFINITY)) {  // (whatever their queries hold)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = lse == -INFINITY ? 0.f : s[kb][i];
+    }
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -161,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_kernel(WeighParams p, WeighS
 }
 
 // Many rows: a workgroup takes NW blocks of a member, one a wave, and one part of the pairs (key head, step of 64 rows),
-// whose Q and LSE it stages in LDS for all of them, a step ahead (reading Q anew for each block: the 1B stream step below 718
+// whose Q it stages in LDS for all of them, a step ahead (reading Q anew for each block: the 1B stream step below 718
 // us).  Bound by the exponentials, 16 of 24 cycles of vector work an element, next to 16 of matrix work: vector work 65%,
 // matrix units 53% busy, with what a wave waits for between them.  12 heads x 4800 rows of a guidance pair over 14700 and
 // 11025 tokens, D = 128: 367 us, 1034 TF.
@@ -170,7 +176,6 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
   constexpr int KK = (D + 15) / 16, NT = 64 * NW, BS = 64;
   constexpr int TE = stage_elems<D, BS, NT>();
   __shared__ __attribute__((aligned(16))) bf16_t Qs[2][TE];
-  __shared__ float lse_s[2][BS];
   __shared__ float sums[NW][64];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -191,7 +196,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
   const int beg = (int)(units * part / p.n_parts), end = (int)(units * (part + 1) / p.n_parts);
   const FragOffsets<D> fo(lane, 0);
   const RowOffsets<D, BS, NT> ro(p.sq.t, tid);
-  const long long lse_b = (long long)b * p.Hkv * G * p.T;
+  const float* lse_b = p.lse + (long long)b * p.Hkv * G * p.T;
+  float lse_row = 0.f;  // of the staged step's row `lane`
   auto stage = [&](int u, int buf) {
     const int hk = u / steps, r0 = (u - hk * steps) * BS;
     const bf16_t* base = p.q + b * p.sq.b + (long long)hk * G * p.sq.h;
@@ -202,10 +208,8 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
     } else {
       stage_rows_direct<D, BS, NT>(Qs[buf], [&](int r) { return p.q + row_offset(p.sq, b, hk, G, min(r0 + r, p.R - 1)); }, tid);
     }
-    if (wave == 0) {
-      const int r = min(r0 + lane, p.R - 1), t = G == 1 ? r : r / G;
-      dma_lds_4(p.lse + lse_b + (long long)(hk * G + r - t * G) * p.T + t, lds_addr(lse_s[buf]));
-    }
+    const int r = min(r0 + lane, p.R - 1), t = G == 1 ? r : r / G;
+    lse_row = lse_b[(long long)(hk * G + r - t * G) * p.T + t];
   };
   f32x16 acc[2] = {zero16(), zero16()};
   bf16x8 kf[2][KK];
@@ -225,8 +229,20 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
     }
     wait_vmem();
     __syncthreads();  // this step has landed, and the other stage has been read
+    const bool none = lse_row == -INFINITY;
+    // rows behind the last one, and rows that saw nothing, weigh nothing; both half waves take rows 0..31, then 32..63
+    const unsigned bits = __float_as_uint(r0 + lane < p.R && !none ? lse_row * 1.4426950408889634f : INFINITY);
+    const auto lse2 = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
     if (u + 1 < end) stage(u + 1, buf ^ 1);
     if (busy) {
+      // queries of rows that saw nothing may hold anything: each wave clears them before it reads (D = 72: also row 0's first
+      // columns behind the last row, which that one's read runs into)
+      if (__builtin_expect(wave_any(none), 0)) {
+#pragma unroll 1
+        for (int i = 0; i < D / 8; ++i)
+          if (none) *reinterpret_cast<bf16x8*>(Qs[buf] + lane * D + 8 * i) = bf16x8{};
+        if (D % 16 != 0 && lane == 0 && none) *reinterpret_cast<bf16x8*>(Qs[buf] + BS * D) = bf16x8{};
+      }
 #pragma unroll
       for (int qb = 0; qb < BS / 32; ++qb) {
         f32x16 s[2] = {zero16(), zero16()};
@@ -238,13 +254,10 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
           for (int kb = 0; kb < 2; ++kb) s[kb] = mfma32(kf[kb][kk], qf, s[kb]);
         }
         __builtin_amdgcn_s_setprio(0);
-        const int row = qb * 32 + (lane & 31);
-        const float lse = lse_s[buf][row];
-        const float lse2 = r0 + row < p.R && lse != -INFINITY ? lse * 1.4426950408889634f : INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[kb][i] += fast_exp2(fmaf(s[kb][i], p.scale_log2, -lse2));
+          for (int i = 0; i < 16; ++i) acc[kb][i] += fast_exp2(fmaf(s[kb][i], p.scale_log2, -__uint_as_float(lse2[qb])));
       }
     }
     buf ^= 1;

@@ -431,3 +431,28 @@ def test_weights_with_a_workspace_of_another_size(mw, H, T, n):
         assert bool((space[nbytes:] == 255).all())
         if nbytes >= need:
             assert torch.equal(w, whole)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("H,Hkv,T,n", [(4, 2, 40, 100), (8, 8, 600, 3000), (6, 2, 400, 5000)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_rows_that_weigh_nothing_may_hold_anything(mw, D, H, Hkv, T, n, bad):
+    """Rows of LSE -inf, next to others and in rows of their own: the weights are those with any other queries there."""
+    import torch
+    cache, model = make(mw, 2 * n // 64 + 4, Hkv, 64, D, 2, n // 64 + 1)
+    for s, m in enumerate((n, n // 3)):
+        mw.mw_kvpages_append(cache, [s], randn((1, Hkv, m, D), 1 + s), randn((1, Hkv, m, D), 3 + s))
+    q = randn((2, H, T, D), 5, "bthd")
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, [0, 1], want_lse=True)
+    none = torch.zeros((2, H, T), dtype=torch.bool, device="cuda")
+    none[0, :, 1::2] = none[1, 0] = none[1, :, -5:] = none[1, 1, 7] = True
+    none[0, -1, 30:] = True
+    lse[none] = -math.inf
+    runs = []
+    for x in (q, torch.where(none[..., None], bad, q.float()).bfloat16()):
+        w = torch.zeros((2, cache.desc.W * 64), device="cuda")
+        mw.mw_kvpages_weigh(cache, [0, 1], x, lse, w)
+        runs.append(w)
+    torch.cuda.synchronize()
+    assert bool(runs[0].isfinite().all()) and bool((runs[0][0, :n] > 0).any())
+    assert torch.equal(*runs)
