@@ -544,3 +544,44 @@ def test_refusals_of_the_binding(mw):
         mw.Packed(edges([T]), T, 3, 2, D)
     with pytest.raises(mw.MWError):
         mw.Packed(edges([T]), T, H, H, 96)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("scale", [8.0, 1e-4])
+@pytest.mark.parametrize("nk,nq,chunk", [([300, 40], None, 1), ([700, 200], [90, 200], 50)])
+def test_gradients_at_large_and_small_scales(mw, D, scale, nk, nq, chunk):
+    """LSE of some hundreds, and of nearly equal scores.  Beside the roundings that attention64 counts, a probability is off by
+    those of its score and of the LSE in 32 bits: the score's sum 2^-22 of its products' magnitudes, LSE and LSE log2 e half a step
+    each and their difference with the score one (together 2^-22 of |LSE| and the magnitudes), and the LSE's own error, in
+    which the scores' come again."""
+    import torch
+    H, Hkv = 4, 2
+    nq_ = nk if nq is None else nq
+    Tq, Tk, G = sum(nq_), sum(nk), H // Hkv
+    q, do = randn((Tq, H, D), 1), randn((Tq, H, D), 2)
+    k, v = randn((Tk, Hkv, D), 3), randn((Tk, Hkv, D), 4)
+    pack = mw.Packed(edges(nq_), Tq, H, Hkv, D, chunk_len=chunk, cu_k=edges(nk), total_k=Tk, backward=True)
+    o, lse = mw.mw_packed_attn_fwd(q, k, v, pack, scale=scale)
+    got = dict(zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *mw.mw_packed_attn_bwd(q, k, v, o, do, lse, pack, scale=scale))))
+    torch.cuda.synchronize()
+    q0 = k0 = 0
+    for s, (a, b) in enumerate(zip(nq_, nk)):
+        i, j = slice(q0, q0 + a), slice(k0, k0 + b)
+        q0, k0 = q0 + a, k0 + b
+        hidden = hidden_of(a, b, chunk).repeat(G, 1)
+        for hk in range(Hkv):
+            h = slice(hk * G, (hk + 1) * G)
+            rows = lambda t: t[i, h].transpose(0, 1).reshape(G * a, -1).double()
+            x, y, g, c = rows(q), rows(do), k[j, hk].double(), v[j, hk].double()
+            want = attention64(x, g, c, hidden, scale, y)
+            p = torch.exp(((x @ g.t()) * scale).masked_fill(hidden, -math.inf) - want["lse"][0][:, None])
+            size = scale * (x.abs() @ g.abs().t())
+            off = p * 2.0 ** -21 * (size + size.masked_fill(hidden, 0).amax(-1, keepdim=True) + want["lse"][0].abs()[:, None])
+            off_o = off @ c.abs()
+            off_ds = off * ((y @ c.t()) - (y * want["o"][0]).sum(-1, keepdim=True)).abs() + p * (y.abs() * off_o).sum(-1, keepdim=True)
+            more = {"o": off_o, "lse": torch.zeros_like(want["lse"][1]), "dq": scale * off_ds @ g.abs(),
+                    "dk": scale * off_ds.t() @ x.abs(), "dv": off.t() @ y.abs()}
+            for name, (value, bound) in want.items():
+                z = got[name]
+                z = z[j, hk] if name in ("dk", "dv") else z[h, i].reshape(-1) if name == "lse" else rows(z)
+                check(f"{name} s={s} hk={hk}", z, value, bound + more[name])

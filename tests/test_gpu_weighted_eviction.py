@@ -456,3 +456,29 @@ def test_rows_that_weigh_nothing_may_hold_anything(mw, D, H, Hkv, T, n, bad):
     torch.cuda.synchronize()
     assert bool(runs[0].isfinite().all()) and bool((runs[0][0, :n] > 0).any())
     assert torch.equal(*runs)
+
+
+@pytest.mark.parametrize("k", [5, 40, 100, 140])
+def test_a_nan_is_lighter_than_minus_infinity(mw, k):
+    """Rows of both, and of finite weights, so that the cut falls within each of the three."""
+    import torch
+    cache, _ = filled(mw, [200], 2, 64, 64, 1, 4, 12)
+    g = torch.Generator().manual_seed(k)
+    kind = torch.randint(0, 3, (256,), generator=g)
+    w = torch.where(kind == 0, math.nan, torch.where(kind == 1, -math.inf, -torch.rand(256, generator=g)))
+    order = sorted(range(3, 190), key=lambda j: (bool(w[j].isnan()), 0.0 if w[j].isnan() else -float(w[j]), j))
+    stay = sorted([0, 1, 2, *order[:k], *range(190, 200)])
+    got = w.cuda()[None].clone()
+    before = [cache.k_pages.clone(), cache.k_scales.clone()]
+    rows = [cache.page_of(0, i) for i in range(4)]
+    mw.mw_kvpages_evict_weighted(cache, [0], got, k + 13, first=3, recent=10)
+    torch.cuda.synchronize()
+    want = torch.zeros(256)
+    want[:k + 13] = w[stay]
+    want[200:] = w[200:]
+    assert torch.equal(got[0].cpu().nan_to_num(nan=1e9), want.nan_to_num(nan=1e9))
+    value = lambda pages, scales, p, t: pages[p, :, t].view(torch.float8_e4m3fn).float() * scales[p]
+    for i, j in enumerate(stay):
+        new = value(cache.k_pages, cache.k_scales, cache.page_of(0, i // 64), i % 64)
+        step = cache.k_scales[cache.page_of(0, i // 64)] * 2.0 ** -10  # (codes that become subnormal)
+        assert bool(((new - value(*before, rows[j // 64], j % 64)).abs() <= step).all()), (i, j)
