@@ -589,14 +589,15 @@ int mw_rope_bands_init(mw_rope_bands* out, const mw_rope_band* bands, int n_band
  * (inverse = 1): the gradients of q and k from those of the outputs.
  * q, q_out : bf16 [B, H, T, D];  k, k_out : bf16 [B, Hkv, T, D], or both NULL
  *            (an output may be its input, with the same strides; else they must not overlap)
- * positions: device integers of pos_bytes = 4 or 8 bytes, any value; of axis a, member b and
+ * positions: device integers of pos_bytes = 4 or 8 bytes; of axis a, member b and
  *            token t at a * pos_strides->h + b * pos_strides->b + t * pos_strides->t (in
  *            integers; strides of 0 share them); or NULL: first + t (bands of one axis)
  * strides  : 4 entries, for q, k, q_out, k_out (NULL = all contiguous)
  * D        : 64, 72 or 128.
  * Arithmetic: the turns in 64 bits, sine, cosine and products in 32, outputs rounded to bf16
- * (nearest even) once.  The calling thread's current device must be the device of the stream
- * and of the tensors.
+ * (nearest even) once.  An angle is off by at most |p| 2^-50 + 2^-22 radians (theta >= 1): bf16's
+ * rounding (2^-8) outweighs that up to |p| = 2^40 or so; far beyond it the outputs say nothing.
+ * The calling thread's current device must be the device of the stream and of the tensors.
  * Errors: MW_EINVAL (null, bands not initialised or beyond D, sizes < 1, several axes
  * without positions), MW_EALIGN, MW_EUNSUPPORTED (D; T > 2^24, B * T >= 2^30, H > 2^14), MW_EHIP. */
 int mw_rope_apply(const void* q, const void* k, void* q_out, void* k_out, const mw_rope_bands* bands, const void* positions,

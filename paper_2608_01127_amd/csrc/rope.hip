@@ -2,10 +2,12 @@
 // pairs (a, b) of up to four bands of the head, t the token's position on the band's axis times the pair's frequency.
 //
 // Bound by HBM: every element is read and written once.  A workgroup takes a few tokens of many heads of both tensors, so
-// that an angle is worked out once for all of them: the turns pos * f / 2 pi in 64 bits, of which the fraction is exact
-// for any position, then sine and cosine of it in 32 bits.  19200 tokens of 24 heads of q and k, D = 128, three bands, 236 MB:
-// 44 to 48 us, 4.9 to 5.3 TB/s (a copy of 1 GiB: 5.15; 50.5 us with a row's token and head found by divisions, whose
-// instructions kept the vector units busy all the time).  Eight tokens take 5 us, a launch.
+// that an angle is worked out once for all of them: the turns pos * f / 2 pi in 64 bits, their fraction (that step is exact),
+// then sine and cosine of it in 32 bits.  The turns are off by a few 2^-53 of themselves (exponent, power, 2 pi, position,
+// product), so the angle by |pos| 2^-50 at most (theta >= 1), more than the 2^-22 of 32 bits from |pos| = 2^28 on.
+// 19200 tokens of 24 heads of q and k, D = 128, three bands, 236 MB: 44 to 48 us, 4.9 to 5.3 TB/s (a copy of 1 GiB: 5.15;
+// 50.5 us with a row's token and head found by divisions, whose instructions kept the vector units busy all the time).
+// Eight tokens take 5 us, a launch.
 #include "mw_device.h"
 #include "mw_kernels.h"
 

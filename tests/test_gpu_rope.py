@@ -299,3 +299,32 @@ def test_refusals_of_the_binding(mw):
         mw.mw_rope_apply(q, k, two)
     with pytest.raises(mw.MWError):  # an output in its input's place, with other strides
         mw.mw_rope_apply(q, k, rb, q_out=q.as_strided(q.shape, (9600, 64, 192, 1)))
+
+
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("factor", [1.0, 8.0])
+def test_far_positions(mw, halves, factor):
+    """Positions beyond 2^31 against angles of 60 digits: off by |position| 2^-50 radians at most (the roundings of the exponent, the
+    power, 2 pi, the position and the product with it, 2^-53 of the angle each and 2^-52 for the power), and 2^-21 for the 32-bit part."""
+    import torch
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+    D, H = 64, 3
+    pos = [0, 1, -1, 2**31 - 1, 2**31, -2**31 - 1, 2**32 + 12345, 10**10 + 7, -(10**11) - 3, 2**38 + 1, -2**40 + 1, 2**40 + 987654321]
+    f = [Decimal(10000) ** (Decimal(-2 * i) / D) / Decimal(factor) for i in range(D // 2)]
+    angle = torch.tensor([[float((p * x) % (2 * pi)) for x in f] for p in pos], dtype=torch.float64)
+    x = randn((1, H, len(pos), D), 70)
+    rb = mw.rope_bands([dict(dim_offset=0, dim_count=D, factor=factor)], halves=halves)
+    p = torch.tensor(pos, device="cuda")
+    got = mw.mw_rope_apply(x, None, rb, p)[0]
+    one = torch.stack([mw.mw_rope_apply(x[:, :, i:i + 1], None, rb, first=n)[0][:, :, 0] for i, n in enumerate(pos)], 2)
+    torch.cuda.synchronize()
+    assert torch.equal(got, one)
+    c, s = angle.cos().cuda(), angle.sin().cuda()
+    e = torch.arange(D // 2, device="cuda")
+    a, b = (e, e + D // 2) if halves else (2 * e, 2 * e + 1)
+    xa, xb = x.double()[..., a], x.double()[..., b]
+    off = (xa.abs() + xb.abs()) * (2.0 ** -21 + p.double().abs()[:, None] * 2.0 ** -50)
+    for at, y in ((a, xa * c - xb * s), (b, xb * c + xa * s)):
+        assert bool(((got.double()[..., at] - y).abs() <= 2.0 ** -8 * y.abs() + off).all())
