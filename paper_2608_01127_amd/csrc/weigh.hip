@@ -270,7 +270,6 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
 }
 
 // Sums of the parts, in order.
-template <int D>
 __global__ __launch_bounds__(256) void weigh_join_kernel(WeighParams p, WeighSeqs seqs) {
   const int id = blockIdx.x * 256 + threadIdx.x, range = id / 64, n = seqs.first[p.B];
   if (range >= n) return;
@@ -313,7 +312,7 @@ hipError_t launch_weigh_dim(const WeighParams& p, const WeighSeqs& seqs, hipStre
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_parts == 1) return e;
-  hipLaunchKernelGGL(weigh_join_kernel<D>, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, stream, p, seqs);
+  hipLaunchKernelGGL(weigh_join_kernel, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0, stream, p, seqs);
   return hipGetLastError();
 }
 
