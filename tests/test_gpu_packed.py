@@ -585,3 +585,65 @@ def test_gradients_at_large_and_small_scales(mw, D, scale, nk, nq, chunk):
                 z = got[name]
                 z = z[j, hk] if name in ("dk", "dv") else z[h, i].reshape(-1) if name == "lse" else rows(z)
                 check(f"{name} s={s} hk={hk}", z, value, bound + more[name])
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("H,lens,nq", [(257, [40, 3], None), (4096, [9], None), (16384, [70, 2], [3, 2])])
+def test_many_heads_of_a_key_head(mw, D, H, lens, nq):
+    """Tiles and steps that hold a part of one token's heads."""
+    verify(mw, lens, H, 1, D, nq=nq, seed=H)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("H,Hkv", [(16384, 16384), (16383, 5461)])
+def test_many_key_heads(mw, D, H, Hkv):
+    """More key heads than places for workgroups; some of them against 64-bit values."""
+    import torch
+    lens, T, G = [1, 0, 66, 5], 72, H // Hkv
+    q, do = randn((T, H, D), 1), randn((T, H, D), 2)
+    k, v = randn((T, Hkv, D), 3), randn((T, Hkv, D), 4)
+    pack = mw.Packed(edges(lens), T, H, Hkv, D, backward=True)
+    o, lse = mw.mw_packed_attn_fwd(q, k, v, pack)
+    dq, dk, dv = mw.mw_packed_attn_bwd(q, k, v, o, do, lse, pack)
+    torch.cuda.synchronize()
+    at = 0
+    for n in lens:
+        i = slice(at, at + n)
+        at += n
+        for hk in (0, 1, Hkv // 2, Hkv - 2, Hkv - 1) if n else ():
+            h = slice(hk * G, (hk + 1) * G)
+            rows = lambda t: t[i, h].transpose(0, 1).reshape(G * n, -1)
+            want = attention64(rows(q), k[i, hk], v[i, hk], hidden_of(n, n, 1).repeat(G, 1), D ** -0.5, rows(do))
+            got = dict(o=rows(o), lse=lse[h, i].reshape(-1), dq=rows(dq), dk=dk[i, hk], dv=dv[i, hk])
+            for name, (value, bound) in want.items():
+                check(f"{name} n={n} hk={hk}", got[name], value, bound)
+
+
+def test_as_many_sequences_as_there_may_be(mw):
+    """2^16 of them, one token or none each, but for a few: every row's output is that of its own keys."""
+    import torch
+    N, H, D = 1 << 16, 2, 64
+    g = torch.Generator().manual_seed(3)
+    lens = torch.randint(0, 2, (N,), generator=g)
+    lens[[0, 1000, 65535]] = torch.tensor([3, 300, 129])
+    T = int(lens.sum())
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)]).to(torch.int32).cuda()
+    q, k, v, do = (randn((T, H, D), 30 + i) for i in range(4))
+    pack = mw.Packed(cu, T, H, H, D, backward=True)
+    o, lse = mw.mw_packed_attn_fwd(q, k, v, pack)
+    dq, dk, dv = mw.mw_packed_attn_bwd(q, k, v, o, do, lse, pack)
+    torch.cuda.synchronize()
+    one = torch.repeat_interleave(lens, lens).cuda() == 1
+    assert torch.equal(o[one], v[one]) and torch.equal(dv[one], do[one])
+    s = (q.double() * k.double()).sum(-1) / 8
+    assert bool(((lse.t().double() - s).abs()[one] <= 2.0 ** -20 * (1 + s.abs() + (q.double() * k.double()).abs().sum(-1) / 8)[one]).all())
+    # (dP - Delta is rounding: sums of 64 products in 32 bits, in two orders)
+    size = (do.double().abs() * v.double().abs()).sum(-1, keepdim=True) * 2.0 ** -18
+    assert bool((dq.double().abs() <= size * k.double().abs())[one].all()) and bool((dk.double().abs() <= size * q.double().abs())[one].all())
+    for s in (0, 1000, 65535):
+        i = slice(int(cu[s]), int(cu[s + 1]))
+        n = i.stop - i.start
+        for h in range(H):
+            want = attention64(q[i, h], k[i, h], v[i, h], hidden_of(n, n, 1), 0.125, do[i, h])
+            for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+                check(f"{name} s={s} h={h}", t[i, h], *want[name])

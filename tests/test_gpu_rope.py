@@ -328,3 +328,21 @@ def test_far_positions(mw, halves, factor):
     off = (xa.abs() + xb.abs()) * (2.0 ** -21 + p.double().abs()[:, None] * 2.0 ** -50)
     for at, y in ((a, xa * c - xb * s), (b, xb * c + xa * s)):
         assert bool(((got.double()[..., at] - y).abs() <= 2.0 ** -8 * y.abs() + off).all())
+
+
+@pytest.mark.parametrize("form", ["interleaved", "halves", "odd halves"])
+@pytest.mark.parametrize("B,H,Hkv,T,layout", [(1, 16384, 3, 2, "bhtd"), (2, 5, 16384, 3, "bthd"), (70000, 2, 1, 1, "bhtd"),
+                                              (1, 3000, 3000, 17, "bhtd")])
+def test_many_heads_and_members(mw, form, B, H, Hkv, T, layout):
+    import torch
+    D = 72
+    bands, halves, gain = FORMS[form](D)
+    axes = 1 + max(b.get("axis", 0) for b in bands)
+    rb = mw.rope_bands(bands, halves=halves, gain=gain)
+    q, k = randn((B, H, T, D), 60, layout), randn((B, Hkv, T, D), 61, layout)
+    pos = positions(axes, B, T, "members", torch.int32)
+    qo, ko = mw.mw_rope_apply(q, k, rb, pos)
+    torch.cuda.synchronize()
+    rows = pos if axes > 1 else pos[None]
+    verify(qo, want64(q, bands, halves, gain, rows))
+    verify(ko, want64(k, bands, halves, gain, rows))

@@ -482,3 +482,41 @@ def test_a_nan_is_lighter_than_minus_infinity(mw, k):
         new = value(cache.k_pages, cache.k_scales, cache.page_of(0, i // 64), i % 64)
         step = cache.k_scales[cache.page_of(0, i // 64)] * 2.0 ** -10  # (codes that become subnormal)
         assert bool(((new - value(*before, rows[j // 64], j % 64)).abs() <= step).all()), (i, j)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_weights_of_many_heads_of_a_key_head(mw, D):
+    cache, model = make(mw, 12, 1, 64, D, 2, 6)
+    for s, n in enumerate((300, 65)):
+        k, v = randn((1, 1, n, D), 1 + s), randn((1, 1, n, D), 3 + s)
+        mw.mw_kvpages_append(cache, [s], k, v)
+        model.append([s], k, v)
+    for H, T in ((16384, 1), (257, 3), (4095, 2)):
+        q = randn((2, H, T, D), 5, "bthd")
+        _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, T, cache, [1, 0], want_lse=True)
+        weights_of(mw, cache, model, [1, 0], q, lse, H, old=0.5)
+
+
+def test_as_many_sequences_as_a_call_names(mw):
+    """256 of them, several empty or short; runs of pages in several launches; one token that stays of each."""
+    H, D, L = 1, 64, 64
+    lens = [(37 * s) % 201 for s in range(256)]
+    cache, model = filled(mw, lens, H, L, D, 256, 5, 1400)
+    q = randn((256, 2, 3, D), 5)
+    seqs = [(s * 101 + 7) % 256 for s in range(256)]
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, 3, cache, seqs, want_lse=True)
+    weights_of(mw, cache, model, seqs, q, lse, 2, add=False)
+    w = some_weights(cache, 3)
+    evict(mw, cache, model, seqs, w, 130, 65, 30)
+    evict(mw, cache, model, seqs, w, 1)
+
+
+def test_pages_of_the_largest_size(mw):
+    """65536 tokens a page: blocks are found by a product's high word."""
+    H, D, L = 1, 64, 1 << 16
+    cache, model = filled(mw, [70_001, 131_072], H, L, D, 2, 2, 8)
+    q = randn((2, 3, 2, D), 5)
+    q = (q.float() / 256).bfloat16()
+    _, lse = mw.mw_chunk_attn_paged(q, None, None, 1, 2, cache, [0, 1], want_lse=True)
+    weights_of(mw, cache, model, [0, 1], q, lse, 3, add=False)
+    evict(mw, cache, model, [1, 0], some_weights(cache, 4), 65_999, 65_537, 200)
