@@ -208,8 +208,9 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
     } else {
       stage_rows_direct<D, BS, NT>(Qs[buf], [&](int r) { return p.q + row_offset(p.sq, b, hk, G, min(r0 + r, p.R - 1)); }, tid);
     }
-    const int r = min(r0 + lane, p.R - 1), t = G == 1 ? r : r / G;
-    lse_row = lse_b[(long long)(hk * G + r - t * G) * p.T + t];
+    const int t0 = G == 1 ? r0 : (unsigned)r0 / (unsigned)G, x = r0 - t0 * G + min(lane, p.R - 1 - r0);
+    const int t = G == 1 ? x : __umulhi((unsigned)x, p.magic);
+    lse_row = lse_b[(long long)(hk * G + x - t * G) * p.T + t0 + t];
   };
   f32x16 acc[2] = {zero16(), zero16()};
   bf16x8 kf[2][KK];
@@ -233,16 +234,16 @@ __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p,
     // rows behind the last one, and rows that saw nothing, weigh nothing; both half waves take rows 0..31, then 32..63
     const unsigned bits = __float_as_uint(r0 + lane < p.R && !none ? lse_row * 1.4426950408889634f : INFINITY);
     const auto lse2 = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    // queries of rows that saw nothing may hold anything: each wave clears them before it reads (D = 72: also row 0's first
+    // columns behind the last row, which that one's read runs into)
+    if (__builtin_expect(wave_any(none), 0)) {
+#pragma unroll 1
+      for (int i = 0; i < D / 8; ++i)
+        if (none) *reinterpret_cast<bf16x8*>(Qs[buf] + lane * D + 8 * i) = bf16x8{};
+      if (D % 16 != 0 && lane == 0 && none) *reinterpret_cast<bf16x8*>(Qs[buf] + BS * D) = bf16x8{};
+    }
     if (u + 1 < end) stage(u + 1, buf ^ 1);
     if (busy) {
-      // queries of rows that saw nothing may hold anything: each wave clears them before it reads (D = 72: also row 0's first
-      // columns behind the last row, which that one's read runs into)
-      if (__builtin_expect(wave_any(none), 0)) {
-#pragma unroll 1
-        for (int i = 0; i < D / 8; ++i)
-          if (none) *reinterpret_cast<bf16x8*>(Qs[buf] + lane * D + 8 * i) = bf16x8{};
-        if (D % 16 != 0 && lane == 0 && none) *reinterpret_cast<bf16x8*>(Qs[buf] + BS * D) = bf16x8{};
-      }
 #pragma unroll
       for (int qb = 0; qb < BS / 32; ++qb) {
         f32x16 s[2] = {zero16(), zero16()};
