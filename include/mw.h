@@ -486,9 +486,11 @@ int mw_cross_attn_bwd(const void* q, const void* k, const void* v, const int32_t
  *     p >= 0  and  floor(j / chunk_len) <= floor(p / chunk_len)
  * (chunk_len = 1: token-causal; chunk_len >= nk: every query of a place >= 0 sees every
  * key).  With nq = nk this is mw_block_causal_attn_* for each sequence; with nq < nk
- * the newest tokens attend to all before them: nq = 1 is the single token of a
- * generation step.  A query that sees no key has O = 0 and LSE = -inf.  H query heads
- * share Hkv key heads (Hkv divides H): query head h reads key head h / (H / Hkv).
+ * the newest tokens attend to all before them, nq = 1: a single one.  (A sequence's keys
+ * end where the next one's begin, so this suits a context that stays, or one sequence
+ * that grows at the end of k and v; sequences that grow side by side: mw_kvpages.)
+ * A query that sees no key has O = 0 and LSE = -inf.  H query heads share Hkv key heads
+ * (Hkv divides H): query head h reads key head h / (H / Hkv).
  *
  * mw_packed is a batch's plan: which workgroup takes which tiles, worked out on the
  * device from cu_q and cu_k by mw_packed_init, for any number of calls on tensors of
@@ -710,6 +712,8 @@ int mw_kvpages_compact(mw_kvpages* c, mw_stream_t stream);
  *           as they grow; it is never above 64 MiB.
  * Products as in mw_chunk_attn_paged, sums in fp32, deterministic (in an order that the sizes and
  * workspace_bytes decide).
+ * A call of mw_chunk_attn_paged that lists a sequence twice (a guidance pair over one rollout) is
+ * weighed by a call for each of its members that share the sequence, with add = 1.
  * Refuses a stream under HIP graph capture (the host's lengths size the call).
  * Errors: MW_EINVAL (also a sequence listed twice), MW_EALIGN, MW_EUNSUPPORTED, MW_EHIP. */
 size_t mw_kvpages_weigh_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int H, int T);
@@ -726,7 +730,8 @@ int mw_kvpages_weigh(const mw_kvpages* c, const int32_t* seqs, int n_seqs, const
  * again as RNE_e4m3(value / scale), which changes only codes that become subnormal.  The
  * row of weights is moved alike; entries from n_keep up to the old length become 0.
  * weights  : fp32 [N, W * L];  workspace: mw_kvpages_evict_weighted_workspace_size(...) bytes
- * The tokens' keys stay as committed.  All or nothing.
+ * The tokens' keys stay as committed.  All or nothing, but for MW_EHIP, after which the listed rows
+ * of weights are undefined too.
  * Errors: MW_EINVAL (n_keep < 1, first + recent > n_keep, a sequence listed twice, workspace too
  * small), MW_EALIGN, MW_EFULL (too few free pages), MW_EUNSUPPORTED, MW_EHIP. */
 size_t mw_kvpages_evict_weighted_workspace_size(const mw_kvpages* c, const int32_t* seqs, int n_seqs, int n_keep, int first);

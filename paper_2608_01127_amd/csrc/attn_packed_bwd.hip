@@ -1,7 +1,7 @@
 // Backward of the packed attention (gfx950): with P recomputed from Q, K and the forward's LSE,
 //   dV = sum_r P_r^T dO_r,  dP = dO V^T,  Delta = rowsum(dO O),  dS = P (dP - Delta),
 //   dQ = scale dS K,  dK = scale sum_r dS_r^T Q_r
-// over the rows r of a key head (attn_packed.hip).
+// over the rows r of a key head (attn_packed.h).
 //
 //   terms kernel : Delta and LSE log2 e of each row.
 //   grad kernel  : dK and dV, of which a wave owns 32 keys and walks the rows that see them, staged in LDS; and dQ, of which

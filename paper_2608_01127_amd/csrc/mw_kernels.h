@@ -416,7 +416,8 @@ struct PackedJoin {
 // Tiles of 128 rows (or keys), or of 64 in two groups of waves that share each step's keys (or rows), for grids that
 // would leave CUs idle.
 enum class PackedTile { wide, pairs };
-// Workgroups that a CU runs at once (of four waves each, so waves a SIMD).
+// Workgroups that a CU runs at once, as the registers are allocated for (of four waves each, so waves a SIMD).  Tiles of 64
+// rows in fact run four at D = 64 (123 registers) and three at D = 72 (146); the plan prices them as two.
 constexpr int packed_fwd_per_cu(int D, PackedTile t) { return t == PackedTile::wide && D != 128 ? 3 : 2; }
 constexpr int packed_bwd_per_cu(int D, PackedTile rows, PackedTile keys) {
   return D == 64 && rows == PackedTile::wide && keys == PackedTile::wide ? 3 : 2;

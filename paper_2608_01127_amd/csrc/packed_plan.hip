@@ -157,8 +157,8 @@ __device__ __forceinline__ int few_tiles_target(const int* tile_steps, int n_til
 // One workgroup for each list.  Tiles are numbered sequence after sequence; with all steps known, a tile longer than a
 // workgroup's share of them is cut into items of about equal length; the items are put in order of their length, longest
 // first, by counting (items of a bin in any order: the order decides when a workgroup runs, not what it computes).
-// A chain of short phases: 15 us for seven sequences of 19200 tokens in all, 17 with the backward's lists, in one launch;
-// a batch is planned once for all layers.
+// A chain of short phases in one launch: 16 us for seven sequences of 19200 tokens in all, 16 to 20 with the backward's lists,
+// 25 for one token of eight sequences, whose few tiles are priced.  A batch is planned once for all layers.
 __global__ __launch_bounds__(kThreads) void packed_plan_kernel(PlanArgs a) {
   __shared__ int wave_sums[kThreads / 64];
   __shared__ int bins[kBins];

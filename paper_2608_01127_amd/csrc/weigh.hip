@@ -1,5 +1,5 @@
-// Eviction from the paged cache by accumulated attention weight (gfx950): what weight each cached token gets from a
-// call's rows, and the copy of a sequence's anchor, newest and heaviest tokens into pages of their own.
+// Attention weight of the paged cache's tokens (gfx950): what each cached token gets from a call's rows.  keep.hip evicts
+// by it.
 #include <algorithm>
 
 #include "attn_rows.h"
@@ -168,9 +168,9 @@ __global__ __launch_bounds__(64 * NW, 3) void weigh_kernel(WeighParams p, WeighS
 
 // Many rows: a workgroup takes NW blocks of a member, one a wave, and one part of the pairs (key head, step of 64 rows),
 // whose Q it stages in LDS for all of them, a step ahead (reading Q anew for each block: the 1B stream step below 718
-// us).  Bound by the exponentials, 16 of 24 cycles of vector work an element, next to 16 of matrix work: vector work 65%,
+// us).  Bound by the exponentials, 16 of 24 cycles of vector work an element, next to 16 of matrix work: vector work 67%,
 // matrix units 53% busy, with what a wave waits for between them.  12 heads x 4800 rows of a guidance pair over 14700 and
-// 11025 tokens, D = 128: 367 us, 1034 TF.
+// 11025 tokens, D = 128: 354 us, 1072 TF.
 template <int D, int NW, int WPS>
 __global__ __launch_bounds__(64 * NW, WPS) void weigh_rows_kernel(WeighParams p, WeighSeqs seqs) {
   constexpr int KK = (D + 15) / 16, NT = 64 * NW, BS = 64;
@@ -328,8 +328,9 @@ hipError_t launch_weigh(const WeighParams& p, const WeighSeqs& seqs, int D, hipS
 // The kernel of a call and the parts of its rows (over all key heads), so that there are workgroups enough for the card.
 // Staging rows for several blocks pays from 65 rows of a key head on, where there is work for the card (12 heads over 14700
 // tokens, D = 128, us: 64 rows 18.3 few | 42.5 many, 128 29.4 | 19.4, 600 82 | 41; 4 heads x 2000 rows over 300 tokens, D =
-// 64, 13.9 | 22.7).  Its parts are those of the least time in rounds of the 512 workgroups that run at once, each of its
-// steps and a beginning as long as three (always about 768 workgroups: the 1B stream step 386 us, so 367).
+// 64, 13.9 | 22.7).  Its parts are those of the least time in rounds of the 512 workgroups that run at once at D = 128
+// (three a CU at D = 64 and 72, priced as two), each of its steps and a beginning as long as three (always about 768 workgroups:
+// the 1B stream step 386 us, so 367).
 // No more parts than the workspace holds, and never more than kWeighBytes of them (by this count of rounds that costs 1.3%
 // at most in 20000 drawn sizes of up to 2^18 blocks and 2^17 rows; without the limit parts of 750 MB came up).
 WeighPlan weigh_plan(int Hkv, int R, long long blocks, size_t bytes) {
